@@ -374,6 +374,117 @@ typedef struct {
 ravel_status ravel_profile_step(ravel_buffer* buf, const void* fop_tokens, float* action_out,
                                 void* stream, ravel_kernel_record* records, int32_t* n);
 
+/* -------------------------------------------------------------------------
+ * Key/value cache in 8 bits.
+ *
+ * A cache holds, for each of n_seq sequences, the keys and values of up to `capacity` tokens as
+ * e4m3 codes (8-bit floating point, largest value 448) with one 32-bit scale per (sequence, KV
+ * head, block of `block` tokens), for keys and values apart; token t's key is code * scale of
+ * block t / block.  Scales are powers of two from 2^-100 on, the smallest by which the block's
+ * largest magnitude stays within 448 when the block is written: division and products by them
+ * are exact, so a stored value is off by at most half an e4m3 step (2^-4 of it, 2^-10 of the
+ * scale below the format's normal numbers).  All memory is the caller's device memory on the current
+ * device; the struct may be copied and is read during the call only.  k and v must be 16-byte
+ * aligned.  The calls are enqueued on `stream` and allocate nothing; they may be captured into a
+ * graph, and read lengths, indices and positions from device memory when they run.  Calls that
+ * write one sequence must be ordered with every other call on it.
+ *
+ *   seq  [batch] device int32: the sequence of each batch row; NULL: row b is sequence b.  A row
+ *        whose index is outside 0..n_seq-1 (say -1, for padding) takes no part in the call.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+  int32_t n_seq;
+  int32_t n_kv_heads;
+  int32_t head_dim; /* 32, 64, 128 or 256                                      */
+  int32_t capacity; /* tokens of a sequence, 1 .. 2^24                         */
+  int32_t block;    /* tokens of a scale: 16, 32, 64 or 128                    */
+  int32_t reserved; /* 0 */
+  void* k;          /* [n_seq, n_kv_heads, capacity, head_dim] e4m3            */
+  void* v;
+  float* k_scale;   /* [n_seq, n_kv_heads, ceil(capacity / block)]             */
+  float* v_scale;
+  int32_t* len;     /* [n_seq] tokens held (values outside 0..capacity count
+                       as the nearer bound)                                    */
+  float* weight;    /* [n_seq, n_kv_heads, capacity] accumulated attention
+                       weights, or NULL                                        */
+} ravel_cache;
+
+/* Store the keys and values of up to n new tokens per batch row from position pos[b] on (NULL: from
+ * the sequence's length on); the length becomes pos[b] + the tokens stored, so a smaller pos takes
+ * earlier tokens back.  count[b] (NULL: n) of the row's n tokens are stored, clamped to 0..n, and
+ * no more than fit; a row with pos outside 0..capacity is left alone.
+ *   k, v: device, dtype RAVEL_F32 or RAVEL_BF16, element (b, t, h, d) at b * batch_stride +
+ *   t * token_stride + h * head_stride + d (in elements; 16-byte aligned rows: strides multiples
+ *   of 8, or 4 in 32 bits).
+ * A block that also holds older tokens keeps its scale, or, where the new tokens need a larger one,
+ * has its older codes rounded to that.  Infinities become the largest code, NaN stays NaN; neither
+ * counts for the scale.  Accumulated weights of the stored tokens start at 0.  pos and count must
+ * not be the cache's len (but pos == len is taken as NULL).  A sequence that an earlier row names
+ * already is not written again.
+ * Errors: E_INVALID (null pointer, alignment, dtype, block), E_SHAPE (sizes, strides). */
+ravel_status ravel_cache_append(const ravel_cache* cache, int32_t batch, const int32_t* seq, const int32_t* pos,
+                                const int32_t* count, int32_t n, int32_t dtype, const void* k, const void* v,
+                                int64_t batch_stride, int64_t token_stride, int64_t head_stride, void* stream);
+
+/* Attention of `rows` query rows per batch row and head over [cached tokens ; own tokens]: the
+ * sequence's len tokens, then the n_self tokens whose keys and values come with the call in the
+ * queries' dtype (every row sees all of both; query head j uses KV head j / (n_q_heads /
+ * n_kv_heads)).  out = softmax(scale q k) v; scores, softmax and sums in 32 bits, in a bf16 call the
+ * probabilities are rounded to bf16 for the second product and out at the end; in a 32-bit call
+ * products are as good as 32 bits.  A row that sees nothing (len 0 and no own tokens, or no
+ * sequence) is 0.  With track, every cached token's softmax weights, summed over the rows and the
+ * query heads of its KV head, are added to the cache's accumulated weight (batch rows that name one
+ * sequence are added in row order).
+ * Strides in elements, (b, row or token, head); 16-byte aligned vectors (multiples of 8 elements, or
+ * 4 in 32 bits).  workspace: ravel_cache_attention_workspace() bytes, 256-byte aligned, of this call
+ * alone until it has run (NULL when that is 0). */
+typedef struct {
+  int32_t dtype; /* RAVEL_F32 or RAVEL_BF16: q, self_k, self_v, out */
+  int32_t batch;
+  int32_t n_q_heads;
+  int32_t rows;   /* query rows per batch row, >= 1            */
+  int32_t n_self; /* own tokens per batch row, >= 0            */
+  int32_t track;  /* nonzero: add to the accumulated weights   */
+  float scale;    /* of the scores, e.g. 1 / sqrt(head_dim)    */
+  int32_t reserved;
+  const int32_t* seq;
+  const void* q;
+  const void* self_k;
+  const void* self_v;
+  void* out;
+  int64_t q_stride[3];
+  int64_t self_stride[3]; /* of self_k and of self_v */
+  int64_t out_stride[3];
+  void* workspace;
+  int64_t workspace_bytes;
+} ravel_cache_query;
+
+/* Bytes of workspace for such a call (only the sizes of both structs are read), in *bytes. */
+ravel_status ravel_cache_attention_workspace(const ravel_cache* cache, const ravel_cache_query* query, int64_t* bytes);
+/* Errors: E_INVALID (null pointer, alignment, dtype, workspace too small, track without weights),
+ * E_SHAPE (sizes, strides, head counts). */
+ravel_status ravel_cache_attention(const ravel_cache* cache, const ravel_cache_query* query, void* stream);
+
+/* Evict: of each (batch row, KV head) the `keep` tokens with the largest accumulated weights stay (of
+ * equal ones those of lower index; NaN counts as the lowest; the sequence's first `first` tokens stay
+ * in any case), each head its own; a sequence of at most keep tokens loses none.  Kept tokens of index
+ * below keep stay at their places, the others fill the holes in ascending order (attention does not
+ * depend on the order of the tokens); codes, scales and weights go along, and the length becomes
+ * min(len, keep).  A block's scale becomes the largest of its tokens' scales, codes of smaller ones
+ * are rounded to it.
+ *   into NULL: in place.  Otherwise the kept tokens go to sequence into_seq[b] (NULL: b) of that
+ *   cache, which shares no memory with the first, has the same heads, head_dim and block, and a
+ *   capacity of at least min(keep, capacity); the first cache is left as it is.
+ *   kept: [batch, n_kv_heads, keep] device int32: the index each place's token had, -1 for places
+ *   beyond the tokens kept (all of them for a row without a sequence).
+ * workspace: ravel_cache_evict_workspace() bytes, 256-byte aligned, of this call alone until it has
+ * run.  A destination that an earlier row names already is not written again.
+ * Errors: E_INVALID (null pointer, no weights, workspace too small), E_SHAPE (sizes, first > keep). */
+ravel_status ravel_cache_evict_workspace(const ravel_cache* cache, int32_t batch, int32_t keep, int64_t* bytes);
+ravel_status ravel_cache_evict(const ravel_cache* cache, int32_t batch, const int32_t* seq, int32_t keep, int32_t first,
+                               const ravel_cache* into, const int32_t* into_seq, int32_t* kept, void* workspace,
+                               int64_t workspace_bytes, void* stream);
+
 /* Message of the calling thread's last non-OK status ("" if none). */
 const char* ravel_last_error(void);
 

@@ -19,7 +19,8 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libravel.so")
-SOURCES = ["gemm.hip", "gemm_tile.hip", "f32.hip", "attention.hip", "adapter.hip", "elementwise.hip", "persistent.hip", "ravel.hip"]
+SOURCES = ["gemm.hip", "gemm_tile.hip", "f32.hip", "attention.hip", "adapter.hip", "cache.hip", "cache_attention.hip",
+           "cache_api.hip", "elementwise.hip", "persistent.hip", "ravel.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -1,0 +1,471 @@
+// Attention over the 8-bit key/value cache and the call's own keys and values
+// (bidirectional, grouped-query heads), and the accumulated weights of its tokens.
+//
+// The G = nq / nkv query heads that share a kv head are flattened with the rows of the
+// call into one row space (row = h * rows + i, R = G * rows).  Scores are computed
+// transposed, S^T = K Q^T: a lane owns one row and four keys of each 16, its softmax
+// statistics stay in registers, and P^T is the second product's B operand as it stands.
+//
+// Codes are exact as bf16, so both products run on the bf16 matrix instruction with 32-bit
+// sums; the scales (one per at least 16 keys: uniform over a 16-key tile) multiply the
+// scores and the probabilities.  32-bit queries, own keys and values and probabilities are
+// split in three bf16 numbers of 8 significand bits each, which hold them exactly; products
+// of the order 2^-24 and below are left out.
+#include <algorithm>
+
+#include "cache.h"
+
+namespace ravel {
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+// The running maximum of a row moves when a tile raises it by more than this (log2 units):
+// between moves the probabilities stay below 2^8 and nothing is rescaled.
+constexpr float kLazy = 8.f;
+constexpr int NW = 4;  // waves of a block; they take every fourth tile and are joined at the end
+
+RAVEL_DEV f32x4_t mfma_bf16(bf16x8_t a, bf16x8_t b, f32x4_t c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+RAVEL_DEV uint32_t codes2(uint32_t w, bool hi) {  // two of four codes as bf16
+  return __builtin_bit_cast(uint32_t, hi ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, true)
+                                         : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, false));
+}
+RAVEL_DEV bf16x8_t codes8(uint32_t w0, uint32_t w1) {
+  return __builtin_bit_cast(bf16x8_t, (u32x4_t{codes2(w0, false), codes2(w0, true), codes2(w1, false), codes2(w1, true)}));
+}
+// 8 values as NP bf16 planes: one, rounded; or three, cut off after 8 significand bits each
+template <int NP>
+RAVEL_DEV void planes(const float (&x)[8], bf16x8_t (&p)[NP]) {
+  if constexpr (NP == 1) {
+    p[0] = __builtin_bit_cast(bf16x8_t, (u32x4_t{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]),
+                                                 pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])}));
+  } else {
+    float r[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = x[i];
+#pragma unroll
+    for (int n = 0; n < NP; ++n) {
+      u32x4_t w;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t a = __float_as_uint(r[2 * i]), b = __float_as_uint(r[2 * i + 1]);
+        w[i] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+        r[2 * i] -= __uint_as_float(a & 0xFFFF0000u);
+        r[2 * i + 1] -= __uint_as_float(b & 0xFFFF0000u);
+      }
+      p[n] = __builtin_bit_cast(bf16x8_t, w);
+    }
+  }
+}
+// 8 consecutive elements of the model's type as planes
+template <bool F32, int NP>
+RAVEL_DEV void load8(const void* base, long long at, bf16x8_t (&p)[NP]) {
+  if constexpr (F32) {
+    const f32x4_t lo = *(const f32x4_t*)((const float*)base + at), hi = *(const f32x4_t*)((const float*)base + at + 4);
+    const float x[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    planes<NP>(x, p);
+  } else {
+    p[0] = *(const bf16x8_t*)((const bf16_t*)base + at);
+  }
+}
+
+// Partial results of a key range: [split][batch][kv head][row]
+struct Part {
+  float* o;   // [..][hd], unnormalised
+  float* ml;  // [..][2]: maximum (log2 units), sum
+  float* lse;  // [batch][kv head][row]: log2 of the softmax's denominator (track)
+  int nsplit;
+};
+
+// raw codes of a wave's 32-key tile: keys as the A operand's rows, 16 (HD 32: 8) dims a
+// load; values 8 keys x HD / 16 consecutive dims a lane
+template <int HD>
+struct Raw {
+  static constexpr int KC = HD >= 64 ? HD / 64 : 1;
+  static constexpr int VW = HD >= 64 ? HD / 64 : 1;
+  u32x4_t k[2][KC];
+  uint32_t v[8][VW];
+};
+
+template <int HD>
+RAVEL_DEV void load_raw(Raw<HD>& r, const uint8_t* k, const uint8_t* v, int key0, int last, int l16, int grp) {
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const uint8_t* p = k + (long long)min(key0 + 16 * u + l16, last) * HD;
+    if constexpr (HD == 32) {
+      const u32x2_t w = *(const u32x2_t*)(p + grp * 8);
+      r.k[u][0] = u32x4_t{w[0], w[1], 0, 0};
+    } else {
+#pragma unroll
+      for (int c = 0; c < HD / 64; ++c) r.k[u][c] = *(const u32x4_t*)(p + c * 64 + grp * 16);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const uint8_t* p = v + (long long)min(key0 + 16 * (j >> 2) + 4 * grp + (j & 3), last) * HD + l16 * (HD / 16);
+    if constexpr (HD == 32) r.v[j][0] = *(const uint16_t*)p;
+    if constexpr (HD == 64) r.v[j][0] = *(const uint32_t*)p;
+    if constexpr (HD == 128) {
+      const u32x2_t w = *(const u32x2_t*)p;
+      r.v[j][0] = w[0];
+      r.v[j][1] = w[1];
+    }
+    if constexpr (HD == 256) {
+      const u32x4_t w = *(const u32x4_t*)p;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r.v[j][i] = w[i];
+    }
+  }
+}
+
+// dims of the query and key operands' k-step ks, group grp: 8 consecutive from here
+template <int HD>
+RAVEL_DEV int kdim(int ks, int grp) {
+  return HD == 32 ? grp * 8 : (ks >> 1) * 64 + grp * 16 + (ks & 1) * 8;
+}
+
+template <int HD>
+RAVEL_DEV bf16x8_t key_operand(const Raw<HD>& r, int u, int ks) {
+  const u32x4_t w = r.k[u][HD == 32 ? 0 : ks >> 1];
+  return (ks & 1) ? codes8(w[2], w[3]) : codes8(w[0], w[1]);
+}
+
+// byte b of eight words
+RAVEL_DEV bf16x8_t byte8(const uint32_t (&w)[8], int b) {
+  const uint32_t s2 = b == 0 ? 0x0c0c0400u : b == 1 ? 0x0c0c0501u : b == 2 ? 0x0c0c0602u : 0x0c0c0703u;
+  const uint32_t a = __builtin_amdgcn_perm(w[1], w[0], s2), c = __builtin_amdgcn_perm(w[3], w[2], s2);
+  const uint32_t d = __builtin_amdgcn_perm(w[5], w[4], s2), e = __builtin_amdgcn_perm(w[7], w[6], s2);
+  return __builtin_bit_cast(bf16x8_t, (u32x4_t{codes2(a, false), codes2(c, false), codes2(d, false), codes2(e, false)}));
+}
+
+template <int HD, bool F32>
+__global__ __launch_bounds__(NW * 64) void cache_attn_kernel(CacheAttnArgs a, Part part, int chunks) {
+  constexpr int KS = HD / 32, NT = HD / 16, NP = F32 ? 3 : 1;
+  __shared__ __attribute__((aligned(16))) float so[NW][16][HD + 4];
+  __shared__ float sml[NW][16][2];
+  const CacheView& c = a.c;
+  const int split = blockIdx.x % part.nsplit, chunk = blockIdx.x / part.nsplit % chunks;
+  const int bg = blockIdx.x / (part.nsplit * chunks), g = bg % c.nkv, b = bg / c.nkv;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l16 = lane & 15, grp = lane >> 4;
+  const int G = a.nq / c.nkv, R = G * a.rows, row = chunk * 16 + l16;
+  const int id = cache_seq(c, a.seq, b), n = id < 0 ? 0 : cache_len(c, id), S = id < 0 ? 0 : a.n_self;
+  const int ct = (n + 31) >> 5, tiles = ct + ((S + 31) >> 5);
+  const int t0 = (int)((long long)tiles * split / part.nsplit), t1 = (int)((long long)tiles * (split + 1) / part.nsplit);
+  const long long head = (long long)max(id, 0) * c.nkv + g;
+  const uint8_t *kc = c.k + head * c.cap * HD, *vc = c.v + head * c.cap * HD;
+  const float *ksc = c.ks + head * c.nblk, *vsc = c.vs + head * c.nblk;
+
+  bf16x8_t q[KS][NP];
+  {
+    const int r = min(row, R - 1);  // rows past the group are computed and never stored
+    const long long at = b * a.qb + r % a.rows * a.qr + (g * G + r / a.rows) * a.qh;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) load8<F32>(a.q, at + kdim<HD>(ks, grp), q[ks]);
+  }
+  f32x4_t o[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) o[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;
+  const float sl2 = a.scale * kLog2e;
+
+  // x: this lane's scores (log2 units, -inf where masked) of keys 16 u + 4 grp + r; leaves
+  // the probabilities times vs[u] in pl, the operand planes
+  const auto softmax = [&](float (&x)[8], const float (&vs)[2], bf16x8_t (&pl)[NP]) {
+    float mx = x[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) mx = fmaxf(mx, x[i]);
+    if (__any(mx > m + kLazy)) {
+      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+      const float mnew = mx > m + kLazy ? mx : m;
+      const float corr = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mnew);
+      m = mnew;
+      l *= corr;
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) o[t][r] *= corr;
+    }
+    const float mref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = __builtin_amdgcn_exp2f(x[i] - mref);
+    l += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] *= vs[i >> 2];
+    planes<NP>(x, pl);
+  };
+
+  // cached tokens
+  const int c1 = min(t1, ct);
+  Raw<HD> nxt;
+  if (t0 + wave < c1) load_raw(nxt, kc, vc, (t0 + wave) * 32, n - 1, l16, grp);
+  for (int t = t0 + wave; t < c1; t += NW) {
+    const Raw<HD> cur = nxt;
+    if (t + NW < c1) load_raw(nxt, kc, vc, (t + NW) * 32, n - 1, l16, grp);
+    const int key0 = t * 32;
+    const int blk0 = key0 >> c.shift, blk1 = min(key0 + 16, n - 1) >> c.shift;
+    const float k2[2] = {ksc[blk0] * sl2, ksc[blk1] * sl2}, vs[2] = {vsc[blk0], vsc[blk1]};
+    float x[8];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const bf16x8_t kf = key_operand<HD>(cur, u, ks);
+#pragma unroll
+        for (int p = NP - 1; p >= 0; --p) s = mfma_bf16(kf, q[ks][p], s);
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) x[4 * u + r] = key0 + 16 * u + 4 * grp + r < n ? s[r] * k2[u] : -INFINITY;
+    }
+    bf16x8_t pl[NP];
+    softmax(x, vs, pl);
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {  // dim tile i: dims l16 * NT + i
+      uint32_t w[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] = cur.v[j][i >> 2];
+      const bf16x8_t vf = byte8(w, i & 3);
+#pragma unroll
+      for (int p = NP - 1; p >= 0; --p) o[i] = mfma_bf16(vf, pl[p], o[i]);
+    }
+  }
+  // the call's own tokens
+  for (int t = max(t0 + wave, ct + ((t0 + wave - ct) & (NW - 1))); t < t1; t += NW) {
+    const int key0 = (t - ct) * 32;
+    float x[8];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const long long at = b * a.sb + (long long)min(key0 + 16 * u + l16, S - 1) * a.st + g * a.sh;
+      f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        bf16x8_t kf[NP];
+        load8<F32>(a.sk, at + kdim<HD>(ks, grp), kf);
+#pragma unroll
+        for (int i = NP - 1; i >= 0; --i)
+#pragma unroll
+          for (int p = NP - 1 - i; p >= 0; --p) s = mfma_bf16(kf[i], q[ks][p], s);
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) x[4 * u + r] = key0 + 16 * u + 4 * grp + r < S ? s[r] * sl2 : -INFINITY;
+    }
+    bf16x8_t pl[NP];
+    const float one[2] = {1.f, 1.f};
+    softmax(x, one, pl);
+    long long va[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      va[j] = b * a.sb + (long long)min(key0 + 16 * (j >> 2) + 4 * grp + (j & 3), S - 1) * a.st + g * a.sh + l16 * NT;
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      bf16x8_t vf[NP];
+      float y[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        y[j] = F32 ? ((const float*)a.sv)[va[j] + i] : bf16_to_f32(((const bf16_t*)a.sv)[va[j] + i]);
+      planes<NP>(y, vf);
+#pragma unroll
+      for (int k = NP - 1; k >= 0; --k)
+#pragma unroll
+        for (int p = NP - 1 - k; p >= 0; --p) o[i] = mfma_bf16(vf[k], pl[p], o[i]);
+    }
+  }
+
+  // join the waves: o[t][r] is dim (4 grp + r) NT + t of row l16
+  l += __shfl_xor(l, 16, 64);
+  l += __shfl_xor(l, 32, 64);
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) so[wave][l16][(4 * grp + r) * NT + t] = o[t][r];
+  if (grp == 0) {
+    sml[wave][l16][0] = m;
+    sml[wave][l16][1] = l;
+  }
+  __syncthreads();
+  constexpr int Q4 = HD / 4;
+  for (int i = tid; i < 16 * Q4; i += NW * 64) {
+    const int r = i / Q4, d = i % Q4 * 4, rr = chunk * 16 + r;
+    if (rr >= R) break;
+    float mm = sml[0][r][0];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) mm = fmaxf(mm, sml[w][r][0]);
+    const float mref = mm == -INFINITY ? 0.f : mm;
+    float num[4] = {0.f, 0.f, 0.f, 0.f}, den = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float wt = __builtin_amdgcn_exp2f(sml[w][r][0] - mref);  // a wave without keys: 0
+      den += wt * sml[w][r][1];
+      const f32x4_t v = *(const f32x4_t*)&so[w][r][d];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) num[k] += wt * v[k];
+    }
+    if (part.nsplit > 1) {
+      const long long pr = (((long long)split * a.batch + b) * c.nkv + g) * R + rr;
+      *(f32x4_t*)(part.o + pr * HD + d) = f32x4_t{num[0], num[1], num[2], num[3]};
+      if (d == 0) {
+        part.ml[pr * 2] = mm;
+        part.ml[pr * 2 + 1] = den;
+      }
+      continue;
+    }
+    const float inv = den == 0.f ? 0.f : 1.f / den;  // a row that sees nothing: 0
+    if (part.lse && d == 0) part.lse[((long long)b * c.nkv + g) * R + rr] = den == 0.f ? INFINITY : mref + log2f(den);
+    const long long at = b * a.ob + rr % a.rows * a.orow + (g * G + rr / a.rows) * a.oh + d;
+    if constexpr (F32)
+      *(f32x4_t*)((float*)a.out + at) = f32x4_t{num[0] * inv, num[1] * inv, num[2] * inv, num[3] * inv};
+    else
+      *(u32x2_t*)((bf16_t*)a.out + at) = u32x2_t{pack_bf16x2(num[0] * inv, num[1] * inv), pack_bf16x2(num[2] * inv, num[3] * inv)};
+  }
+}
+
+// The key ranges joined in range order, four dims a thread.
+template <bool F32>
+__global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a, Part part) {
+  const CacheView& c = a.c;
+  const int G = a.nq / c.nkv, R = G * a.rows, Q4 = c.hd / 4;
+  const long long rows = (long long)a.batch * c.nkv * R, i = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (i >= rows * Q4) return;
+  const long long pr = i / Q4;
+  const int d = (int)(i % Q4) * 4, rr = (int)(pr % R), g = (int)(pr / R % c.nkv), b = (int)(pr / R / c.nkv);
+  float mm = -INFINITY;
+  for (int s = 0; s < part.nsplit; ++s) mm = fmaxf(mm, part.ml[(s * rows + pr) * 2]);
+  const float mref = mm == -INFINITY ? 0.f : mm;
+  float num[4] = {0.f, 0.f, 0.f, 0.f}, den = 0.f;
+  for (int s = 0; s < part.nsplit; ++s) {
+    const float2 ml = *(const float2*)(part.ml + (s * rows + pr) * 2);
+    const float wt = __builtin_amdgcn_exp2f(ml.x - mref);
+    const f32x4_t v = *(const f32x4_t*)(part.o + (s * rows + pr) * c.hd + d);
+    den += wt * ml.y;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) num[k] += wt * v[k];
+  }
+  const float inv = den == 0.f ? 0.f : 1.f / den;
+  if (part.lse && d == 0) part.lse[pr] = den == 0.f ? INFINITY : mref + log2f(den);
+  const long long at = b * a.ob + rr % a.rows * a.orow + (g * G + rr / a.rows) * a.oh + d;
+  if constexpr (F32)
+    *(f32x4_t*)((float*)a.out + at) = f32x4_t{num[0] * inv, num[1] * inv, num[2] * inv, num[3] * inv};
+  else
+    *(u32x2_t*)((bf16_t*)a.out + at) = u32x2_t{pack_bf16x2(num[0] * inv, num[1] * inv), pack_bf16x2(num[2] * inv, num[3] * inv)};
+}
+
+// Accumulated weights: every wave owns 32 keys of a (sequence, kv head), forms their scores
+// once more and adds 2^(score - lse) over all rows.  Batch rows that name one sequence are
+// added in row order by the first of them, so that the sums have one order.
+template <int HD, bool F32>
+__global__ __launch_bounds__(NW * 64) void cache_weight_kernel(CacheAttnArgs a, const float* lse) {
+  constexpr int KS = HD / 32, NP = F32 ? 3 : 1;
+  const CacheView& c = a.c;
+  const int g = blockIdx.y, b0 = blockIdx.z;
+  const int id = cache_seq(c, a.seq, b0);
+  if (id < 0 || cache_seq_before(c, a.seq, b0, id)) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l16 = lane & 15, grp = lane >> 4;
+  const int n = cache_len(c, id), key0 = (blockIdx.x * NW + wave) * 32;
+  if (key0 >= n) return;
+  const int G = a.nq / c.nkv, R = G * a.rows;
+  const long long head = (long long)id * c.nkv + g;
+  bf16x8_t kf[2][KS];
+  float k2[2];
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int key = min(key0 + 16 * u, n - 1);
+    k2[u] = c.ks[head * c.nblk + (key >> c.shift)] * (a.scale * kLog2e);
+    const uint8_t* p = c.k + (head * c.cap + min(key0 + 16 * u + l16, n - 1)) * HD;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const u32x2_t w = *(const u32x2_t*)(p + kdim<HD>(ks, grp));
+      kf[u][ks] = codes8(w[0], w[1]);
+    }
+  }
+  float acc[2][4] = {};
+  for (int b = b0; b < a.batch; ++b) {
+    if (b != b0 && cache_seq(c, a.seq, b) != id) continue;
+    for (int r0 = 0; r0 < R; r0 += 16) {
+      const int row = r0 + l16, r = min(row, R - 1);
+      const long long at = b * a.qb + r % a.rows * a.qr + (g * G + r / a.rows) * a.qh;
+      const float ls = row < R ? lse[((long long)b * c.nkv + g) * R + row] : INFINITY;
+      f32x4_t s[2] = {f32x4_t{0.f, 0.f, 0.f, 0.f}, f32x4_t{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        bf16x8_t q[NP];
+        load8<F32>(a.q, at + kdim<HD>(ks, grp), q);
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int p = NP - 1; p >= 0; --p) s[u] = mfma_bf16(kf[u][ks], q[p], s[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) acc[u][k] += __builtin_amdgcn_exp2f(s[u][k] * k2[u] - ls);
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      float v = acc[u][k];
+#pragma unroll
+      for (int off = 1; off < 16; off <<= 1) v += __shfl_xor(v, off, 64);
+      const int key = key0 + 16 * u + 4 * grp + k;
+      if (l16 == 0 && key < n) c.weight[head * c.cap + key] += v;
+    }
+}
+
+struct Plan {
+  int chunks, nsplit;
+  size_t o_off, ml_off, lse_off, bytes;
+};
+size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+
+Plan plan_of(const CacheAttnArgs& a) {
+  Plan p;
+  const long long R = (long long)(a.nq / a.c.nkv) * a.rows, heads = (long long)a.batch * a.c.nkv;
+  p.chunks = (int)((R + 15) / 16);
+  const long long blocks = p.chunks * heads, tiles = (a.c.cap + 31) / 32 + (a.n_self + 31) / 32;
+  // two blocks a CU, at least one tile a wave in every key range
+  p.nsplit = (int)std::max(1ll, std::min({512 / std::max(blocks, 1ll), tiles / NW, 64ll}));
+  p.o_off = 0;
+  p.ml_off = p.nsplit > 1 ? up256((size_t)p.nsplit * heads * R * a.c.hd * 4) : 0;
+  p.lse_off = p.ml_off + (p.nsplit > 1 ? up256((size_t)p.nsplit * heads * R * 8) : 0);
+  p.bytes = p.lse_off + (a.track ? up256((size_t)heads * R * 4) : 0);
+  return p;
+}
+
+template <int HD, bool F32>
+hipError_t launch_hd(const CacheAttnArgs& a, hipStream_t s) {
+  const Plan p = plan_of(a);
+  const long long heads = (long long)a.batch * a.c.nkv, R = (long long)(a.nq / a.c.nkv) * a.rows;
+  char* ws = (char*)a.ws;
+  const Part part{(float*)(ws + p.o_off), (float*)(ws + p.ml_off), a.track ? (float*)(ws + p.lse_off) : nullptr, p.nsplit};
+  const long long blocks = p.chunks * heads * p.nsplit, joins = (heads * R * (HD / 4) + 255) / 256;
+  if (blocks > 0x7FFFFFFF || joins > 0x7FFFFFFF) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((cache_attn_kernel<HD, F32>), dim3((unsigned)blocks), dim3(NW * 64), 0, s, a, part, p.chunks);
+  if (p.nsplit > 1) hipLaunchKernelGGL(cache_join_kernel<F32>, dim3((unsigned)joins), dim3(256), 0, s, a, part);
+  if (a.track)
+    hipLaunchKernelGGL((cache_weight_kernel<HD, F32>), dim3((a.c.cap + 32 * NW - 1) / (32 * NW), a.c.nkv, a.batch),
+                       dim3(NW * 64), 0, s, a, part.lse);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t cache_attn_workspace(const CacheAttnArgs& a) { return a.batch == 0 ? 0 : plan_of(a).bytes; }
+
+hipError_t launch_cache_attention(const CacheAttnArgs& a, hipStream_t s) {
+  if (a.batch == 0) return hipSuccess;
+  switch (a.c.hd) {
+    case 32: return a.f32 ? launch_hd<32, true>(a, s) : launch_hd<32, false>(a, s);
+    case 64: return a.f32 ? launch_hd<64, true>(a, s) : launch_hd<64, false>(a, s);
+    case 128: return a.f32 ? launch_hd<128, true>(a, s) : launch_hd<128, false>(a, s);
+    case 256: return a.f32 ? launch_hd<256, true>(a, s) : launch_hd<256, false>(a, s);
+    default: return hipErrorInvalidValue;
+  }
+}
+
+}  // namespace ravel

@@ -14,6 +14,7 @@
 #include <string>
 #include <vector>
 
+#include "cache.h"
 #include "kernels.h"
 #include "persistent.h"
 #include "ravel.h"
@@ -24,9 +25,17 @@ namespace {
 
 thread_local std::string g_err;
 
-ravel_status fail(ravel_status s, const std::string& msg) {
+}  // namespace
+
+ravel_status ravel::set_error(ravel_status s, const std::string& msg) {
   g_err = msg;
   return s;
+}
+
+namespace {
+
+ravel_status fail(ravel_status s, const std::string& msg) {
+  return set_error(s, msg);
 }
 
 #define HIP_TRY(expr)                                                                        \

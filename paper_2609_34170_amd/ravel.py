@@ -9,6 +9,7 @@ without it raises immediately -- there is no CPU fallback.
 
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Dict, List, Optional, Tuple
@@ -49,6 +50,20 @@ class KernelRecord(ctypes.Structure):
                 ("ms", ctypes.c_float)]
 
 
+class RavelCache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "n_seq", "n_kv_heads", "head_dim", "capacity", "block", "reserved")] + [
+        (n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "len", "weight")]
+
+
+class RavelCacheQuery(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "batch", "n_q_heads", "rows", "n_self", "track")] + [
+        ("scale", ctypes.c_float), ("reserved", ctypes.c_int32)] + [
+        (n, ctypes.c_void_p) for n in ("seq", "q", "self_k", "self_v", "out")] + [
+        (n, ctypes.c_int64 * 3) for n in ("q_stride", "self_stride", "out_stride")] + [
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_int64)]
+
+
 SYMBOLS = [
     "ravel_create", "ravel_destroy", "ravel_model_weight_bytes", "ravel_buffer_create",
     "ravel_buffer_destroy", "ravel_buffer_set_option", "ravel_context_acquire", "ravel_set_context",
@@ -56,6 +71,8 @@ SYMBOLS = [
     "ravel_fop_encode", "ravel_fop_encode_noalloc", "ravel_buffer_sync", "ravel_debug_state",
     "ravel_publish_log", "ravel_buffer_query",
     "ravel_buffer_save", "ravel_buffer_load", "ravel_profile_step", "ravel_last_error",
+    "ravel_cache_append", "ravel_cache_attention_workspace", "ravel_cache_attention", "ravel_cache_evict_workspace",
+    "ravel_cache_evict",
 ]
 
 _lib = None
@@ -93,6 +110,13 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "ravel_buffer_load": ([vp, vp, ctypes.c_size_t], i32),
         "ravel_profile_step": ([vp, vp, vp, vp, ctypes.POINTER(KernelRecord), ctypes.POINTER(i32)], i32),
         "ravel_last_error": ([], ctypes.c_char_p),
+        "ravel_cache_append": ([ctypes.POINTER(RavelCache), i32, vp, vp, vp, i32, i32, vp, vp, i64, i64, i64, vp], i32),
+        "ravel_cache_attention_workspace": ([ctypes.POINTER(RavelCache), ctypes.POINTER(RavelCacheQuery),
+                                             ctypes.POINTER(i64)], i32),
+        "ravel_cache_attention": ([ctypes.POINTER(RavelCache), ctypes.POINTER(RavelCacheQuery), vp], i32),
+        "ravel_cache_evict_workspace": ([ctypes.POINTER(RavelCache), i32, i32, ctypes.POINTER(i64)], i32),
+        "ravel_cache_evict": ([ctypes.POINTER(RavelCache), i32, vp, i32, i32, ctypes.POINTER(RavelCache), vp, vp, vp,
+                               i64, vp], i32),
     }
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
@@ -293,3 +317,162 @@ class Buffer:
             self.close()
         except Exception:
             pass
+
+
+class Cache:
+    """A key/value cache in 8 bits (the ravel_cache_* calls) over tensors that the caller owns.
+
+    ``k``, ``v``: e4m3 codes ``[n_seq, n_kv_heads, capacity, head_dim]`` (float8_e4m3fn or uint8); ``k_scale``,
+    ``v_scale``: float32 ``[n_seq, n_kv_heads, ceil(capacity / block)]``; ``length``: int32 ``[n_seq]``; ``weight``:
+    float32 ``[n_seq, n_kv_heads, capacity]`` or None.  ``Cache.empty`` makes them.  Indices, positions and counts are
+    int32 tensors on the same device.  Calls are enqueued on ``stream`` (default: torch's current one).
+    """
+
+    def __init__(self, k, v, k_scale, v_scale, length, block: int, weight=None):
+        import torch
+
+        n_seq, n_kv, cap, hd = k.shape
+        blocks = (n_seq, n_kv, -(-cap // block) if block > 0 else 0)
+        for name, t, shape, types in (
+                ("k", k, k.shape, (torch.float8_e4m3fn, torch.uint8)), ("v", v, k.shape, (torch.float8_e4m3fn, torch.uint8)),
+                ("k_scale", k_scale, blocks, (torch.float32,)), ("v_scale", v_scale, blocks, (torch.float32,)),
+                ("length", length, (n_seq,), (torch.int32,)), ("weight", weight, (n_seq, n_kv, cap), (torch.float32,))):
+            if t is None and name == "weight":
+                continue
+            if tuple(t.shape) != tuple(shape) or t.dtype not in types or t.device != k.device or not t.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous {types[0]} tensor {tuple(shape)} on {k.device}")
+        self.k, self.v, self.k_scale, self.v_scale, self.length, self.weight = k, v, k_scale, v_scale, length, weight
+        self.block, self.device = block, k.device
+        self._c = RavelCache(n_seq, n_kv, hd, cap, block, 0, k.data_ptr(), v.data_ptr(), k_scale.data_ptr(),
+                             v_scale.data_ptr(), length.data_ptr(), None if weight is None else weight.data_ptr())
+        self._ref = ctypes.byref(self._c)
+
+    @classmethod
+    def empty(cls, n_seq: int, n_kv_heads: int, capacity: int, head_dim: int, block: int = 64, weight: bool = False,
+              device="cuda"):
+        """A cache of empty sequences: codes 0 under the smallest scale, so that positions skipped by an append are zeros
+        and leave their block's scale to its tokens."""
+        import torch
+
+        codes = [torch.zeros((n_seq, n_kv_heads, capacity, head_dim), dtype=torch.uint8, device=device)
+                 .view(torch.float8_e4m3fn) for _ in range(2)]
+        scales = [torch.full((n_seq, n_kv_heads, -(-capacity // block)), 2.0 ** -100, device=device) for _ in range(2)]
+        return cls(*codes, *scales, torch.zeros(n_seq, dtype=torch.int32, device=device), block,
+                   torch.zeros((n_seq, n_kv_heads, capacity), device=device) if weight else None)
+
+    def _on(self, stream, *tensors):
+        """(guard that makes this cache's device and the call's stream current, or None; stream handle)."""
+        import torch
+
+        for t in tensors:
+            if t is not None and t.device != self.device:
+                raise ValueError(f"every tensor of the call must be on {self.device}")
+        if stream is None:
+            if self.device.index in (None, torch.cuda.current_device()):
+                return None, torch.cuda.current_stream().cuda_stream
+            return torch.cuda.device(self.device), torch.cuda.current_stream(self.device).cuda_stream
+        if isinstance(stream, int):
+            stream = torch.cuda.ExternalStream(stream, device=self.device)
+        return torch.cuda.stream(stream), stream.cuda_stream
+
+    def _index(self, name, t, batch):
+        import torch
+
+        if t is None:
+            return None
+        if t.dtype is not torch.int32 or t.dim() != 1 or t.shape[0] != batch or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous int32 tensor [{batch}]")
+        return t.data_ptr()
+
+    def append(self, k, v, pos=None, count=None, seq=None, stream=None):
+        """Store k, v ``[batch, n, n_kv_heads, head_dim]`` (bf16 or float32) from ``pos`` (default: the lengths) on."""
+        c = self._c
+        if k.dim() != 4 or k.shape != v.shape or k.shape[2] != c.n_kv_heads or k.shape[3] != c.head_dim or \
+                v.dtype is not k.dtype:
+            raise ValueError(f"k and v must be [batch, n, {c.n_kv_heads}, {c.head_dim}] of one dtype")
+        if k.stride() != v.stride() or (k.stride(3) != 1 and k.numel()):
+            raise ValueError("k and v must have the same strides, head_dim contiguous")
+        guard, s = self._on(stream, k, v, pos, count, seq)
+        B, n, sb, st, sh = k.shape[0], k.shape[1], *k.stride()[:3]
+        args = (self._ref, B, self._index("seq", seq, B), self._index("pos", pos, B), self._index("count", count, B),
+                n, _cache_dtype(k), k.data_ptr(), v.data_ptr(), sb, st, sh, s)
+        if guard is None:
+            _check(load_library().ravel_cache_append(*args))
+        else:
+            with guard:
+                _check(load_library().ravel_cache_append(*args))
+
+    def attention(self, q, out, self_k=None, self_v=None, seq=None, scale=None, track=False, stream=None):
+        """out = attention of q ``[batch, rows, n_q_heads, head_dim]`` over the sequences' tokens and the call's own
+        ``self_k``, ``self_v`` ``[batch, n_self, n_kv_heads, head_dim]``; ``track``: add to the accumulated weights."""
+        c = self._c
+        if q.dim() != 4 or q.shape[3] != c.head_dim or out.shape != q.shape or out.dtype is not q.dtype:
+            raise ValueError(f"q and out must be [batch, rows, n_q_heads, {c.head_dim}] of one dtype")
+        B, rows, nq, hd = q.shape
+        qs, os = q.stride(), out.stride()
+        if (qs[3] != 1 or os[3] != 1) and q.numel():
+            raise ValueError("head_dim must be contiguous")
+        x = RavelCacheQuery(_cache_dtype(q), B, nq, rows, 0, 1 if track else 0, hd ** -0.5 if scale is None else scale, 0,
+                            self._index("seq", seq, B), q.data_ptr(), None, None, out.data_ptr(), qs[:3], (0, 0, 0), os[:3])
+        if (self_k is None) != (self_v is None):
+            raise ValueError("self_k and self_v must both be given or both None")
+        if self_k is not None:
+            if self_k.dim() != 4 or self_k.shape != self_v.shape or self_k.shape[0] != B or \
+                    self_k.shape[2] != c.n_kv_heads or self_k.shape[3] != hd or \
+                    self_k.dtype is not q.dtype or self_v.dtype is not q.dtype:
+                raise ValueError(f"self_k and self_v must be [{B}, n_self, {c.n_kv_heads}, {hd}] of the queries' dtype")
+            ss = self_k.stride()
+            if self_v.stride() != ss or (ss[3] != 1 and self_k.numel()):
+                raise ValueError("self_k and self_v must have the same strides, head_dim contiguous")
+            x.n_self, x.self_k, x.self_v, x.self_stride = self_k.shape[1], self_k.data_ptr(), self_v.data_ptr(), ss[:3]
+        guard, s = self._on(stream, q, out, self_k, self_v, seq)
+        if guard is None:
+            self._attention(x, s)
+        else:
+            with guard:
+                self._attention(x, s)
+
+    def _attention(self, x, s):
+        import torch
+
+        lib, n = load_library(), ctypes.c_int64(0)
+        _check(lib.ravel_cache_attention_workspace(self._ref, ctypes.byref(x), ctypes.byref(n)))
+        if n.value:
+            # of this call alone: torch keeps it from later calls on the stream until this one has run
+            ws = torch.empty(n.value, dtype=torch.uint8, device=self.device)
+            x.workspace, x.workspace_bytes = ws.data_ptr(), n.value
+        _check(lib.ravel_cache_attention(self._ref, ctypes.byref(x), s))
+
+    def evict(self, keep: int, first: int = 0, seq=None, into: Optional["Cache"] = None, into_seq=None, kept=None,
+              stream=None):
+        """Keep the ``keep`` tokens of the largest accumulated weight per row and KV head, in place or in another cache;
+        returns the index each place's token had, int32 ``[batch, n_kv_heads, keep]`` (``kept``, or a new tensor)."""
+        import torch
+
+        c = self._c
+        B = seq.shape[0] if seq is not None else c.n_seq
+        if into is not None and into.device != self.device:
+            raise ValueError(f"every tensor of the call must be on {self.device}")
+        guard, s = self._on(stream, seq, into_seq, kept)
+        with guard if guard is not None else contextlib.nullcontext():
+            if kept is None:
+                kept = torch.empty((B, c.n_kv_heads, max(keep, 0)), dtype=torch.int32, device=self.device)
+            elif tuple(kept.shape) != (B, c.n_kv_heads, keep) or kept.dtype is not torch.int32 or not kept.is_contiguous():
+                raise ValueError(f"kept must be a contiguous int32 tensor [{B}, {c.n_kv_heads}, {keep}]")
+            lib, n = load_library(), ctypes.c_int64(0)
+            _check(lib.ravel_cache_evict_workspace(self._ref, B, keep, ctypes.byref(n)))
+            ws = torch.empty(n.value, dtype=torch.uint8, device=self.device)
+            _check(lib.ravel_cache_evict(self._ref, B, self._index("seq", seq, B), keep, first,
+                                         None if into is None else into._ref, self._index("into_seq", into_seq, B),
+                                         kept.data_ptr(), ws.data_ptr(), n.value, s))
+        return kept
+
+
+def _cache_dtype(t) -> int:
+    import torch
+
+    if t.dtype is torch.bfloat16:
+        return BF16
+    if t.dtype is torch.float32:
+        return F32
+    raise ValueError(f"bf16 or float32 expected, got {t.dtype}")
