@@ -485,6 +485,35 @@ ravel_status ravel_cache_evict(const ravel_cache* cache, int32_t batch, const in
                                const ravel_cache* into, const int32_t* into_seq, int32_t* kept, void* workspace,
                                int64_t workspace_bytes, void* stream);
 
+/* A buffer that holds its contexts in such a cache (otherwise as ravel_buffer_create makes it): half the
+ * memory of a bf16 model's contexts and half the bytes its steps read of them (a quarter in 32 bits).
+ * ravel_set_context stores the given keys and values, in the model dtype, through ravel_cache_append's
+ * kernel (k and v must not be NULL: there is no zero-copy publication, and ravel_context_acquire is
+ * E_STATE); every expert pass attends through ravel_cache_attention's kernels; one kernel per operation
+ * (RAVEL_OPT_PERSISTENT is E_STATE).  Sequence (slot * batch + env) * layers + layer of the cache holds
+ * one layer's prefix, slot 0 or 1.  Saved states go with buffers of the same block only.
+ * Errors: as ravel_buffer_create; E_SHAPE for analytic models, models without prefix tokens or with a
+ * head_dim that the cache does not take; E_INVALID (block). */
+ravel_status ravel_buffer_create_quantized(ravel_model* model, int32_t batch, uint64_t seed, int32_t block,
+                                           ravel_buffer** out);
+
+/* on != 0: every later expert pass over this buffer's contexts adds the softmax weights that its self-
+ * attention gives the prefix tokens to their accumulated weights (a token's start at 0 when its context
+ * is stored); 0 (the default): not.  E_STATE on a buffer without a quantized context. */
+ravel_status ravel_context_track(ravel_buffer* buf, int32_t on);
+
+/* ravel_cache_evict, in place, on every layer of env's active context (env = -1: of every env's),
+ * enqueued on `stream` in the order of the steps: later passes attend over the `keep` tokens of each
+ * layer and KV head with the largest accumulated weights.  The next context published starts whole.
+ * Must be ordered with the buffer's steps as these are among themselves.  Errors: E_STATE (no quantized
+ * contexts, an env without an applied context), E_INVALID (env), E_SHAPE (keep < 1, first outside 0..keep). */
+ravel_status ravel_context_evict(ravel_buffer* buf, int32_t env, int32_t keep, int32_t first, void* stream);
+
+/* env's active context as a cache of `layers` sequences in the buffer's own memory, for reading and for
+ * the ravel_cache_* calls; it stays the active one until a step applies a newer context.  E_STATE (no
+ * quantized contexts, no applied context), E_INVALID (null pointer, env). */
+ravel_status ravel_context_cache(ravel_buffer* buf, int32_t env, ravel_cache* cache);
+
 /* Message of the calling thread's last non-OK status ("" if none). */
 const char* ravel_last_error(void);
 

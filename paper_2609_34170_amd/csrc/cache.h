@@ -26,11 +26,12 @@ struct CacheView {
   int shift, nblk;  // tokens per scale block = 1 << shift; blocks per (sequence, head)
 };
 
-// Batch row b's sequence: idx[b] * mul + b * row + add (idx null: the first term is 0).  Rows
-// whose sequence falls outside the cache take no part in a call.
+// Batch row b's sequence: idx[b / div] * mul + b * row + add (idx null: the first term is 0).
+// Rows whose sequence falls outside the cache take no part in a call.  With row != 0 the rows
+// name distinct sequences.
 struct SeqMap {
   const int* idx;
-  int mul, row, add;
+  int div, mul, row, add;
 };
 
 struct CacheAppendArgs {
@@ -74,13 +75,13 @@ hipError_t launch_cache_evict(const CacheEvictArgs& a, hipStream_t s);
 
 #ifdef __HIPCC__
 RAVEL_DEV int cache_seq(const CacheView& c, const SeqMap& m, int b) {  // negative: none
-  const long long id = (m.idx ? (long long)m.idx[b] * m.mul : 0) + (long long)b * m.row + m.add;
+  const long long id = (m.idx ? (long long)m.idx[m.div == 1 ? b : b / m.div] * m.mul : 0) + (long long)b * m.row + m.add;
   return id >= 0 && id < c.n_seq ? (int)id : -1;
 }
 RAVEL_DEV int cache_len(const CacheView& c, int id) { return min(max(c.len[id], 0), c.cap); }
 // Whether a row before b names the same sequence (uniform over the block; every thread calls).
 RAVEL_DEV bool cache_seq_before(const CacheView& c, const SeqMap& m, int b, int id) {
-  if (!m.idx) return false;  // distinct by construction
+  if (!m.idx || m.row) return false;
   bool hit = false;
   for (int i = threadIdx.x; i < b; i += blockDim.x) hit |= cache_seq(c, m, i) == id;
   return __syncthreads_or(hit) != 0;

@@ -74,7 +74,7 @@ CacheView view(const ravel_cache* c) {
   return v;
 }
 
-SeqMap seq_map(const int32_t* seq) { return seq ? SeqMap{seq, 1, 0, 0} : SeqMap{nullptr, 0, 1, 0}; }
+SeqMap seq_map(const int32_t* seq) { return seq ? SeqMap{seq, 1, 1, 0, 0} : SeqMap{nullptr, 1, 0, 1, 0}; }
 
 ravel_status launched(const char* call, hipError_t e) {
   return e == hipSuccess ? RAVEL_OK : set_error(RAVEL_E_HIP, std::string(call) + ": " + hipGetErrorString(e));

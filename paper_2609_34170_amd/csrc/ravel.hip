@@ -336,11 +336,12 @@ struct GraphEntry {
   const float* state;
   float* action;
   bool persistent;
+  bool track;
   hipGraph_t graph;
   hipGraphExec_t exec;
 };
 
-// (fop, state, action, execution path) of a step, as numbers
+// (fop, state, action, execution path and tracking) of a step, as numbers
 using PointerSet = std::array<uintptr_t, 4>;
 // Sets remembered before their second use.  More than any ring of action buffers a caller
 // would cycle through (a table of 8 left rings of 9 and more unrecorded for good); a full
@@ -361,6 +362,16 @@ struct ravel_buffer {
   void* ctx_k = nullptr;
   void* ctx_v = nullptr;
   size_t ctx_elems = 0;  // per env per slot: L * P * nkv * hd
+  // contexts in 8 bits (ravel_buffer_create_quantized): sequence (slot B + env) L + layer; block 0: not
+  int quant_block = 0;
+  CacheView qc{};
+  bool track = false;            // expert passes add to the tokens' accumulated weights
+  int* qpos = nullptr;           // [L] zeros: a context is stored from position 0 on
+  void* qws = nullptr;           // attention workspace
+  void* qevict_ws = nullptr;     // eviction workspace and its indices
+  int* qkept = nullptr;
+  void* qstage = nullptr;        // a context's keys and values given in host memory
+  hipEvent_t stage_free = nullptr;
   // activations
   float* x = nullptr;
   void* cond = nullptr;
@@ -570,6 +581,44 @@ ravel_status run_attn(ravel_buffer* b, hipStream_t s, KernelRecorder* rec, const
     HIP_TRY(launch_attn_bf16(a, s));
   else
     HIP_TRY(launch_attn_f32(a, s));
+  if (rec) rec->end();
+  return RAVEL_OK;
+}
+
+// Self-attention of layer l over the active contexts in 8 bits and the buffer's own rows.
+CacheAttnArgs cache_attn_args(const ravel_buffer* b, int l) {
+  const ravel_config& c = b->m->cfg;
+  const int qd = c.n_q_heads * c.head_dim, kvd = c.n_kv_heads * c.head_dim, ld = qd + 2 * kvd;
+  const size_t elt = b->m->elt;
+  CacheAttnArgs a;
+  a.c = b->qc;
+  a.seq = SeqMap{b->slot, 1, b->B * c.layers, c.layers, l};
+  a.batch = b->B;
+  a.nq = c.n_q_heads;
+  a.rows = a.n_self = c.horizon;
+  a.q = b->qkv;
+  a.sk = (const char*)b->qkv + qd * elt;
+  a.sv = (const char*)b->qkv + (qd + kvd) * elt;
+  a.qb = a.sb = (long long)c.horizon * ld;
+  a.qr = a.st = ld;
+  a.qh = a.sh = a.oh = c.head_dim;
+  a.out = b->att;
+  a.ob = (long long)c.horizon * qd;
+  a.orow = qd;
+  a.scale = 1.0f / sqrtf((float)c.head_dim);
+  a.f32 = !b->m->bf16;
+  a.track = b->track;
+  a.ws = b->qws;
+  return a;
+}
+
+ravel_status run_cache_attn(ravel_buffer* b, hipStream_t s, KernelRecorder* rec, int l) {
+  const ravel_config& c = b->m->cfg;
+  const double elt = (double)b->m->elt, row = (double)c.n_kv_heads * c.head_dim, H = c.horizon;
+  const double bytes = b->B * (H * c.n_q_heads * c.head_dim * 2 * elt + (c.prefix_len + H * elt) * row * 2);
+  const double flops = 4.0 * b->B * c.n_q_heads * H * (c.prefix_len + H) * c.head_dim;
+  if (rec) rec->begin("cache_attn", bytes, flops);
+  HIP_TRY(launch_cache_attention(cache_attn_args(b, l), s));
   if (rec) rec->end();
   return RAVEL_OK;
 }
@@ -901,7 +950,10 @@ ravel_status enqueue_transformer(ravel_buffer* b, const void* fop, hipStream_t s
       a.s_ld = qkvd;
       a.out = b->att;
       a.ldo = qd;
-      RV_TRY(run_attn<T>(b, s, rec, "attn", a));
+      if (b->quant_block)
+        RV_TRY(run_cache_attn(b, s, rec, l));
+      else
+        RV_TRY(run_attn<T>(b, s, rec, "attn", a));
     }
     RV_TRY(resid_norm<T>(b, s, rec, "o", b->att, qd, L.o_w, qd, qd, mod + 2 * w, nullptr, ldm, rowmap,
                          ad ? NormOf{L.gamma, nullptr, 1} : norm2));
@@ -1098,6 +1150,45 @@ ravel_status apply_publishes(ravel_buffer* b, hipStream_t s) {
   return RAVEL_OK;
 }
 
+bool on_device(const void* p) {
+  hipPointerAttribute_t at;
+  if (hipPointerGetAttributes(&at, p) == hipSuccess) return at.type == hipMemoryTypeDevice;
+  (void)hipGetLastError();  // plain host memory
+  return false;
+}
+
+// Quantise one env's context into its inactive slot (acquired for `producer`).
+ravel_status store_context(ravel_buffer* b, int env, const void* k, const void* v, hipStream_t producer) {
+  const ravel_config& c = b->m->cfg;
+  const size_t bytes = b->ctx_elems * b->m->elt;
+  const bool staged = !on_device(k) || !on_device(v);
+  if (staged) {
+    // the staging rows are free once the last context given in host memory is stored
+    HIP_TRY(hipStreamWaitEvent(producer, b->stage_free, 0));
+    HIP_TRY(hipMemcpyAsync(b->qstage, k, bytes, hipMemcpyDefault, producer));
+    HIP_TRY(hipMemcpyAsync((char*)b->qstage + bytes, v, bytes, hipMemcpyDefault, producer));
+    k = b->qstage;
+    v = (const char*)b->qstage + bytes;
+  }
+  const int kvd = c.n_kv_heads * c.head_dim, inactive = b->active[env] ^ 1;
+  CacheAppendArgs a;
+  a.c = b->qc;
+  a.seq = SeqMap{nullptr, 1, 0, 1, (inactive * b->B + env) * c.layers};
+  a.batch = c.layers;
+  a.n = c.prefix_len;
+  a.pos = b->qpos;
+  a.count = nullptr;
+  a.k = k;
+  a.v = v;
+  a.sb = (long long)c.prefix_len * kvd;
+  a.st = kvd;
+  a.sh = c.head_dim;
+  a.f32 = !b->m->bf16;
+  HIP_TRY(launch_cache_append(a, producer));
+  if (staged) HIP_TRY(hipEventRecord(b->stage_free, producer));
+  return RAVEL_OK;
+}
+
 ravel_status acquire_locked(ravel_buffer* b, int env, void** k, void** v, hipStream_t producer) {
   ravel_model* m = b->m;
   b->pending[env].valid = false;  // a not-yet-applied publish of this env is superseded
@@ -1116,7 +1207,7 @@ ravel_status acquire_locked(ravel_buffer* b, int env, void** k, void** v, hipStr
 bool persistent_eligible(const ravel_buffer* b) {
   const ravel_model* m = b->m;
   const ravel_config& c = m->cfg;
-  if (!m->bf16 || c.model_kind != RAVEL_TRANSFORMER || !b->mod_all) return false;
+  if (!m->bf16 || c.model_kind != RAVEL_TRANSFORMER || !b->mod_all || b->quant_block) return false;
   const int BH = b->B * c.horizon, hd = c.head_dim;
   const int qd = c.n_q_heads * hd, kvd = c.n_kv_heads * hd;
   if (BH > 64 || b->B > 64) return false;
@@ -2202,7 +2293,7 @@ void ravel_destroy(ravel_model* m) {
   delete m;
 }
 
-ravel_status ravel_buffer_create(ravel_model* m, int32_t batch, uint64_t seed, ravel_buffer** out) {
+static ravel_status buffer_create(ravel_model* m, int32_t batch, uint64_t seed, int block, ravel_buffer** out) {
   if (!m || !out) return fail(RAVEL_E_INVALID, "null argument");
   if (batch < 1) return fail(RAVEL_E_SHAPE, "batch must be >= 1");
   *out = nullptr;
@@ -2215,6 +2306,7 @@ ravel_status ravel_buffer_create(ravel_model* m, int32_t batch, uint64_t seed, r
   b->m = m;
   b->B = batch;
   b->seed = seed;
+  b->quant_block = block;
   const int B = batch, H = c.horizon, D = c.action_dim, BH = B * H;
   const size_t E = m->elt;
   Arena ar;
@@ -2234,8 +2326,32 @@ ravel_status ravel_buffer_create(ravel_model* m, int32_t batch, uint64_t seed, r
     const int w = c.width, qd = c.n_q_heads * c.head_dim, kvd = c.n_kv_heads * c.head_dim;
     const int qkvd = qd + 2 * kvd, F = c.mlp_dim;
     b->ctx_elems = (size_t)c.layers * c.prefix_len * kvd;
-    ar.want(&b->ctx_k, 2 * (size_t)B * b->ctx_elems * E);
-    ar.want(&b->ctx_v, 2 * (size_t)B * b->ctx_elems * E);
+    if (block) {
+      CacheView& q = b->qc;
+      q.n_seq = 2 * B * c.layers;
+      q.nkv = c.n_kv_heads;
+      q.hd = c.head_dim;
+      q.cap = c.prefix_len;
+      while (1 << q.shift < block) ++q.shift;
+      q.nblk = (q.cap + block - 1) / block;
+      const size_t heads = (size_t)q.n_seq * q.nkv;
+      ar.want((void**)&q.k, heads * q.cap * q.hd);
+      ar.want((void**)&q.v, heads * q.cap * q.hd);
+      ar.want((void**)&q.ks, heads * q.nblk * 4);
+      ar.want((void**)&q.vs, heads * q.nblk * 4);
+      ar.want((void**)&q.len, (size_t)q.n_seq * 4);
+      ar.want((void**)&q.weight, heads * q.cap * 4);
+      ar.want((void**)&b->qpos, (size_t)c.layers * 4);
+      CacheAttnArgs a = cache_attn_args(b, 0);
+      a.track = true;
+      ar.want(&b->qws, cache_attn_workspace(a));
+      ar.want(&b->qevict_ws, cache_evict_workspace(B * c.layers, q.nkv, q.cap));
+      ar.want((void**)&b->qkept, heads / 2 * q.cap * 4);
+      ar.want(&b->qstage, 2 * b->ctx_elems * E);
+    } else {
+      ar.want(&b->ctx_k, 2 * (size_t)B * b->ctx_elems * E);
+      ar.want(&b->ctx_v, 2 * (size_t)B * b->ctx_elems * E);
+    }
     ar.want((void**)&b->x, (size_t)BH * w * 4);
     ar.want(&b->cond, (size_t)BH * w * E);
     ar.want(&b->h1, (size_t)B * w * E);
@@ -2312,7 +2428,8 @@ ravel_status ravel_buffer_create(ravel_model* m, int32_t batch, uint64_t seed, r
     at.nq = c.n_q_heads;
     at.nkv = c.n_kv_heads;
     at.hd = c.head_dim;
-    if (m->bf16) plan_attn(at);
+    at.nsplit = 1;
+    if (m->bf16 && !block) plan_attn(at);
     if (at.nsplit > 1) {
       ar.want((void**)&b->apart_o, (size_t)at.nsplit * BH * qd * 4);
       ar.want((void**)&b->apart_ml, (size_t)at.nsplit * BH * c.n_q_heads * 2 * 4);
@@ -2348,6 +2465,8 @@ ravel_status ravel_buffer_create(ravel_model* m, int32_t batch, uint64_t seed, r
   }
   if (hipStreamCreateWithFlags(&b->cap_stream, hipStreamNonBlocking) != hipSuccess)
     return bail(fail(RAVEL_E_HIP, "stream create"));
+  if (block && hipEventCreateWithFlags(&b->stage_free, hipEventDisableTiming) != hipSuccess)
+    return bail(fail(RAVEL_E_HIP, "event create"));
   if (persistent_eligible(b)) {
     if (build_persistent(b) == RAVEL_OK) {
       // One kernel per operation is the faster path at every size measured (us per step,
@@ -2375,6 +2494,24 @@ ravel_status ravel_buffer_create(ravel_model* m, int32_t batch, uint64_t seed, r
   return RAVEL_OK;
 }
 
+ravel_status ravel_buffer_create(ravel_model* m, int32_t batch, uint64_t seed, ravel_buffer** out) {
+  return buffer_create(m, batch, seed, 0, out);
+}
+
+ravel_status ravel_buffer_create_quantized(ravel_model* m, int32_t batch, uint64_t seed, int32_t block,
+                                           ravel_buffer** out) {
+  if (!m || !out) return fail(RAVEL_E_INVALID, "null argument");
+  const ravel_config& c = m->cfg;
+  if (block != 16 && block != 32 && block != 64 && block != 128)
+    return fail(RAVEL_E_INVALID, "block must be 16, 32, 64 or 128");
+  if (c.model_kind != RAVEL_TRANSFORMER) return fail(RAVEL_E_SHAPE, "analytic models have no context");
+  if (c.prefix_len < 1 || c.prefix_len > 1 << 24) return fail(RAVEL_E_SHAPE, "prefix_len must be in 1..2^24");
+  if (c.head_dim != 32 && c.head_dim != 64 && c.head_dim != 128 && c.head_dim != 256)
+    return fail(RAVEL_E_SHAPE, "quantized contexts need a head_dim of 32, 64, 128 or 256");
+  if (batch > 32767 / c.layers) return fail(RAVEL_E_SHAPE, "quantized contexts: batch times layers must be at most 32767");
+  return buffer_create(m, batch, seed, block, out);
+}
+
 void ravel_buffer_destroy(ravel_buffer* b) {
   if (!b) return;
   (void)hipDeviceSynchronize();
@@ -2387,6 +2524,7 @@ void ravel_buffer_destroy(ravel_buffer* b) {
     if (b->retire[e]) (void)hipEventDestroy(b->retire[e]);
   }
   if (b->cap_stream) (void)hipStreamDestroy(b->cap_stream);
+  if (b->stage_free) (void)hipEventDestroy(b->stage_free);
   if (b->hflag) (void)hipHostFree(b->hflag);
   for (void* p : b->pallocs) (void)hipFree(p);
   for (auto& kv : b->full_tables) (void)hipFree(kv.second);
@@ -2420,6 +2558,7 @@ ravel_status ravel_context_acquire(ravel_buffer* b, int32_t env, void** k, void*
   if (!b || !k || !v) return fail(RAVEL_E_INVALID, "null argument");
   if (b->m->cfg.model_kind != RAVEL_TRANSFORMER) return fail(RAVEL_E_STATE, "analytic models have no context");
   if (env < 0 || env >= b->B) return fail(RAVEL_E_INVALID, "env out of range");
+  if (b->quant_block) return fail(RAVEL_E_STATE, "quantized contexts are stored by ravel_set_context");
   std::lock_guard<std::mutex> lk(b->mu);
   return acquire_locked(b, env, k, v, (hipStream_t)producer);
 }
@@ -2431,6 +2570,9 @@ ravel_status ravel_set_context(ravel_buffer* b, int32_t env, const void* k, cons
   if (env < -1 || env >= b->B) return fail(RAVEL_E_INVALID, "env out of range");
   if ((k == nullptr) != (v == nullptr)) return fail(RAVEL_E_INVALID, "k and v must both be given or both NULL");
   if (env == -1 && !k) return fail(RAVEL_E_INVALID, "env = -1 needs k and v ([B, L, P, n_kv, hd])");
+  if (b->quant_block && !k) return fail(RAVEL_E_STATE, "quantized contexts need k and v");
+  if (b->quant_block && ((uintptr_t)k % 16 || (uintptr_t)v % 16))
+    return fail(RAVEL_E_INVALID, "quantized contexts: k and v must be 16-byte aligned");
   hipStream_t ps = (hipStream_t)producer;
   std::lock_guard<std::mutex> lk(b->mu);
   const int e0 = env < 0 ? 0 : env, e1 = env < 0 ? b->B : env + 1;
@@ -2446,6 +2588,13 @@ ravel_status ravel_set_context(ravel_buffer* b, int32_t env, const void* k, cons
       void *dk, *dv;
       RV_TRY(acquire_locked(b, e, &dk, &dv, ps));
       const size_t src = env < 0 ? (size_t)e * bytes : 0;  // [B, L, P, n_kv, hd]: env e's block
+      if (b->quant_block) {
+        RV_TRY(store_context(b, e, (const char*)k + src, (const char*)v + src, ps));
+        HIP_TRY(hipEventRecord(b->pending[e].ready, ps));
+        b->pending[e].valid = true;
+        b->pending[e].t_obs = t_obs;
+        continue;
+      }
       HIP_TRY(hipMemcpyAsync(dk, (const char*)k + src, bytes, hipMemcpyDefault, ps));
       HIP_TRY(hipMemcpyAsync(dv, (const char*)v + src, bytes, hipMemcpyDefault, ps));
     }
@@ -2453,6 +2602,49 @@ ravel_status ravel_set_context(ravel_buffer* b, int32_t env, const void* k, cons
     b->pending[e].valid = true;
     b->pending[e].t_obs = t_obs;
   }
+  return RAVEL_OK;
+}
+
+ravel_status ravel_context_track(ravel_buffer* b, int32_t on) {
+  if (!b) return fail(RAVEL_E_INVALID, "null buffer");
+  std::lock_guard<std::mutex> lk(b->mu);
+  if (!b->quant_block) return fail(RAVEL_E_STATE, "the buffer's contexts are not quantized");
+  b->track = on != 0;
+  return RAVEL_OK;
+}
+
+ravel_status ravel_context_evict(ravel_buffer* b, int32_t env, int32_t keep, int32_t first, void* stream) {
+  if (!b) return fail(RAVEL_E_INVALID, "null buffer");
+  std::lock_guard<std::mutex> lk(b->mu);
+  if (!b->quant_block) return fail(RAVEL_E_STATE, "the buffer's contexts are not quantized");
+  if (env < -1 || env >= b->B) return fail(RAVEL_E_INVALID, "env out of range");
+  if (keep < 1 || first < 0 || first > keep) return fail(RAVEL_E_SHAPE, "keep must be >= 1 and first in 0..keep");
+  for (int e = env < 0 ? 0 : env; e < (env < 0 ? b->B : env + 1); ++e)
+    if (!b->has_ctx[e]) return fail(RAVEL_E_STATE, "env " + std::to_string(e) + " has no context yet");
+  const int L = b->m->cfg.layers;
+  CacheEvictArgs a;
+  a.src = a.dst = b->qc;
+  a.seq = env < 0 ? SeqMap{b->slot, L, b->B * L, 1, 0} : SeqMap{b->slot + env, L, b->B * L, 1, env * L};
+  a.dst_seq = a.seq;
+  a.batch = env < 0 ? b->B * L : L;
+  a.keep = std::min(keep, b->qc.cap);  // (a context never holds more)
+  a.first = std::min(first, a.keep);
+  a.kept = b->qkept;
+  a.ws = b->qevict_ws;
+  HIP_TRY(launch_cache_evict(a, (hipStream_t)stream));
+  return RAVEL_OK;
+}
+
+ravel_status ravel_context_cache(ravel_buffer* b, int32_t env, ravel_cache* out) {
+  if (!b || !out) return fail(RAVEL_E_INVALID, "null argument");
+  std::lock_guard<std::mutex> lk(b->mu);
+  if (!b->quant_block) return fail(RAVEL_E_STATE, "the buffer's contexts are not quantized");
+  if (env < 0 || env >= b->B) return fail(RAVEL_E_INVALID, "env out of range");
+  if (!b->has_ctx[env]) return fail(RAVEL_E_STATE, "env " + std::to_string(env) + " has no context yet");
+  const CacheView& q = b->qc;
+  const size_t s0 = ((size_t)b->active[env] * b->B + env) * b->m->cfg.layers, h0 = s0 * q.nkv;
+  *out = ravel_cache{b->m->cfg.layers,     q.nkv, q.hd, q.cap, b->quant_block, 0, q.k + h0 * q.cap * q.hd, q.v + h0 * q.cap * q.hd,
+                     q.ks + h0 * q.nblk, q.vs + h0 * q.nblk, q.len + s0, q.weight + h0 * q.cap};
   return RAVEL_OK;
 }
 
@@ -2645,13 +2837,16 @@ static ravel_status step_impl(ravel_buffer* b, const void* fop, const float* sta
     // one captured graph per (fop, state, action) pointer set and execution path
     GraphEntry* ge = nullptr;
     for (auto& g : b->graphs)
-      if (g.fop == fop && g.state == state && g.action == action && g.persistent == b->persistent) ge = &g;
+      if (g.fop == fop && g.state == state && g.action == action && g.persistent == b->persistent &&
+          g.track == b->track)
+        ge = &g;
     // a pointer set is captured the second time it is seen: recording and instantiating
     // costs about as much as the step itself (1140 us of a first step of 18 layers, against 980
     // replayed), which a caller that passes fresh tensors would pay at every step
     bool again = false;
     if (!ge) {
-      const PointerSet set = {(uintptr_t)fop, (uintptr_t)state, (uintptr_t)action, (uintptr_t)b->persistent};
+      const PointerSet set = {(uintptr_t)fop, (uintptr_t)state, (uintptr_t)action,
+                              (uintptr_t)b->persistent | (uintptr_t)b->track << 1};
       again = b->seen_sets.erase(set) != 0;
       if (!again) {
         if (b->seen_sets.size() == kSeenSets) b->seen_sets.clear();
@@ -2662,7 +2857,7 @@ static ravel_status step_impl(ravel_buffer* b, const void* fop, const float* sta
       RV_TRY(b->persistent ? enqueue_persistent_step(b, fop, state, action, s, nullptr)
                            : enqueue_step(b, fop, state, action, s, nullptr));
     } else if (!ge) {
-      GraphEntry g{fop, state, action, b->persistent, nullptr, nullptr};
+      GraphEntry g{fop, state, action, b->persistent, b->track, nullptr, nullptr};
       HIP_TRY(hipStreamBeginCapture(b->cap_stream, hipStreamCaptureModeRelaxed));
       ravel_status st = b->persistent ? enqueue_persistent_step(b, fop, state, action, b->cap_stream, nullptr)
                                       : enqueue_step(b, fop, state, action, b->cap_stream, nullptr);
@@ -2831,16 +3026,40 @@ struct BlobHeader {
   int32_t B, H, D, L, P, kvd, dtype, kind;
   uint64_t seed;
   int64_t t;
-  int32_t relative, pad;  // relative actions: mask [D], s_prev [B, D], has_prev [B] follow the contexts
+  int32_t relative;
+  int32_t block;  // of quantized contexts, 0: contexts in the model dtype
+  // with relative actions: mask [D], s_prev [B, D], has_prev [B] follow the contexts
 };
 const uint64_t kMagic = 0x5241564C53544154ull;  // "RAVLSTAT"
+
+// The memory of one env's active context, piece by piece: keys and values, or the tensors of
+// its sequences in the cache (half of them counted as keys, half as values, so that a context
+// takes 2 ctx_blob_bytes either way).
+std::vector<std::pair<void*, size_t>> ctx_pieces(const ravel_buffer* b, int e) {
+  const size_t slot = (size_t)b->active[e] * b->B + e;
+  if (!b->quant_block) {
+    const size_t cs = b->ctx_elems * b->m->elt;
+    return {{(char*)b->ctx_k + slot * cs, cs}, {(char*)b->ctx_v + slot * cs, cs}};
+  }
+  const CacheView& q = b->qc;
+  const size_t L = b->m->cfg.layers, s0 = slot * L, h0 = s0 * q.nkv, heads = L * q.nkv, row = (size_t)q.cap * q.hd;
+  return {{q.k + h0 * row, heads * row},         {q.v + h0 * row, heads * row},
+          {q.ks + h0 * q.nblk, heads * q.nblk * 4}, {q.vs + h0 * q.nblk, heads * q.nblk * 4},
+          {q.weight + h0 * q.cap, heads * q.cap * 4}, {q.len + s0, L * 4}};
+}
+size_t ctx_blob_bytes(const ravel_buffer* b) {  // half of a context's
+  if (b->m->cfg.model_kind != RAVEL_TRANSFORMER) return 0;
+  size_t n = 0;
+  for (const auto& p : ctx_pieces(b, 0)) n += p.second;
+  return (n + 1) / 2;
+}
 }  // namespace
 
 ravel_status ravel_buffer_save(ravel_buffer* b, void* blob, size_t* n) {
   if (!b || !n) return fail(RAVEL_E_INVALID, "null argument");
   const ravel_config& c = b->m->cfg;
   const size_t xs = (size_t)b->B * c.horizon * c.action_dim * 4;
-  const size_t cs = b->ctx_elems * b->m->elt;
+  const size_t cs = ctx_blob_bytes(b);
   const size_t rs = b->relative ? (size_t)c.action_dim * 4 + (size_t)b->B * c.action_dim * 4 + (size_t)b->B * 4 : 0;
   const size_t need = sizeof(BlobHeader) + (size_t)b->B * (8 + 4 + 4) + xs + (size_t)b->B * 2 * cs + rs;
   if (!blob) {
@@ -2852,7 +3071,7 @@ ravel_status ravel_buffer_save(ravel_buffer* b, void* blob, size_t* n) {
   HIP_TRY(hipDeviceSynchronize());
   char* p = (char*)blob;
   BlobHeader h{kMagic, b->B, c.horizon, c.action_dim, c.layers, c.prefix_len,
-               c.n_kv_heads * c.head_dim, c.dtype, c.model_kind, b->seed, 0, b->relative ? 1 : 0, 0};
+               c.n_kv_heads * c.head_dim, c.dtype, c.model_kind, b->seed, 0, b->relative ? 1 : 0, b->quant_block};
   HIP_TRY(hipMemcpy(&h.t, b->t, 8, hipMemcpyDeviceToHost));
   memcpy(p, &h, sizeof h);
   p += sizeof h;
@@ -2866,11 +3085,12 @@ ravel_status ravel_buffer_save(ravel_buffer* b, void* blob, size_t* n) {
   HIP_TRY(hipMemcpy(p, b->X, xs, hipMemcpyDeviceToHost));
   p += xs;
   for (int e = 0; e < b->B; ++e) {
-    const size_t off = ((size_t)b->active[e] * b->B + e) * cs;
-    if (cs) {
-      HIP_TRY(hipMemcpy(p, (char*)b->ctx_k + off, cs, hipMemcpyDeviceToHost));
-      HIP_TRY(hipMemcpy(p + cs, (char*)b->ctx_v + off, cs, hipMemcpyDeviceToHost));
-    }
+    char* q = p;
+    if (cs)
+      for (const auto& pc : ctx_pieces(b, e)) {
+        HIP_TRY(hipMemcpy(q, pc.first, pc.second, hipMemcpyDeviceToHost));
+        q += pc.second;
+      }
     p += 2 * cs;
   }
   if (b->relative) {
@@ -2887,10 +3107,13 @@ ravel_status ravel_buffer_load(ravel_buffer* b, const void* blob, size_t n) {
   if (!b || !blob) return fail(RAVEL_E_INVALID, "null argument");
   const ravel_config& c = b->m->cfg;
   const size_t xs = (size_t)b->B * c.horizon * c.action_dim * 4;
-  const size_t cs = b->ctx_elems * b->m->elt;
+  const size_t cs = ctx_blob_bytes(b);
   if (n < sizeof(BlobHeader)) return fail(RAVEL_E_INVALID, "blob too small");
   BlobHeader h;
   memcpy(&h, blob, sizeof h);
+  if (h.magic == kMagic && h.block != b->quant_block)
+    return fail(RAVEL_E_SHAPE, "checkpoint does not match this buffer's contexts (tokens per scale " +
+                                   std::to_string(h.block) + ", here " + std::to_string(b->quant_block) + ")");
   const size_t rs = h.relative ? (size_t)c.action_dim * 4 + (size_t)b->B * c.action_dim * 4 + (size_t)b->B * 4 : 0;
   const size_t need = sizeof(BlobHeader) + (size_t)b->B * (8 + 4 + 4) + xs + (size_t)b->B * 2 * cs + rs;
   if (n < need) return fail(RAVEL_E_INVALID, "blob too small");
@@ -2917,11 +3140,12 @@ ravel_status ravel_buffer_load(ravel_buffer* b, const void* blob, size_t n) {
   HIP_TRY(hipMemcpy(b->X, p, xs, hipMemcpyHostToDevice));
   p += xs;
   for (int e = 0; e < b->B; ++e) {
-    const size_t off = ((size_t)b->active[e] * b->B + e) * cs;
-    if (cs) {
-      HIP_TRY(hipMemcpy((char*)b->ctx_k + off, p, cs, hipMemcpyHostToDevice));
-      HIP_TRY(hipMemcpy((char*)b->ctx_v + off, p + cs, cs, hipMemcpyHostToDevice));
-    }
+    const char* q = p;
+    if (cs)
+      for (const auto& pc : ctx_pieces(b, e)) {
+        HIP_TRY(hipMemcpy(pc.first, q, pc.second, hipMemcpyHostToDevice));
+        q += pc.second;
+      }
     p += 2 * cs;
   }
   b->relative = h.relative != 0;

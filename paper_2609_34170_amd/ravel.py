@@ -72,7 +72,8 @@ SYMBOLS = [
     "ravel_publish_log", "ravel_buffer_query",
     "ravel_buffer_save", "ravel_buffer_load", "ravel_profile_step", "ravel_last_error",
     "ravel_cache_append", "ravel_cache_attention_workspace", "ravel_cache_attention", "ravel_cache_evict_workspace",
-    "ravel_cache_evict",
+    "ravel_cache_evict", "ravel_buffer_create_quantized", "ravel_context_track", "ravel_context_evict",
+    "ravel_context_cache",
 ]
 
 _lib = None
@@ -117,6 +118,10 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "ravel_cache_evict_workspace": ([ctypes.POINTER(RavelCache), i32, i32, ctypes.POINTER(i64)], i32),
         "ravel_cache_evict": ([ctypes.POINTER(RavelCache), i32, vp, i32, i32, ctypes.POINTER(RavelCache), vp, vp, vp,
                                i64, vp], i32),
+        "ravel_buffer_create_quantized": ([vp, i32, u64, i32, ctypes.POINTER(vp)], i32),
+        "ravel_context_track": ([vp, i32], i32),
+        "ravel_context_evict": ([vp, i32, i32, i32, vp], i32),
+        "ravel_context_cache": ([vp, i32, ctypes.POINTER(RavelCache)], i32),
     }
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
@@ -210,15 +215,19 @@ class Model:
 
 
 class Buffer:
-    """Rolling state of B environments (ravel_buffer_create)."""
+    """Rolling state of B environments (ravel_buffer_create); ``quantized``: tokens per scale of contexts held in 8 bits
+    (ravel_buffer_create_quantized), 0: contexts in the model's dtype."""
 
-    def __init__(self, model: Model, batch: int, seed: int = 0):
+    def __init__(self, model: Model, batch: int, seed: int = 0, quantized: int = 0):
         lib = load_library()
         self.model = model
         self.B = batch
         self.seed = seed
         h = ctypes.c_void_p()
-        _check(lib.ravel_buffer_create(model.h, batch, seed, ctypes.byref(h)))
+        if quantized:
+            _check(lib.ravel_buffer_create_quantized(model.h, batch, seed, int(quantized), ctypes.byref(h)))
+        else:
+            _check(lib.ravel_buffer_create(model.h, batch, seed, ctypes.byref(h)))
         self.h = h
 
     # -- options -----------------------------------------------------------
@@ -234,6 +243,30 @@ class Buffer:
 
     def set_context(self, env: int, k, v, t_obs: int, stream=None):
         _check(load_library().ravel_set_context(self.h, env, _ptr(k), _ptr(v), int(t_obs), _stream(stream)))
+
+    def track_context(self, on: bool = True):
+        _check(load_library().ravel_context_track(self.h, int(bool(on))))
+
+    def evict_context(self, env: int, keep: int, first: int = 0, stream=None):
+        _check(load_library().ravel_context_evict(self.h, env, int(keep), int(first), _stream(stream)))
+
+    def context_cache(self, env: int) -> "Cache":
+        """env's active context as a cache of ``layers`` sequences in the buffer's memory (which must outlive it)."""
+        import torch
+
+        c = RavelCache()
+        _check(load_library().ravel_context_cache(self.h, env, ctypes.byref(c)))
+        lead, blocks = (c.n_seq, c.n_kv_heads), -(-c.capacity // c.block)
+
+        def tensor(ptr, shape, kind):
+            at = type("DeviceMemory", (), {"__cuda_array_interface__": {
+                "shape": shape, "typestr": kind, "data": (ptr, False), "version": 2}})()
+            return torch.as_tensor(at, device="cuda")
+
+        code = lead + (c.capacity, c.head_dim)
+        return Cache(tensor(c.k, code, "|u1"), tensor(c.v, code, "|u1"), tensor(c.k_scale, lead + (blocks,), "<f4"),
+                     tensor(c.v_scale, lead + (blocks,), "<f4"), tensor(c.len, (c.n_seq,), "<i4"), c.block,
+                     weight=tensor(c.weight, lead + (c.capacity,), "<f4"))
 
     # -- hot path ----------------------------------------------------------
     def step(self, fop_tokens, action_out, stream=None):
