@@ -71,6 +71,18 @@ RAVEL_DEV void load8(const void* base, long long at, bf16x8_t (&p)[NP]) {
   }
 }
 
+// Blocks are dealt out to the 8 XCDs in turn; this numbering gives each XCD a run of
+// consecutive ones, so that those which read the same keys share an L2.
+RAVEL_DEV int xcd_block() {
+  const int n = gridDim.x, x = blockIdx.x & 7;
+  return x * (n >> 3) + min(x, n & 7) + (blockIdx.x >> 3);
+}
+
+// a buffer of `bytes` readable bytes from p on (uniform)
+RAVEL_DEV __amdgpu_buffer_rsrc_t buffer_of(const void* p, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00027000);
+}
+
 // Partial results of a key range: [split][batch][kv head][row]
 struct Part {
   float* o;   // [..][hd], unnormalised
@@ -153,7 +165,7 @@ __global__ __launch_bounds__(NW * 64) void cache_attn_kernel(CacheAttnArgs a, Pa
   const int G = a.nq / c.nkv, R = G * a.rows, row = chunk * 16 + l16;
   const int id = cache_seq(c, a.seq, b), n = id < 0 ? 0 : cache_len(c, id), S = id < 0 ? 0 : a.n_self;
   const int ct = (n + 31) >> 5, tiles = ct + ((S + 31) >> 5);
-  const int t0 = (int)((long long)tiles * split / part.nsplit), t1 = (int)((long long)tiles * (split + 1) / part.nsplit);
+  const int t0 = tiles * split / part.nsplit, t1 = tiles * (split + 1) / part.nsplit;  // (at most 64 splits)
   const long long head = (long long)max(id, 0) * c.nkv + g;
   const uint8_t *kc = c.k + head * c.cap * HD, *vc = c.v + head * c.cap * HD;
   const float *ksc = c.ks + head * c.nblk, *vsc = c.vs + head * c.nblk;
@@ -323,6 +335,331 @@ __global__ __launch_bounds__(NW * 64) void cache_attn_kernel(CacheAttnArgs a, Pa
   }
 }
 
+// ---------------------------------------------------------------------------
+// Many rows: a block of 8 waves owns 128 rows of a (batch row, kv head) and walks stages of 64
+// keys; wave (rg, kh) takes the 32 rows of group rg over the half kh of every stage, and the two
+// waves of a group are joined at the end.  (One wave a group with twice the keys would need more
+// than the 256 registers that vector instructions reach; two also overlap one's exponentials with
+// the other's matrix instructions where a CU holds one block.)  On the 32 x 32 matrix
+// instruction a lane owns one row of S^T and O^T, and 16 of each 32 keys (the other 16 the lane
+// 32 further on).
+//
+// Codes become bf16, scale included, on the way into LDS, where they lie as the call's own
+// tokens do (converted on the way into the products the four row groups would each repeat it, and
+// vector instructions bind as it is: matrix and vector instructions of a SIMD hardly overlap).
+// 16-byte chunks are XOR-swizzled by row, so that a fragment's rows fall on distinct
+// banks.  Values are read transposed: 16 lanes fetch 4 keys x 16 dims and each receives one
+// dim's 4 keys.  The next stage's codes are on their way into registers while one is computed on,
+// by buffer loads, which leave the addresses to scalar registers and give 0 past the last token.
+// One barrier a stage.
+// ---------------------------------------------------------------------------
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16_t;
+typedef __attribute__((__vector_size__(4 * sizeof(short)))) short s16x4_t;
+
+RAVEL_DEV uint32_t scaled2(uint32_t w, float s, bool hi) {
+  return __builtin_bit_cast(uint32_t, hi ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, true)
+                                         : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, false));
+}
+RAVEL_DEV bf16x8_t scaled8(uint32_t w0, uint32_t w1, float s) {
+  return __builtin_bit_cast(bf16x8_t, (u32x4_t{scaled2(w0, s, false), scaled2(w0, s, true), scaled2(w1, s, false),
+                                               scaled2(w1, s, true)}));
+}
+RAVEL_DEV f32x16_t mfma32(bf16x8_t a, bf16x8_t b, f32x16_t c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+typedef __attribute__((address_space(3))) char lds_char;
+RAVEL_DEV lds_char* lds_ptr(void* p) { return (lds_char*)p; }
+RAVEL_DEV float half_max(float x) {  // over a lane and the one 32 further on
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+RAVEL_DEV float half_sum(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+template <int HD>
+__global__ __launch_bounds__(512, 2) void cache_attn_tile_kernel(CacheAttnArgs a, Part part, int chunks) {
+  constexpr int RB = 128, SK = 64;  // rows of a block, keys of a stage
+  constexpr int KS = HD / 16, DT = HD / 32;
+  constexpr int CH = HD / 16;                     // 16-byte chunks of a token's codes
+  constexpr int CB = SK * HD;                     // bytes of a stage's codes (keys or values)
+  constexpr int NL = CB >= 8192 ? CB / 8192 : 1;  // 16-byte loads per thread
+  constexpr int CH2 = HD / 8;                     // the same of bf16 rows, as they lie in LDS
+  constexpr int TB = SK * 2 * HD;
+  constexpr int NL2 = TB >= 8192 ? TB / 8192 : 1;
+  constexpr int RP = CH2 >= 16 ? 1 : 16 / CH2;    // tokens per 256 bytes (all banks)
+  constexpr int XK = (CH2 < 16 ? CH2 : 16) - 1;   // swizzle masks: keys' fragments take 16 rows' same chunk,
+  constexpr int XV = (CH2 < 16 ? CH2 : 16) / 4 - 1;  // values' four rows' same four chunks
+  // two buffers of keys and values; at the end half of a row group's accumulators, then a wave's
+  // output rows
+  __shared__ __attribute__((aligned(1024))) char buf[4 * TB];
+  __shared__ float ml_s[RB][2];
+  // at 256 dims the last QL query fragments live in LDS: with all of them in registers some
+  // spill, and a reload waits for every load of the next stage
+  constexpr int QL = HD == 256 ? 7 : 0;
+  __shared__ __attribute__((aligned(16))) char q_s[QL ? 4 * QL * 1024 : 16];
+
+  const CacheView& c = a.c;
+  const int bid = xcd_block();
+  const int chunk = bid % chunks, split = bid / chunks % part.nsplit;
+  const int bg = bid / (part.nsplit * chunks), g = bg % c.nkv, b = bg / c.nkv;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rg = wave >> 1, kh = wave & 1;
+  const int l32 = lane & 31, h = lane >> 5;
+  const int G = a.nq / c.nkv, R = G * a.rows, row0 = chunk * RB + rg * 32, row = row0 + l32;
+  const bool idle = row0 >= R;  // a group without rows: stages keys, and no more
+  const int id = __builtin_amdgcn_readfirstlane(cache_seq(c, a.seq, b));
+  const int n = __builtin_amdgcn_readfirstlane(id < 0 ? 0 : cache_len(c, id)), S = id < 0 ? 0 : a.n_self;
+  const int st = (S + SK - 1) / SK, tiles = st + (n + SK - 1) / SK;
+  const int t0 = tiles * split / part.nsplit, t1 = tiles * (split + 1) / part.nsplit;  // (at most 64 splits)
+  const int c0 = max(t0 - st, 0), c1 = t1 - st;  // stages of cached tokens
+  const long long head = (long long)max(id, 0) * c.nkv + g;
+  const uint8_t *kc = c.k + head * c.cap * HD, *vc = c.v + head * c.cap * HD;
+  const float *ksc = c.ks + head * c.nblk, *vsc = c.vs + head * c.nblk;
+
+  // codes on their way to LDS, with the scales of their tokens: a stage starts on a scale block's
+  // border or, with 128 tokens to a scale, halfway
+  u32x4_t kl[NL], vl[NL];
+  float kscale[NL], vscale[NL];
+  const int cn = max(n - c0 * SK, 0), sblk = (c0 * SK) >> c.shift;
+  // (a key range holds less than 2^31 bytes)
+  const auto rk = buffer_of(kc + (long long)c0 * SK * HD, min(cn, (c1 - c0) * SK) * HD);
+  const auto rv = buffer_of(vc + (long long)c0 * SK * HD, min(cn, (c1 - c0) * SK) * HD);
+  const auto rks = buffer_of(ksc + sblk, (c.nblk - sblk) * 4), rvs = buffer_of(vsc + sblk, (c.nblk - sblk) * 4);
+  int voff[NL], soff[NL];
+#pragma unroll
+  for (int i = 0; i < NL; ++i) {
+    const int p = tid + i * 512;
+    voff[i] = CB < 8192 && p >= CB / 16 ? 0x7FFFFFF0 : p * 16;  // (past the end: nothing is read)
+    soff[i] = ((p / CH) >> c.shift) * 4;
+  }
+  const auto load = [&](int t) {
+    const int at = (t - c0) * CB, sat = (((t * SK) >> c.shift) - sblk) * 4;
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      kl[i] = __builtin_amdgcn_raw_buffer_load_b128(rk, voff[i], at, 0);
+      vl[i] = __builtin_amdgcn_raw_buffer_load_b128(rv, voff[i], at, 0);
+      kscale[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rks, soff[i], sat, 0));
+      vscale[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rvs, soff[i], sat, 0));
+    }
+  };
+  // chunk ch of row r in LDS
+  const auto k_at = [](int r, int ch) { return r * 2 * HD + ((ch ^ ((r / RP) & XK)) << 4); };
+  const auto v_at = [](int r, int ch) { return TB + r * 2 * HD + ((ch ^ ((r / RP) & XV) << 2) << 4); };
+  if (c0 < c1 && t0 >= st) load(c0);
+
+  bf16x8_t q[KS - QL];
+  {
+    const int r = min(row, R - 1);  // rows past the group are computed and never stored
+    const bf16_t* qr = (const bf16_t*)a.q + b * a.qb + r % a.rows * a.qr + (g * G + r / a.rows) * a.qh + h * 16;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const bf16x8_t x = *(const bf16x8_t*)(qr + (ks >> 1) * 32 + (ks & 1) * 8);
+      if (ks < KS - QL)
+        q[ks] = x;
+      else if (kh == 0)
+        *(bf16x8_t*)(q_s + (rg * QL + ks - (KS - QL)) * 1024 + lane * 16) = x;
+    }
+  }
+  f32x16_t o[DT];
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
+  float m = -INFINITY, l = 0.f;
+  const float sl2 = a.scale * kLog2e;
+
+  // LDS addresses of this lane's first fragments; the others' differ in bits that the swizzle
+  // leaves alone or only flips
+  const int ka0 = k_at(kh * 32 + l32, h * 2);
+  const int va0 = v_at(kh * 32 + 4 * h + ((lane & 15) >> 2), ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) + (lane & 1) * 8;
+
+  for (int t = t0; t < t1; ++t) {
+    char* const kb = buf + (t & 1) * 2 * TB;
+    int left;  // keys of this wave's half that are there; without any the probabilities are 0
+    if (t < st) {  // own tokens
+      left = S - t * SK - kh * 32;
+#pragma unroll
+      for (int i = 0; i < NL2; ++i) {
+        const int p = tid + i * 512, r = p / CH2, ch = p % CH2;
+        if (TB < 8192 && p >= TB / 16) break;
+        const long long at = b * a.sb + (long long)min(t * SK + r, S - 1) * a.st + g * a.sh + ch * 8;
+        *(u32x4_t*)(kb + k_at(r, ch)) = *(const u32x4_t*)((const bf16_t*)a.sk + at);
+        *(u32x4_t*)(kb + v_at(r, ch)) = *(const u32x4_t*)((const bf16_t*)a.sv + at);
+      }
+    } else {
+      left = n - (t - st) * SK - kh * 32;
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {
+        const int p = tid + i * 512, r = p / CH, ch = p % CH * 2;
+        if (CB < 8192 && p >= CB / 16) break;
+        const int ka = k_at(r, ch), va = v_at(r, ch);
+        *(bf16x8_t*)(kb + ka) = scaled8(kl[i][0], kl[i][1], kscale[i]);
+        *(bf16x8_t*)(kb + (ka ^ 16)) = scaled8(kl[i][2], kl[i][3], kscale[i]);
+        *(bf16x8_t*)(kb + va) = scaled8(vl[i][0], vl[i][1], vscale[i]);
+        *(bf16x8_t*)(kb + (va ^ 16)) = scaled8(vl[i][2], vl[i][3], vscale[i]);
+      }
+    }
+    __syncthreads();
+    if (t + 1 >= st && t + 1 < t1) load(t + 1 - st);
+
+    // scores: s[r] is key 8 (r / 4) + 4 h + r % 4; fragments are read ahead and the steps kept in order
+    int ka = ka0, va = va0;
+    asm volatile("" : "+v"(ka), "+v"(va));  // the addresses of the fragments are formed here, not kept
+    const auto read_k = [&](int ks) { return *(const bf16x8_t*)(kb + (ka ^ ((ks >> 1) << 6 | (ks & 1) << 4))); };
+    const auto read_v = [&](int j) {  // step j: 16 keys j / DT, dims j % DT
+      u32x2_t w[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        w[k] = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                               (__attribute__((address_space(3))) s16x4_t*)(lds_ptr(kb) + (va ^ (j % DT << 6)) +
+                                                                                            (16 * (j / DT) + 8 * k) * 2 * HD)));
+      return __builtin_bit_cast(bf16x8_t, (u32x4_t{w[0][0], w[0][1], w[1][0], w[1][1]}));
+    };
+    constexpr int PK = HD == 256 ? 2 : KS < 4 ? KS : 4, PV = HD == 256 ? 2 : 2 * DT < 4 ? 2 * DT : 4;
+    bf16x8_t kf[PK], vf[PV], ql[2];
+    f32x16_t s;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < PK; ++ks) kf[ks] = read_k(ks);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      if (ks + 1 >= KS - QL && ks + 1 < KS) ql[(ks + 1) & 1] = *(const bf16x8_t*)(q_s + (rg * QL + ks + 1 - (KS - QL)) * 1024 + lane * 16);
+      __builtin_amdgcn_sched_barrier(0);
+      if (ks < KS - QL)
+        s = mfma32(kf[ks % PK], q[ks], s);
+      else
+        s = mfma32(kf[ks % PK], ql[ks & 1], s);
+      if (ks + PK < KS) kf[ks % PK] = read_k(ks + PK);
+    }
+#pragma unroll
+    for (int j = 0; j < PV; ++j) vf[j] = read_v(j);
+    __builtin_amdgcn_sched_barrier(0);
+
+    float x[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) x[r] = s[r];
+    if (left < 32) {
+      const int mine = left - 4 * h;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        float y = 8 * (r >> 2) + (r & 3) < mine ? x[r] : -INFINITY;
+        asm volatile("" : "+v"(y));  // stays in its branch
+        x[r] = y;
+      }
+    }
+    float mx = x[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, x[r]);
+    mx = half_max(mx) * sl2;
+    if (__any(mx > m + kLazy)) {
+      const float mnew = mx > m + kLazy ? mx : m;
+      const float corr = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mnew);
+      m = mnew;
+      l *= corr;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[d][r] *= corr;
+    }
+    const float mref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], sl2, -mref));
+#pragma unroll
+    for (int r = 0; r < 16; r += 4) l += (x[r] + x[r + 1]) + (x[r + 2] + x[r + 3]);
+    bf16x8_t p[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      p[i] = __builtin_bit_cast(bf16x8_t, (u32x4_t{pack_bf16x2(x[8 * i], x[8 * i + 1]), pack_bf16x2(x[8 * i + 2], x[8 * i + 3]),
+                                                   pack_bf16x2(x[8 * i + 4], x[8 * i + 5]), pack_bf16x2(x[8 * i + 6], x[8 * i + 7])}));
+#pragma unroll
+    for (int j = 0; j < 2 * DT; ++j) {
+      __builtin_amdgcn_sched_barrier(0);
+      o[j % DT] = mfma32(vf[j % PV], p[j / DT], o[j % DT]);
+      if (j + PV < 2 * DT) vf[j % PV] = read_v(j + PV);
+    }
+  }
+
+  // join the two waves of a row group (their lanes hold the same dims of the same rows), half of
+  // the accumulators at a time: each wave gives one half and keeps the other
+  l = half_sum(l);
+  __syncthreads();  // the buffers are free
+  if (kh == 1 && h == 0) {
+    ml_s[rg * 32 + l32][0] = m;
+    ml_s[rg * 32 + l32][1] = l;
+  }
+  float* jb = (float*)buf + rg * DT * 8 * 64 + lane;  // (a group: 32 rows of 2 HD bytes)
+  constexpr int HR = DT * 16;  // accumulators of a lane
+  if (kh == 1) {
+#pragma unroll
+    for (int r = 0; r < HR / 2; ++r) jb[r * 64] = o[r / 16][r % 16];
+  }
+  __syncthreads();
+  float mm = m, w0 = 1.f, w1 = 0.f, den = l;
+  if (kh == 0) {
+    const float m1 = ml_s[rg * 32 + l32][0], l1 = ml_s[rg * 32 + l32][1];
+    mm = fmaxf(m, m1);
+    const float ref = mm == -INFINITY ? 0.f : mm;
+    w0 = __builtin_amdgcn_exp2f(m - ref);
+    w1 = __builtin_amdgcn_exp2f(m1 - ref);
+    den = w0 * l + w1 * l1;
+#pragma unroll
+    for (int r = 0; r < HR / 2; ++r) o[r / 16][r % 16] = o[r / 16][r % 16] * w0 + jb[r * 64] * w1;
+  }
+  __syncthreads();
+  if (kh == 1) {
+#pragma unroll
+    for (int r = HR / 2; r < HR; ++r) jb[(r - HR / 2) * 64] = o[r / 16][r % 16];
+  }
+  __syncthreads();
+  if (kh == 1 || idle) return;
+#pragma unroll
+  for (int r = HR / 2; r < HR; ++r) o[r / 16][r % 16] = o[r / 16][r % 16] * w0 + jb[(r - HR / 2) * 64] * w1;
+  // o[d][r]: dim 32 d + 8 (r / 4) + 4 h + r % 4
+  if (part.nsplit > 1) {
+    if (row >= R) return;
+    const long long pr = (((long long)split * a.batch + b) * c.nkv + g) * R + row;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4)
+        *(f32x4_t*)(part.o + pr * HD + d * 32 + r * 2 + h * 4) = f32x4_t{o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]};
+    if (h == 0) {
+      part.ml[pr * 2] = mm;
+      part.ml[pr * 2 + 1] = den;
+    }
+    return;
+  }
+  const float inv = den == 0.f ? 0.f : 1.f / den;  // a row that sees nothing: 0
+  if (part.lse && h == 0 && row < R) part.lse[((long long)b * c.nkv + g) * R + row] = den == 0.f ? INFINITY : mm + log2f(den);
+  // through LDS (this group's part of the join's), so that whole rows are written: 8-byte pieces
+  // XOR-swizzled by row
+  constexpr int PX = HD / 4 - 1 < 31 ? HD / 4 - 1 : 31;
+  char* ob = buf + rg * 64 * HD;
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; r += 4)
+      *(u32x2_t*)(ob + l32 * 2 * HD + (((8 * d + r / 2 + h) ^ (l32 * 2 & PX)) << 3)) =
+          u32x2_t{pack_bf16x2(o[d][r] * inv, o[d][r + 1] * inv), pack_bf16x2(o[d][r + 2] * inv, o[d][r + 3] * inv)};
+  constexpr int RS = 512 / HD;  // rows a store
+  int r = lane / (HD / 8), ix = (row0 + r) % a.rows, hx = (row0 + r) / a.rows;
+  const int x = lane % (HD / 8);
+#pragma unroll 4
+  for (int i = 0; i < HD / 16; ++i) {
+    const u32x4_t w = *(const u32x4_t*)(ob + r * 2 * HD + (((2 * x) ^ (r * 2 & PX)) << 3));
+    if (row0 + r < R) *(u32x4_t*)((bf16_t*)a.out + b * a.ob + ix * a.orow + (g * G + hx) * a.oh + x * 8) = w;
+    r += RS;
+    ix += RS;
+    while (ix >= a.rows) {
+      ix -= a.rows;
+      ++hx;
+    }
+  }
+}
+
 // The key ranges joined in range order, four dims a thread.
 template <bool F32>
 __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a, Part part) {
@@ -418,6 +755,7 @@ __global__ __launch_bounds__(NW * 64) void cache_weight_kernel(CacheAttnArgs a, 
 }
 
 struct Plan {
+  bool tile;
   int chunks, nsplit;
   size_t o_off, ml_off, lse_off, bytes;
 };
@@ -426,10 +764,13 @@ size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 Plan plan_of(const CacheAttnArgs& a) {
   Plan p;
   const long long R = (long long)(a.nq / a.c.nkv) * a.rows, heads = (long long)a.batch * a.c.nkv;
-  p.chunks = (int)((R + 15) / 16);
-  const long long blocks = p.chunks * heads, tiles = (a.c.cap + 31) / 32 + (a.n_self + 31) / 32;
-  // two blocks a CU, at least one tile a wave in every key range
-  p.nsplit = (int)std::max(1ll, std::min({512 / std::max(blocks, 1ll), tiles / NW, 64ll}));
+  p.tile = !a.f32 && R > 32;
+  const int rows = p.tile ? 128 : 16, keys = p.tile ? 64 : 32 * NW;
+  p.chunks = (int)((R + rows - 1) / rows);
+  const long long blocks = p.chunks * heads, tiles = (a.c.cap + keys - 1) / keys + (a.n_self + keys - 1) / keys;
+  // one (tile) or two blocks a CU, at least one tile a wave in every key range
+  p.nsplit = (int)std::max(1ll, std::min({(p.tile ? 256 : 512) / std::max(blocks, 1ll), tiles, 64ll}));
+  if (p.tile) p.nsplit = std::max(p.nsplit, (int)(((long long)a.c.cap * a.c.hd >> 30) + 1));  // 32-bit offsets in a range
   p.o_off = 0;
   p.ml_off = p.nsplit > 1 ? up256((size_t)p.nsplit * heads * R * a.c.hd * 4) : 0;
   p.lse_off = p.ml_off + (p.nsplit > 1 ? up256((size_t)p.nsplit * heads * R * 8) : 0);
@@ -445,7 +786,11 @@ hipError_t launch_hd(const CacheAttnArgs& a, hipStream_t s) {
   const Part part{(float*)(ws + p.o_off), (float*)(ws + p.ml_off), a.track ? (float*)(ws + p.lse_off) : nullptr, p.nsplit};
   const long long blocks = p.chunks * heads * p.nsplit, joins = (heads * R * (HD / 4) + 255) / 256;
   if (blocks > 0x7FFFFFFF || joins > 0x7FFFFFFF) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((cache_attn_kernel<HD, F32>), dim3((unsigned)blocks), dim3(NW * 64), 0, s, a, part, p.chunks);
+  if constexpr (!F32) {
+    if (p.tile) hipLaunchKernelGGL((cache_attn_tile_kernel<HD>), dim3((unsigned)blocks), dim3(512), 0, s, a, part, p.chunks);
+  }
+  if (!p.tile)
+    hipLaunchKernelGGL((cache_attn_kernel<HD, F32>), dim3((unsigned)blocks), dim3(NW * 64), 0, s, a, part, p.chunks);
   if (p.nsplit > 1) hipLaunchKernelGGL(cache_join_kernel<F32>, dim3((unsigned)joins), dim3(256), 0, s, a, part);
   if (a.track)
     hipLaunchKernelGGL((cache_weight_kernel<HD, F32>), dim3((a.c.cap + 32 * NW - 1) / (32 * NW), a.c.nkv, a.batch),
