@@ -380,7 +380,8 @@ RAVEL_DEV float half_sum(float x) {
 
 template <int HD>
 __global__ __launch_bounds__(512, 2) void cache_attn_tile_kernel(CacheAttnArgs a, Part part, int chunks) {
-  constexpr int RB = 128, SK = 64;  // rows of a block, keys of a stage
+  // rows of a block, 32-key tiles of a wave in a stage (256 dims: LDS holds one for each), keys of a stage
+  constexpr int RB = 128, NT = HD == 256 ? 1 : 2, SK = 64 * NT;
   constexpr int KS = HD / 16, DT = HD / 32;
   constexpr int CH = HD / 16;                     // 16-byte chunks of a token's codes
   constexpr int CB = SK * HD;                     // bytes of a stage's codes (keys or values)
@@ -418,8 +419,8 @@ __global__ __launch_bounds__(512, 2) void cache_attn_tile_kernel(CacheAttnArgs a
   const uint8_t *kc = c.k + head * c.cap * HD, *vc = c.v + head * c.cap * HD;
   const float *ksc = c.ks + head * c.nblk, *vsc = c.vs + head * c.nblk;
 
-  // codes on their way to LDS, with the scales of their tokens: a stage starts on a scale block's
-  // border or, with 128 tokens to a scale, halfway
+  // codes on their way to LDS, with the scales of their tokens (a stage starts on a scale block's
+  // border or, stages of 64 with 128 tokens to a scale, halfway)
   u32x4_t kl[NL], vl[NL];
   float kscale[NL], vscale[NL];
   const int cn = max(n - c0 * SK, 0), sblk = (c0 * SK) >> c.shift;
@@ -427,21 +428,18 @@ __global__ __launch_bounds__(512, 2) void cache_attn_tile_kernel(CacheAttnArgs a
   const auto rk = buffer_of(kc + (long long)c0 * SK * HD, min(cn, (c1 - c0) * SK) * HD);
   const auto rv = buffer_of(vc + (long long)c0 * SK * HD, min(cn, (c1 - c0) * SK) * HD);
   const auto rks = buffer_of(ksc + sblk, (c.nblk - sblk) * 4), rvs = buffer_of(vsc + sblk, (c.nblk - sblk) * 4);
-  int voff[NL], soff[NL];
-#pragma unroll
-  for (int i = 0; i < NL; ++i) {
-    const int p = tid + i * 512;
-    voff[i] = CB < 8192 && p >= CB / 16 ? 0x7FFFFFF0 : p * 16;  // (past the end: nothing is read)
-    soff[i] = ((p / CH) >> c.shift) * 4;
-  }
+  // a thread's loads lie 8 KB apart: LR tokens, whole scale blocks or inside one
+  constexpr int LR = 512 / CH;
+  const int voff = CB < 8192 && tid >= CB / 16 ? 0x7FFFFFF0 : tid * 16;  // (past the end: nothing is read)
+  const int soff = (tid / CH >> c.shift) * 4;
   const auto load = [&](int t) {
     const int at = (t - c0) * CB, sat = (((t * SK) >> c.shift) - sblk) * 4;
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-      kl[i] = __builtin_amdgcn_raw_buffer_load_b128(rk, voff[i], at, 0);
-      vl[i] = __builtin_amdgcn_raw_buffer_load_b128(rv, voff[i], at, 0);
-      kscale[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rks, soff[i], sat, 0));
-      vscale[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rvs, soff[i], sat, 0));
+      kl[i] = __builtin_amdgcn_raw_buffer_load_b128(rk, voff, at + i * 8192, 0);
+      vl[i] = __builtin_amdgcn_raw_buffer_load_b128(rv, voff, at + i * 8192, 0);
+      kscale[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rks, soff, sat + (i * LR >> c.shift) * 4, 0));
+      vscale[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rvs, soff, sat + (i * LR >> c.shift) * 4, 0));
     }
   };
   // chunk ch of row r in LDS
@@ -472,14 +470,14 @@ __global__ __launch_bounds__(512, 2) void cache_attn_tile_kernel(CacheAttnArgs a
 
   // LDS addresses of this lane's first fragments; the others' differ in bits that the swizzle
   // leaves alone or only flips
-  const int ka0 = k_at(kh * 32 + l32, h * 2);
-  const int va0 = v_at(kh * 32 + 4 * h + ((lane & 15) >> 2), ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) + (lane & 1) * 8;
+  const int ka0 = k_at(kh * 32 * NT + l32, h * 2);
+  const int va0 = v_at(kh * 32 * NT + 4 * h + ((lane & 15) >> 2), ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) + (lane & 1) * 8;
 
   for (int t = t0; t < t1; ++t) {
     char* const kb = buf + (t & 1) * 2 * TB;
-    int left;  // keys of this wave's half that are there; without any the probabilities are 0
+    int left;  // keys of this wave's part that are there; without any the probabilities are 0
     if (t < st) {  // own tokens
-      left = S - t * SK - kh * 32;
+      left = S - t * SK - kh * 32 * NT;
 #pragma unroll
       for (int i = 0; i < NL2; ++i) {
         const int p = tid + i * 512, r = p / CH2, ch = p % CH2;
@@ -489,7 +487,7 @@ __global__ __launch_bounds__(512, 2) void cache_attn_tile_kernel(CacheAttnArgs a
         *(u32x4_t*)(kb + v_at(r, ch)) = *(const u32x4_t*)((const bf16_t*)a.sv + at);
       }
     } else {
-      left = n - (t - st) * SK - kh * 32;
+      left = n - (t - st) * SK - kh * 32 * NT;
 #pragma unroll
       for (int i = 0; i < NL; ++i) {
         const int p = tid + i * 512, r = p / CH, ch = p % CH * 2;
@@ -504,10 +502,15 @@ __global__ __launch_bounds__(512, 2) void cache_attn_tile_kernel(CacheAttnArgs a
     __syncthreads();
     if (t + 1 >= st && t + 1 < t1) load(t + 1 - st);
 
-    // scores: s[r] is key 8 (r / 4) + 4 h + r % 4; fragments are read ahead and the steps kept in order
+    // Fragments are read ahead, and the steps keep their order: with two tiles the exponentials of
+    // the first lie between the matrix instructions of the second's scores, those of the
+    // second between the first's of the second product.
     int ka = ka0, va = va0;
     asm volatile("" : "+v"(ka), "+v"(va));  // the addresses of the fragments are formed here, not kept
-    const auto read_k = [&](int ks) { return *(const bf16x8_t*)(kb + (ka ^ ((ks >> 1) << 6 | (ks & 1) << 4))); };
+    const auto read_k = [&](int j) {  // step j: tile j / KS, dims j % KS
+      const int ks = j % KS;
+      return *(const bf16x8_t*)(kb + (ka ^ ((ks >> 1) << 6 | (ks & 1) << 4)) + j / KS * 64 * HD);
+    };
     const auto read_v = [&](int j) {  // step j: 16 keys j / DT, dims j % DT
       u32x2_t w[2];
 #pragma unroll
@@ -519,66 +522,101 @@ __global__ __launch_bounds__(512, 2) void cache_attn_tile_kernel(CacheAttnArgs a
     };
     constexpr int PK = HD == 256 ? 2 : KS < 4 ? KS : 4, PV = HD == 256 ? 2 : 2 * DT < 4 ? 2 * DT : 4;
     bf16x8_t kf[PK], vf[PV], ql[2];
-    f32x16_t s;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) s[r] = 0.f;
-#pragma unroll
-    for (int ks = 0; ks < PK; ++ks) kf[ks] = read_k(ks);
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      if (ks + 1 >= KS - QL && ks + 1 < KS) ql[(ks + 1) & 1] = *(const bf16x8_t*)(q_s + (rg * QL + ks + 1 - (KS - QL)) * 1024 + lane * 16);
-      __builtin_amdgcn_sched_barrier(0);
-      if (ks < KS - QL)
-        s = mfma32(kf[ks % PK], q[ks], s);
-      else
-        s = mfma32(kf[ks % PK], ql[ks & 1], s);
-      if (ks + PK < KS) kf[ks % PK] = read_k(ks + PK);
-    }
-#pragma unroll
-    for (int j = 0; j < PV; ++j) vf[j] = read_v(j);
-    __builtin_amdgcn_sched_barrier(0);
-
+    f32x16_t s[NT];
     float x[16];
+    uint32_t pw[NT][8];  // probabilities: each tile's two B operands of the second product
+    float mref = 0.f;
+    // s[u][r] is key 32 u + 8 (r / 4) + 4 h + r % 4: masked, and the running maximum moved where it has to
+    const auto maximum = [&](int u) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) x[r] = s[r];
-    if (left < 32) {
-      const int mine = left - 4 * h;
+      for (int r = 0; r < 16; ++r) x[r] = s[u][r];
+      if (left < 32 * (u + 1)) {
+        const int mine = left - 32 * u - 4 * h;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        float y = 8 * (r >> 2) + (r & 3) < mine ? x[r] : -INFINITY;
-        asm volatile("" : "+v"(y));  // stays in its branch
-        x[r] = y;
+        for (int r = 0; r < 16; ++r) {
+          float y = 8 * (r >> 2) + (r & 3) < mine ? x[r] : -INFINITY;
+          asm volatile("" : "+v"(y));  // stays in its branch
+          x[r] = y;
+        }
       }
+      float mx = x[0];
+#pragma unroll
+      for (int r = 1; r < 16; ++r) mx = fmaxf(mx, x[r]);
+      mx = half_max(mx) * sl2;
+      if (__any(mx > m + kLazy)) {
+        const float mnew = mx > m + kLazy ? mx : m;
+        const float corr = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mnew);
+        m = mnew;
+        l *= corr;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[d][r] *= corr;
+        if (u == 1) {  // the first tile's are not in the sums yet (and rounded a second time here)
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            pw[0][i] = pack_bf16x2(__uint_as_float(pw[0][i] << 16) * corr, __uint_as_float(pw[0][i] & 0xFFFF0000u) * corr);
+        }
+      }
+      mref = m == -INFINITY ? 0.f : m;
+    };
+    const auto exponentials = [&](int u, int e0, int e1) {
+#pragma unroll
+      for (int e = e0; e < e1; ++e) {
+        x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], sl2, -mref));
+        if (e & 1) {
+          l += x[e - 1] + x[e];
+          pw[u][e >> 1] = pack_bf16x2(x[e - 1], x[e]);
+        }
+      }
+    };
+    const auto scores = [&](int u) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[u][r] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const int j = u * KS + ks;
+        if (ks + 1 >= KS - QL && ks + 1 < KS) ql[(ks + 1) & 1] = *(const bf16x8_t*)(q_s + (rg * QL + ks + 1 - (KS - QL)) * 1024 + lane * 16);
+        if (u == 1) exponentials(0, ks * 16 / KS, (ks + 1) * 16 / KS);
+        __builtin_amdgcn_sched_barrier(0);
+        if (ks < KS - QL)
+          s[u] = mfma32(kf[j % PK], q[ks], s[u]);
+        else
+          s[u] = mfma32(kf[j % PK], ql[ks & 1], s[u]);
+        if (j + PK < NT * KS) kf[j % PK] = read_k(j + PK);
+      }
+    };
+    const auto outputs = [&](int u) {
+#pragma unroll
+      for (int i = 0; i < 2 * DT; ++i) {
+        const int j = u * 2 * DT + i;
+        if (u == 0 && NT == 2) exponentials(1, i * 8 / DT, (i + 1) * 8 / DT);
+        __builtin_amdgcn_sched_barrier(0);
+        const uint32_t* w = &pw[u][i / DT * 4];
+        o[i % DT] = mfma32(vf[j % PV], __builtin_bit_cast(bf16x8_t, (u32x4_t{w[0], w[1], w[2], w[3]})), o[i % DT]);
+        if (j + PV < NT * 2 * DT) vf[j % PV] = read_v(j + PV);
+      }
+    };
+#pragma unroll
+    for (int j = 0; j < PK; ++j) kf[j] = read_k(j);
+    scores(0);
+    if constexpr (NT == 2) {
+      maximum(0);
+      scores(1);
     }
-    float mx = x[0];
+    if constexpr (NT == 2) {
 #pragma unroll
-    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, x[r]);
-    mx = half_max(mx) * sl2;
-    if (__any(mx > m + kLazy)) {
-      const float mnew = mx > m + kLazy ? mx : m;
-      const float corr = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mnew);
-      m = mnew;
-      l *= corr;
-#pragma unroll
-      for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) o[d][r] *= corr;
-    }
-    const float mref = m == -INFINITY ? 0.f : m;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], sl2, -mref));
-#pragma unroll
-    for (int r = 0; r < 16; r += 4) l += (x[r] + x[r + 1]) + (x[r + 2] + x[r + 3]);
-    bf16x8_t p[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      p[i] = __builtin_bit_cast(bf16x8_t, (u32x4_t{pack_bf16x2(x[8 * i], x[8 * i + 1]), pack_bf16x2(x[8 * i + 2], x[8 * i + 3]),
-                                                   pack_bf16x2(x[8 * i + 4], x[8 * i + 5]), pack_bf16x2(x[8 * i + 6], x[8 * i + 7])}));
-#pragma unroll
-    for (int j = 0; j < 2 * DT; ++j) {
+      for (int j = 0; j < PV; ++j) vf[j] = read_v(j);
       __builtin_amdgcn_sched_barrier(0);
-      o[j % DT] = mfma32(vf[j % PV], p[j / DT], o[j % DT]);
-      if (j + PV < 2 * DT) vf[j % PV] = read_v(j + PV);
+      maximum(1);
+      outputs(0);
+      outputs(1);
+    } else {
+      maximum(0);
+      exponentials(0, 0, 16);
+#pragma unroll
+      for (int j = 0; j < PV; ++j) vf[j] = read_v(j);
+      outputs(0);
     }
   }
 
@@ -765,7 +803,7 @@ Plan plan_of(const CacheAttnArgs& a) {
   Plan p;
   const long long R = (long long)(a.nq / a.c.nkv) * a.rows, heads = (long long)a.batch * a.c.nkv;
   p.tile = !a.f32 && R > 32;
-  const int rows = p.tile ? 128 : 16, keys = p.tile ? 64 : 32 * NW;
+  const int rows = p.tile ? 128 : 16, keys = !p.tile || a.c.hd < 256 ? 128 : 64;
   p.chunks = (int)((R + rows - 1) / rows);
   const long long blocks = p.chunks * heads, tiles = (a.c.cap + keys - 1) / keys + (a.n_self + keys - 1) / keys;
   // one (tile) or two blocks a CU, at least one tile a wave in every key range
