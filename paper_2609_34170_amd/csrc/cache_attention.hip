@@ -698,29 +698,46 @@ __global__ __launch_bounds__(512, 2) void cache_attn_tile_kernel(CacheAttnArgs a
   }
 }
 
-// The key ranges joined in range order, four dims a thread.
+// The key ranges joined in range order, four dims a thread, eight ranges' loads in flight (one
+// after the other, 64 ranges are 64 round trips to memory: 18 us).
 template <bool F32>
-__global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a, Part part) {
+__global__ __launch_bounds__(64) void cache_join_kernel(CacheAttnArgs a, Part part) {
   const CacheView& c = a.c;
   const int G = a.nq / c.nkv, R = G * a.rows, Q4 = c.hd / 4;
-  const long long rows = (long long)a.batch * c.nkv * R, i = (long long)blockIdx.x * 256 + threadIdx.x;
+  const long long rows = (long long)a.batch * c.nkv * R, i = (long long)blockIdx.x * 64 + threadIdx.x;
   if (i >= rows * Q4) return;
   const long long pr = i / Q4;
   const int d = (int)(i % Q4) * 4, rr = (int)(pr % R), g = (int)(pr / R % c.nkv), b = (int)(pr / R / c.nkv);
-  float mm = -INFINITY;
-  for (int s = 0; s < part.nsplit; ++s) mm = fmaxf(mm, part.ml[(s * rows + pr) * 2]);
-  const float mref = mm == -INFINITY ? 0.f : mm;
-  float num[4] = {0.f, 0.f, 0.f, 0.f}, den = 0.f;
-  for (int s = 0; s < part.nsplit; ++s) {
-    const float2 ml = *(const float2*)(part.ml + (s * rows + pr) * 2);
-    const float wt = __builtin_amdgcn_exp2f(ml.x - mref);
-    const f32x4_t v = *(const f32x4_t*)(part.o + (s * rows + pr) * c.hd + d);
-    den += wt * ml.y;
+  float m = -INFINITY, den = 0.f;
+  f32x4_t num = {0.f, 0.f, 0.f, 0.f};
+  for (int s0 = 0; s0 < part.nsplit; s0 += 8) {
+    float2 ml[8];
+    f32x4_t v[8];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) num[k] += wt * v[k];
+    for (int k = 0; k < 8; ++k) {
+      const long long at = (long long)min(s0 + k, part.nsplit - 1) * rows + pr;
+      ml[k] = *(const float2*)(part.ml + at * 2);
+      v[k] = *(const f32x4_t*)(part.o + at * c.hd + d);
+    }
+    __builtin_amdgcn_sched_barrier(0);  // without it the compiler sinks the loads to their uses
+    float mx = m;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) mx = fmaxf(mx, ml[k].x);
+    const float ref = mx == -INFINITY ? 0.f : mx, corr = __builtin_amdgcn_exp2f(m - ref);
+    m = mx;
+    den *= corr;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) num[j] *= corr;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float wt = s0 + k < part.nsplit ? __builtin_amdgcn_exp2f(ml[k].x - ref) : 0.f;
+      den += wt * ml[k].y;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) num[j] += wt * v[k][j];
+    }
   }
   const float inv = den == 0.f ? 0.f : 1.f / den;
-  if (part.lse && d == 0) part.lse[pr] = den == 0.f ? INFINITY : mref + log2f(den);
+  if (part.lse && d == 0) part.lse[pr] = den == 0.f ? INFINITY : m + log2f(den);
   const long long at = b * a.ob + rr % a.rows * a.orow + (g * G + rr / a.rows) * a.oh + d;
   if constexpr (F32)
     *(f32x4_t*)((float*)a.out + at) = f32x4_t{num[0] * inv, num[1] * inv, num[2] * inv, num[3] * inv};
@@ -728,68 +745,90 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a, Part p
     *(u32x2_t*)((bf16_t*)a.out + at) = u32x2_t{pack_bf16x2(num[0] * inv, num[1] * inv), pack_bf16x2(num[2] * inv, num[3] * inv)};
 }
 
-// Accumulated weights: every wave owns 32 keys of a (sequence, kv head), forms their scores
-// once more and adds 2^(score - lse) over all rows.  Batch rows that name one sequence are
-// added in row order by the first of them, so that the sums have one order.
+// Accumulated weights: a block owns 64 keys of a (sequence, kv head), forms their scores with
+// every row once more, 32 rows at a time dealt out to its waves, and adds 2^(score - lse).  Rows
+// are the first operand's here: a lane owns a key of each of two tiles and adds over its
+// registers.  Batch rows that name one sequence are added in row order by the first of them, so
+// that the sums have one order.
 template <int HD, bool F32>
 __global__ __launch_bounds__(NW * 64) void cache_weight_kernel(CacheAttnArgs a, const float* lse) {
-  constexpr int KS = HD / 32, NP = F32 ? 3 : 1;
+  constexpr int KS = HD / 16, NP = F32 ? 3 : 1;
+  __shared__ float sum_s[NW][64];
   const CacheView& c = a.c;
-  const int g = blockIdx.y, b0 = blockIdx.z;
-  const int id = cache_seq(c, a.seq, b0);
+  const int bid = xcd_block(), nkt = (c.cap + 63) / 64;
+  const int g = bid / nkt % c.nkv, b0 = bid / nkt / c.nkv;
+  const int id = __builtin_amdgcn_readfirstlane(cache_seq(c, a.seq, b0));
   if (id < 0 || cache_seq_before(c, a.seq, b0, id)) return;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int l16 = lane & 15, grp = lane >> 4;
-  const int n = cache_len(c, id), key0 = (blockIdx.x * NW + wave) * 32;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l32 = lane & 31, h = lane >> 5;
+  const int n = cache_len(c, id), key0 = bid % nkt * 64;
   if (key0 >= n) return;
   const int G = a.nq / c.nkv, R = G * a.rows;
   const long long head = (long long)id * c.nkv + g;
   bf16x8_t kf[2][KS];
-  float k2[2];
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
-    const int key = min(key0 + 16 * u, n - 1);
-    k2[u] = c.ks[head * c.nblk + (key >> c.shift)] * (a.scale * kLog2e);
-    const uint8_t* p = c.k + (head * c.cap + min(key0 + 16 * u + l16, n - 1)) * HD;
+    const int key = min(key0 + 32 * u + l32, n - 1);
+    const float sc = c.ks[head * c.nblk + (key >> c.shift)];
+    const uint8_t* p = c.k + (head * c.cap + key) * HD + h * 16;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      const u32x2_t w = *(const u32x2_t*)(p + kdim<HD>(ks, grp));
-      kf[u][ks] = codes8(w[0], w[1]);
+    for (int j = 0; j < KS / 2; ++j) {
+      const u32x4_t w = *(const u32x4_t*)(p + j * 32);
+      kf[u][2 * j] = scaled8(w[0], w[1], sc);
+      kf[u][2 * j + 1] = scaled8(w[2], w[3], sc);
     }
   }
-  float acc[2][4] = {};
+  const float sl2 = a.scale * kLog2e;
+  float acc[2] = {0.f, 0.f};
   for (int b = b0; b < a.batch; ++b) {
     if (b != b0 && cache_seq(c, a.seq, b) != id) continue;
-    for (int r0 = 0; r0 < R; r0 += 16) {
-      const int row = r0 + l16, r = min(row, R - 1);
-      const long long at = b * a.qb + r % a.rows * a.qr + (g * G + r / a.rows) * a.qh;
-      const float ls = row < R ? lse[((long long)b * c.nkv + g) * R + row] : INFINITY;
-      f32x4_t s[2] = {f32x4_t{0.f, 0.f, 0.f, 0.f}, f32x4_t{0.f, 0.f, 0.f, 0.f}};
+    const float* lr = lse + ((long long)b * c.nkv + g) * R;
+    for (int r0 = wave * 32; r0 < R; r0 += NW * 32) {
+      const int r = min(r0 + l32, R - 1);
+      const long long at = b * a.qb + r % a.rows * a.qr + (g * G + r / a.rows) * a.qh + h * 16;
+      // 32 bits: planes are made fragment by fragment; bf16: every fragment on its way at once
+      bf16x8_t q[F32 ? 1 : KS][NP];
+      if constexpr (!F32) {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) load8<false>(a.q, at + (ks >> 1) * 32 + (ks & 1) * 8, q[ks]);
+      }
+      float ls[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int rr = r0 + 8 * (i >> 2) + 4 * h + (i & 3);
+        ls[i] = rr < R ? lr[min(rr, R - 1)] : INFINITY;
+      }
+      f32x16_t s[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[u][i] = 0.f;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        bf16x8_t q[NP];
-        load8<F32>(a.q, at + kdim<HD>(ks, grp), q);
+        if constexpr (F32) load8<true>(a.q, at + (ks >> 1) * 32 + (ks & 1) * 8, q[0]);
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
-          for (int p = NP - 1; p >= 0; --p) s[u] = mfma_bf16(kf[u][ks], q[p], s[u]);
+          for (int p = NP - 1; p >= 0; --p) s[u] = mfma32(q[F32 ? 0 : ks][p], kf[u][ks], s[u]);
       }
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) acc[u][k] += __builtin_amdgcn_exp2f(s[u][k] * k2[u] - ls);
+        for (int i = 0; i < 16; ++i) acc[u] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i], sl2, -ls[i]));
     }
   }
 #pragma unroll
-  for (int u = 0; u < 2; ++u)
+  for (int u = 0; u < 2; ++u) {
+    acc[u] = half_sum(acc[u]);
+    if (h == 0) sum_s[wave][u * 32 + l32] = acc[u];
+  }
+  __syncthreads();
+  if (tid < 64 && key0 + tid < n) {
+    float v = sum_s[0][tid];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      float v = acc[u][k];
-#pragma unroll
-      for (int off = 1; off < 16; off <<= 1) v += __shfl_xor(v, off, 64);
-      const int key = key0 + 16 * u + 4 * grp + k;
-      if (l16 == 0 && key < n) c.weight[head * c.cap + key] += v;
-    }
+    for (int w = 1; w < NW; ++w) v += sum_s[w][tid];
+    c.weight[head * c.cap + key0 + tid] += v;
+  }
 }
 
 struct Plan {
@@ -822,17 +861,17 @@ hipError_t launch_hd(const CacheAttnArgs& a, hipStream_t s) {
   const long long heads = (long long)a.batch * a.c.nkv, R = (long long)(a.nq / a.c.nkv) * a.rows;
   char* ws = (char*)a.ws;
   const Part part{(float*)(ws + p.o_off), (float*)(ws + p.ml_off), a.track ? (float*)(ws + p.lse_off) : nullptr, p.nsplit};
-  const long long blocks = p.chunks * heads * p.nsplit, joins = (heads * R * (HD / 4) + 255) / 256;
-  if (blocks > 0x7FFFFFFF || joins > 0x7FFFFFFF) return hipErrorInvalidValue;
+  const long long blocks = p.chunks * heads * p.nsplit, joins = (heads * R * (HD / 4) + 63) / 64;
+  if (blocks > 0x7FFFFFFF || joins > 0x7FFFFFFF || heads * ((a.c.cap + 63) / 64) > 0x7FFFFFFF) return hipErrorInvalidValue;
   if constexpr (!F32) {
     if (p.tile) hipLaunchKernelGGL((cache_attn_tile_kernel<HD>), dim3((unsigned)blocks), dim3(512), 0, s, a, part, p.chunks);
   }
   if (!p.tile)
     hipLaunchKernelGGL((cache_attn_kernel<HD, F32>), dim3((unsigned)blocks), dim3(NW * 64), 0, s, a, part, p.chunks);
-  if (p.nsplit > 1) hipLaunchKernelGGL(cache_join_kernel<F32>, dim3((unsigned)joins), dim3(256), 0, s, a, part);
+  if (p.nsplit > 1) hipLaunchKernelGGL(cache_join_kernel<F32>, dim3((unsigned)joins), dim3(64), 0, s, a, part);
   if (a.track)
-    hipLaunchKernelGGL((cache_weight_kernel<HD, F32>), dim3((a.c.cap + 32 * NW - 1) / (32 * NW), a.c.nkv, a.batch),
-                       dim3(NW * 64), 0, s, a, part.lse);
+    hipLaunchKernelGGL((cache_weight_kernel<HD, F32>), dim3((unsigned)(heads * ((a.c.cap + 63) / 64))), dim3(NW * 64), 0, s, a,
+                       part.lse);
   return hipGetLastError();
 }
 
