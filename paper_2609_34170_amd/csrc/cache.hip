@@ -56,34 +56,29 @@ RAVEL_DEV uint32_t block_max(uint32_t v, uint32_t* lds) {  // over the block; ev
   return v;
 }
 
-// 16 elements from p as floats
+// 16 elements, as they lie in memory
 template <typename T>
-RAVEL_DEV void load16(const T* p, float (&x)[16]) {
-  if constexpr (sizeof(T) == 4) {
+struct Unit {
+  u32x4_t w[sizeof(T)];  // 2 bytes an element: 2 x 16 bytes; 4: 4 x 16
+  RAVEL_DEV void load(const T* p) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const f32x4_t v = *(const f32x4_t*)(p + 4 * i);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) x[4 * i + j] = v[j];
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const u32x4_t v = *(const u32x4_t*)(p + 8 * i);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        x[8 * i + 2 * j] = __uint_as_float(v[j] << 16);
-        x[8 * i + 2 * j + 1] = __uint_as_float(v[j] & 0xFFFF0000u);
-      }
-    }
+    for (int i = 0; i < (int)sizeof(T); ++i) w[i] = *(const u32x4_t*)(p + i * (16 / sizeof(T)));
   }
-}
+  RAVEL_DEV float operator[](int i) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[i / 4][i % 4]);
+    const uint32_t x = w[i / 8][i % 8 / 2];
+    return __uint_as_float(i % 2 ? x & 0xFFFF0000u : x << 16);
+  }
+};
 
 // ---------------------------------------------------------------------------
 // Append: one block per (scale block that the row's tokens touch, kv head, K or V of a batch row).
+// The tokens are read once: their NU units a thread (of TH threads) wait in registers for the
+// scale that all of them together give (reading them again from the cache: 9.0 us for a context
+// of 18 x 816 tokens of 256 dims, 135 for 96 x 1250 tokens of 4 x 128 in 32 bits).
 // ---------------------------------------------------------------------------
-template <typename T>
-__global__ __launch_bounds__(256) void cache_append_kernel(CacheAppendArgs a) {
+template <typename T, int NU, int TH>
+__global__ __launch_bounds__(TH) void cache_append_kernel(CacheAppendArgs a) {
   __shared__ uint32_t red[4];
   const CacheView& c = a.c;
   const int h = blockIdx.y, b = blockIdx.z >> 1;
@@ -99,46 +94,52 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheAppendArgs a) {
   const int lo = max(pos, b0), hi = min(pos + cnt, b0 + (1 << c.shift));
   if (lo >= hi) return;
 
-  const int upr = c.hd >> 4;  // units of 16 elements per row
-  const int units = (hi - lo) * upr;
+  const int us = c.hd == 32 ? 1 : c.hd == 64 ? 2 : c.hd == 128 ? 3 : 4;  // log2 of the units of a row
+  const int units = (hi - lo) << us;
   const T* src = (const T*)(is_v ? a.v : a.k) + (long long)b * a.sb + h * a.sh + (long long)(lo - pos) * a.st;
-  uint32_t amax = 0;
-  for (int i = threadIdx.x; i < units; i += blockDim.x) {
-    float x[16];
-    load16(src + (long long)(i / upr) * a.st + (i % upr) * 16, x);
+  Unit<T> x[NU];
 #pragma unroll
-    for (int j = 0; j < 16; ++j) amax = max(amax, finite_abs(x[j]));
+  for (int k = 0; k < NU; ++k) {
+    const int i = min((int)threadIdx.x + k * TH, units - 1);  // (past the end: the last one again)
+    x[k].load(src + (long long)(i >> us) * a.st + (i & ((1 << us) - 1)) * 16);
   }
+  uint32_t amax = 0;
+#pragma unroll
+  for (int k = 0; k < NU; ++k)
+#pragma unroll
+    for (int j = 0; j < 16; ++j) amax = max(amax, finite_abs(x[k][j]));
   float s = scale_for(block_max(amax, red));
   const long long head = (long long)id * c.nkv + h;
   float* sc = (is_v ? c.vs : c.ks) + head * c.nblk + blk;
   uint8_t* dst = (is_v ? c.v : c.k) + (head * c.cap + b0) * c.hd;
-  const float s0 = *sc;
   if (lo > b0) {  // older tokens share the block
+    const float s0 = *sc;
     if (s > s0) {
       const float r = s0 * reciprocal(s);
-      for (int i = threadIdx.x; i < (lo - b0) * upr; i += blockDim.x) {
+      for (int i = threadIdx.x; i < (lo - b0) << us; i += TH) {
         u32x4_t* p = (u32x4_t*)(dst + (size_t)i * 16);
         *p = rescale16(*p, r);
       }
     } else {
       s = s0;
     }
+    __syncthreads();  // every thread has read the old scale
   }
   const float inv = reciprocal(s);
   dst += (size_t)(lo - b0) * c.hd;
-  for (int i = threadIdx.x; i < units; i += blockDim.x) {
-    float x[16];
-    load16(src + (long long)(i / upr) * a.st + (i % upr) * 16, x);
+#pragma unroll
+  for (int k = 0; k < NU; ++k) {
+    const int i = threadIdx.x + k * TH;
+    if (i >= units) break;
     u32x4_t w;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) w[j] = to_codes(x[4 * j] * inv, x[4 * j + 1] * inv, x[4 * j + 2] * inv, x[4 * j + 3] * inv);
+    for (int j = 0; j < 4; ++j)
+      w[j] = to_codes(x[k][4 * j] * inv, x[k][4 * j + 1] * inv, x[k][4 * j + 2] * inv, x[k][4 * j + 3] * inv);
     *(u32x4_t*)(dst + (size_t)i * 16) = w;
   }
-  __syncthreads();  // every thread has read the old scale
   if (threadIdx.x == 0) *sc = s;
   if (c.weight && !is_v)
-    for (int t = lo + threadIdx.x; t < hi; t += blockDim.x) c.weight[head * c.cap + t] = 0.f;
+    for (int t = lo + threadIdx.x; t < hi; t += TH) c.weight[head * c.cap + t] = 0.f;
 }
 
 __global__ __launch_bounds__(64) void cache_append_len_kernel(CacheAppendArgs a) {
@@ -151,16 +152,26 @@ __global__ __launch_bounds__(64) void cache_append_len_kernel(CacheAppendArgs a)
 
 }  // namespace
 
-hipError_t launch_cache_append(const CacheAppendArgs& a, hipStream_t s) {
-  if (a.batch == 0) return hipSuccess;
+template <typename T>
+static void append(const CacheAppendArgs& a, hipStream_t s) {
   const int block = 1 << a.c.shift;
   const int wb = std::max(1, std::min(a.c.nblk, (a.n + block - 2) / block + 1));
   const int units = std::min(a.n, block) * (a.c.hd / 16);
-  const dim3 grid(wb, a.c.nkv, a.batch * 2), threads(units <= 64 ? 64 : 256);
+  const dim3 grid(wb, a.c.nkv, a.batch * 2);
+  const auto kernel = units <= 64    ? cache_append_kernel<T, 1, 64>
+                      : units <= 256 ? cache_append_kernel<T, 1, 256>
+                      : units <= 512 ? cache_append_kernel<T, 2, 256>
+                      : units <= 1024 ? cache_append_kernel<T, 4, 256>
+                                      : cache_append_kernel<T, 8, 256>;
+  hipLaunchKernelGGL(kernel, grid, dim3(units <= 64 ? 64 : 256), 0, s, a);
+}
+
+hipError_t launch_cache_append(const CacheAppendArgs& a, hipStream_t s) {
+  if (a.batch == 0) return hipSuccess;
   if (a.f32)
-    hipLaunchKernelGGL(cache_append_kernel<float>, grid, threads, 0, s, a);
+    append<float>(a, s);
   else
-    hipLaunchKernelGGL(cache_append_kernel<bf16_t>, grid, threads, 0, s, a);
+    append<bf16_t>(a, s);
   if (!a.pos) hipLaunchKernelGGL(cache_append_len_kernel, dim3(a.batch), dim3(64), 0, s, a);
   return hipGetLastError();
 }
@@ -186,7 +197,7 @@ RAVEL_DEV uint32_t weight_key(float w) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-constexpr int kSelThreads = 1024;
+constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;
 
 RAVEL_DEV int block_scan(int v, int* lds, int& total) {  // exclusive; every thread calls
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -201,16 +212,25 @@ RAVEL_DEV int block_scan(int v, int* lds, int& total) {  // exclusive; every thr
   __syncthreads();
   int base = 0;
   total = 0;
-  for (int i = 0; i < kSelThreads / 64; ++i) {
+#pragma unroll
+  for (int i = 0; i < kSelWaves; ++i) {
     if (i < wave) base += lds[i];
     total += lds[i];
   }
   return base + x - v;
 }
 
+// The keep-th largest weight is found 11, 11 and 10 bits of its key at a time, by a histogram of
+// the keys that share the bits found so far; then the kept tokens are the keys above it and
+// the first of those equal to it.  A thread holds KPT consecutive tokens' keys in registers (where
+// that is not all of them, 1024 KPT at a time), so that ranks in token order take two scans over
+// the threads' counts.  One workgroup for all of a (sequence, head): its vector instructions bind
+// (16384 tokens: 47 us with a scan for every 1024 of them and a pass over memory for every digit).
+template <int KPT>
 __global__ __launch_bounds__(kSelThreads) void cache_select_kernel(CacheEvictArgs a, EvictInfo* info, int* holes) {
-  __shared__ unsigned hist[256];
-  __shared__ int scan[kSelThreads / 64];
+  constexpr int CHUNK = kSelThreads * KPT;
+  __shared__ unsigned hist[2048];
+  __shared__ int scan[kSelWaves];
   __shared__ unsigned digit_s, above_s;
   const CacheView& c = a.src;
   const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
@@ -240,69 +260,96 @@ __global__ __launch_bounds__(kSelThreads) void cache_select_kernel(CacheEvictArg
     return;
   }
   const float* w = c.weight + head * c.cap;
-  const auto key_of = [&](int i) { return i < a.first ? 0xFFFFFFFFu : weight_key(w[i]); };
+  uint32_t k[KPT];
+  const auto load = [&](int base) {  // 0 past the end, as NaN has
+    const int i0 = base + tid * KPT;
+    float x[KPT];
+    if (i0 + KPT <= n) {
+      typedef float __attribute__((ext_vector_type(KPT), aligned(4))) vec_t;
+      const vec_t v = *(const vec_t*)(w + i0);
+#pragma unroll
+      for (int j = 0; j < KPT; ++j) x[j] = v[j];
+    } else {
+#pragma unroll
+      for (int j = 0; j < KPT; ++j) x[j] = i0 + j < n ? w[i0 + j] : __uint_as_float(0x7FC00000u);
+    }
+#pragma unroll
+    for (int j = 0; j < KPT; ++j) k[j] = i0 + j < a.first ? 0xFFFFFFFFu : weight_key(x[j]);
+  };
+  load(0);
+  const bool one = n <= CHUNK;
 
-  // the keep-th largest key, 8 bits at a time; `want`: its rank among the keys of the same prefix
+  // `want`: the rank looked for among the keys that share the bits of prefix
   uint32_t prefix = 0;
   unsigned want = keep;
-  for (int sh = 24; sh >= 0; sh -= 8) {
-    for (int i = tid; i < 256; i += kSelThreads) hist[i] = 0;
+#pragma unroll
+  for (int round = 0; round < 3; ++round) {
+    const int sh = round == 0 ? 21 : round == 1 ? 10 : 0, bits = round == 2 ? 10 : 11;
+    hist[tid] = 0;
+    hist[tid + 1024] = 0;
     __syncthreads();
-    for (int i = tid; i < n; i += kSelThreads) {
-      const uint32_t k = key_of(i);
-      if (sh == 24 || (k >> (sh + 8)) == (prefix >> (sh + 8))) atomicAdd(&hist[(k >> sh) & 255], 1u);
+    for (int base = 0; base < n; base += CHUNK) {
+      if (!one) load(base);
+      const int mine = n - base - tid * KPT;
+#pragma unroll
+      for (int j = 0; j < KPT; ++j)
+        if (j < mine && (round == 0 || k[j] >> (sh + bits) == prefix >> (sh + bits)))
+          atomicAdd(&hist[(k[j] >> sh) & ((1u << bits) - 1)], 1u);
     }
     __syncthreads();
-    if (tid < 64) {  // 4 digits a lane, from the largest down
-      unsigned v[4], sum = 0;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        v[j] = hist[255 - (tid * 4 + j)];
-        sum += v[j];
-      }
-      unsigned inc = sum;
-#pragma unroll
-      for (int off = 1; off < 64; off <<= 1) {
-        const unsigned y = __shfl_up(inc, off, 64);
-        if (tid >= off) inc += y;
-      }
-      unsigned before = inc - sum;
-      if (before < want && want <= inc) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if (before < want && want <= before + v[j]) {
-            digit_s = 255 - (tid * 4 + j);
-            above_s = before;
-          }
-          before += v[j];
-        }
-      }
+    // two digits a thread, from the largest down
+    const unsigned v0 = hist[2047 - 2 * tid], v1 = hist[2046 - 2 * tid];
+    int total;
+    const unsigned before = block_scan((int)(v0 + v1), scan, total);
+    if (before < want && want <= before + v0) {
+      digit_s = 2047 - 2 * tid;
+      above_s = before;
+    } else if (before + v0 < want && want <= before + v0 + v1) {
+      digit_s = 2046 - 2 * tid;
+      above_s = before + v0;
     }
     __syncthreads();
     prefix |= digit_s << sh;
     want -= above_s;
-    __syncthreads();
   }
-  // kept: keys above the threshold, and the first `want` equal to it
+
   int* hole = holes + out;
   int eq_base = 0, hole_base = 0, arr_base = 0;
-  for (int t0 = 0; t0 < n; t0 += kSelThreads) {
-    const int i = t0 + tid;
-    const uint32_t k = i < n ? key_of(i) : 0;
-    const int eq = i < n && k == prefix;
+  for (int base = 0; base < n; base += CHUNK) {
+    if (!one) load(base);
+    const int i0 = base + tid * KPT;
+    // a thread's tokens as bits: there, equal to the threshold, below keep
+    const unsigned all = (1u << min(max(n - i0, 0), KPT)) - 1, low = (1u << min(max(keep - i0, 0), KPT)) - 1;
+    unsigned over = 0, eq = 0;
+#pragma unroll
+    for (int j = 0; j < KPT; ++j) {
+      over |= k[j] > prefix ? 1u << j : 0u;
+      eq |= k[j] == prefix ? 1u << j : 0u;
+    }
+    eq &= all;
     int total;
-    const int eq_rank = eq_base + block_scan(eq, scan, total);
+    // the first `want` of the equal ones, in token order, stay
+    int left = (int)want - eq_base - block_scan(__popc(eq), scan, total);
     eq_base += total;
-    const bool keep_it = i < n && (k > prefix || (eq && eq_rank < (int)want));
-    const int is_hole = i < keep && !keep_it, is_arr = i >= keep && keep_it;
-    const int rank = block_scan(is_hole | is_arr << 16, scan, total);  // both counts in one scan (1024 a round)
-    if (i < keep && keep_it) kept[i] = i;
-    if (is_hole) hole[hole_base + (rank & 0xFFFF)] = i;
-    const int ht = total & 0xFFFF;
-    __syncthreads();  // a round may hold holes and arrivals: the holes are written first
-    if (is_arr) kept[hole[arr_base + (rank >> 16)]] = i;
-    hole_base += ht;
-    arr_base += total >> 16;
+    unsigned stays = over & all;
+#pragma unroll
+    for (int j = 0; j < KPT; ++j)
+      if (eq >> j & 1 && left-- > 0) stays |= 1u << j;
+    // ranks of the holes below keep and of the arrivals from keep on (at most 16384 of either)
+    const unsigned gone = all & low & ~stays, come = stays & ~low;
+    const int rank = block_scan(__popc(gone) | __popc(come) << 16, scan, total);
+    int hr = hole_base + (rank & 0xFFFF), ar = arr_base + (int)((unsigned)rank >> 16);
+#pragma unroll
+    for (int j = 0; j < KPT; ++j) {
+      if (stays & low & 1u << j) kept[i0 + j] = i0 + j;
+      if (gone >> j & 1) hole[hr++] = i0 + j;
+    }
+    __syncthreads();  // the holes are there
+#pragma unroll
+    for (int j = 0; j < KPT; ++j)
+      if (come >> j & 1) kept[hole[ar++]] = i0 + j;
+    hole_base += total & 0xFFFF;
+    arr_base += (int)((unsigned)total >> 16);
   }
 }
 
@@ -362,7 +409,9 @@ hipError_t launch_cache_evict(const CacheEvictArgs& a, hipStream_t s) {
   if (a.batch == 0) return hipSuccess;
   EvictInfo* info = (EvictInfo*)a.ws;
   int* holes = (int*)((char*)a.ws + evict_info_bytes(a.batch, a.src.nkv));
-  hipLaunchKernelGGL(cache_select_kernel, dim3(a.src.nkv, a.batch), dim3(kSelThreads), 0, s, a, info, holes);
+  const auto select = a.src.cap <= kSelThreads ? cache_select_kernel<1> : a.src.cap <= 4 * kSelThreads ? cache_select_kernel<4>
+                                                                                                       : cache_select_kernel<16>;
+  hipLaunchKernelGGL(select, dim3(a.src.nkv, a.batch), dim3(kSelThreads), 0, s, a, info, holes);
   const int block = 1 << a.src.shift, nb = (std::min(a.keep, a.src.cap) + block - 1) / block;
   hipLaunchKernelGGL(cache_move_kernel, dim3(nb, a.src.nkv, a.batch * 2), dim3(256), 0, s, a, info);
   return hipGetLastError();

@@ -841,11 +841,18 @@ size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 Plan plan_of(const CacheAttnArgs& a) {
   Plan p;
   const long long R = (long long)(a.nq / a.c.nkv) * a.rows, heads = (long long)a.batch * a.c.nkv;
-  p.tile = !a.f32 && R > 32;
+  // 128-row blocks once the work is worth their start (13 us at 256 dims, 7 at 128): rows in
+  // chunks of 16 times keys.  us, 16-row blocks / 128-row blocks: 400 rows of 256 dims over 866 keys,
+  // 8 sequences (1.7e5) 30 / 32, 16 (3.5e5) 34 / 34, 32 64 / 41; 400 rows of 128 dims over 2148
+  // keys, 4 heads (2.1e5) 17 / 21, 16 (8.6e5) 31 / 29, 64 97 / 46; 64 rows of 64 dims over 320 keys, 128
+  // heads (1.6e5) 7 / 14, 512 (6.6e5) 22 / 18.  Up to 32 rows they never win: 512 heads of
+  // 128 dims over 1024 keys, 32 rows 43 / 48, 48 rows 61 / 49.
+  const long long work = (R + 15) / 16 * heads * (a.c.cap + a.n_self);
+  p.tile = !a.f32 && R > 32 && work >= 300000;
   const int rows = p.tile ? 128 : 16, keys = !p.tile || a.c.hd < 256 ? 128 : 64;
   p.chunks = (int)((R + rows - 1) / rows);
   const long long blocks = p.chunks * heads, tiles = (a.c.cap + keys - 1) / keys + (a.n_self + keys - 1) / keys;
-  // one (tile) or two blocks a CU, at least one tile a wave in every key range
+  // key ranges: one (128 rows) or two blocks a CU, at least one tile a wave in every range
   p.nsplit = (int)std::max(1ll, std::min({(p.tile ? 256 : 512) / std::max(blocks, 1ll), tiles, 64ll}));
   if (p.tile) p.nsplit = std::max(p.nsplit, (int)(((long long)a.c.cap * a.c.hd >> 30) + 1));  // 32-bit offsets in a range
   p.o_off = 0;

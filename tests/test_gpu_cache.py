@@ -200,6 +200,12 @@ ATTEND = [
     (128, 4, 4, 16, 90, [90, 16, 17], 3, 40, "f32"),
     (64, 8, 8, 32, 257, [257, 0, 100], 16, 16, "f32"),
     (32, 4, 2, 64, 33, [33, 32, 1], 1, 0, "f32"),
+    # enough work for the blocks of 128 rows: every head dim, block, ragged stages, a last block of few rows
+    (256, 8, 1, 64, 2500, [2500, 0, 1999], 50, 50, "bf16"),
+    (256, 8, 1, 16, 3001, [2977, 65, 64], 41, 0, "bf16"),
+    (128, 16, 4, 128, 1100, [1100, 129, 1000], 100, 130, "bf16"),
+    (64, 12, 3, 16, 900, [900, 899, 5], 100, 7, "bf16"),
+    (32, 4, 4, 32, 2000, [2000, 1, 1025], 128, 8, "bf16"),
 ]
 
 
@@ -218,7 +224,7 @@ def test_attention(hd, nq, nkv, block, cap, lens, rows, n_self, dtype):
     _same(g, c)
 
 
-@pytest.mark.parametrize("hd,nq,nkv,block,cap,lens,rows,n_self,dtype", ATTEND[:1] + ATTEND[2:9:2] + ATTEND[9:])
+@pytest.mark.parametrize("hd,nq,nkv,block,cap,lens,rows,n_self,dtype", ATTEND[:1] + ATTEND[2:9:2] + ATTEND[9:13] + ATTEND[13:16])
 def test_accumulated_weights(hd, nq, nkv, block, cap, lens, rows, n_self, dtype):
     r = np.random.default_rng(hd + cap + rows + 1)
     c = _draw_cache(r, 4, nkv, cap, hd, block, lens + [cap])
@@ -278,6 +284,7 @@ EVICT = [
     (32, 2, 65, 32, [65, 64, 2, 1], 1, 1),
     (64, 1, 40, 16, [40, 39, 38, 1], 39, 5),
     (32, 1, 20000, 16, [20000, 19999, 17000, 4], 16500, 0),
+    (32, 1, 40000, 32, [40000, 33000, 16385, 16384], 130, 7),
 ]
 
 
