@@ -12,6 +12,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import os
+import struct
 from typing import Dict, List, Optional, Tuple
 
 import numpy as np
@@ -64,6 +65,10 @@ class RavelCacheQuery(ctypes.Structure):
         ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_int64)]
 
 
+# RavelCacheQuery's fields in one call (filling the structure field by field costs more than a launch)
+_pack_query = struct.Struct("@6ifi5P9qPq").pack
+
+
 SYMBOLS = [
     "ravel_create", "ravel_destroy", "ravel_model_weight_bytes", "ravel_buffer_create",
     "ravel_buffer_destroy", "ravel_buffer_set_option", "ravel_context_acquire", "ravel_set_context",
@@ -112,9 +117,8 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "ravel_profile_step": ([vp, vp, vp, vp, ctypes.POINTER(KernelRecord), ctypes.POINTER(i32)], i32),
         "ravel_last_error": ([], ctypes.c_char_p),
         "ravel_cache_append": ([ctypes.POINTER(RavelCache), i32, vp, vp, vp, i32, i32, vp, vp, i64, i64, i64, vp], i32),
-        "ravel_cache_attention_workspace": ([ctypes.POINTER(RavelCache), ctypes.POINTER(RavelCacheQuery),
-                                             ctypes.POINTER(i64)], i32),
-        "ravel_cache_attention": ([ctypes.POINTER(RavelCache), ctypes.POINTER(RavelCacheQuery), vp], i32),
+        "ravel_cache_attention_workspace": ([ctypes.POINTER(RavelCache), vp, ctypes.POINTER(i64)], i32),
+        "ravel_cache_attention": ([ctypes.POINTER(RavelCache), vp, vp], i32),
         "ravel_cache_evict_workspace": ([ctypes.POINTER(RavelCache), i32, i32, ctypes.POINTER(i64)], i32),
         "ravel_cache_evict": ([ctypes.POINTER(RavelCache), i32, vp, i32, i32, ctypes.POINTER(RavelCache), vp, vp, vp,
                                i64, vp], i32),
@@ -375,7 +379,11 @@ class Cache:
             if tuple(t.shape) != tuple(shape) or t.dtype not in types or t.device != k.device or not t.is_contiguous():
                 raise ValueError(f"{name} must be a contiguous {types[0]} tensor {tuple(shape)} on {k.device}")
         self.k, self.v, self.k_scale, self.v_scale, self.length, self.weight = k, v, k_scale, v_scale, length, weight
-        self.block, self.device = block, k.device
+        self.block, self.device, self._device_index, self._torch = block, k.device, k.get_device(), torch
+        self._lib, self._workspace = load_library(), {}
+        self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda device: torch.cuda.current_stream(device).cuda_stream)
+        self._codes_shape = (n_kv, hd)
         self._c = RavelCache(n_seq, n_kv, hd, cap, block, 0, k.data_ptr(), v.data_ptr(), k_scale.data_ptr(),
                              v_scale.data_ptr(), length.data_ptr(), None if weight is None else weight.data_ptr())
         self._ref = ctypes.byref(self._c)
@@ -395,94 +403,99 @@ class Cache:
 
     def _on(self, stream, *tensors):
         """(guard that makes this cache's device and the call's stream current, or None; stream handle)."""
-        import torch
-
+        device = self._device_index
         for t in tensors:
-            if t is not None and t.device != self.device:
+            if t is not None and t.get_device() != device:
                 raise ValueError(f"every tensor of the call must be on {self.device}")
+        cuda = self._torch.cuda
         if stream is None:
-            if self.device.index in (None, torch.cuda.current_device()):
-                return None, torch.cuda.current_stream().cuda_stream
-            return torch.cuda.device(self.device), torch.cuda.current_stream(self.device).cuda_stream
+            if device == cuda.current_device():
+                return None, self._raw_stream(device)
+            return cuda.device(self.device), self._raw_stream(device)
         if isinstance(stream, int):
-            stream = torch.cuda.ExternalStream(stream, device=self.device)
-        return torch.cuda.stream(stream), stream.cuda_stream
+            stream = cuda.ExternalStream(stream, device=self.device)
+        return cuda.stream(stream), stream.cuda_stream
 
     def _index(self, name, t, batch):
-        import torch
-
         if t is None:
             return None
-        if t.dtype is not torch.int32 or t.dim() != 1 or t.shape[0] != batch or not t.is_contiguous():
+        if t.dtype is not self._torch.int32 or t.dim() != 1 or t.shape[0] != batch or not t.is_contiguous():
             raise ValueError(f"{name} must be a contiguous int32 tensor [{batch}]")
         return t.data_ptr()
 
+    def _dtype(self, t) -> int:
+        if t.dtype is self._torch.bfloat16:
+            return BF16
+        if t.dtype is self._torch.float32:
+            return F32
+        raise ValueError(f"bf16 or float32 expected, got {t.dtype}")
+
     def append(self, k, v, pos=None, count=None, seq=None, stream=None):
         """Store k, v ``[batch, n, n_kv_heads, head_dim]`` (bf16 or float32) from ``pos`` (default: the lengths) on."""
-        c = self._c
-        if k.dim() != 4 or k.shape != v.shape or k.shape[2] != c.n_kv_heads or k.shape[3] != c.head_dim or \
-                v.dtype is not k.dtype:
-            raise ValueError(f"k and v must be [batch, n, {c.n_kv_heads}, {c.head_dim}] of one dtype")
-        if k.stride() != v.stride() or (k.stride(3) != 1 and k.numel()):
+        shape, strides = k.shape, k.stride()
+        if len(shape) != 4 or shape[2:] != self._codes_shape or v.shape != shape or v.dtype is not k.dtype:
+            raise ValueError("k and v must be [batch, n, %d, %d] of one dtype" % self._codes_shape)
+        if v.stride() != strides or (strides[3] != 1 and k.numel()):
             raise ValueError("k and v must have the same strides, head_dim contiguous")
         guard, s = self._on(stream, k, v, pos, count, seq)
-        B, n, sb, st, sh = k.shape[0], k.shape[1], *k.stride()[:3]
+        B = shape[0]
         args = (self._ref, B, self._index("seq", seq, B), self._index("pos", pos, B), self._index("count", count, B),
-                n, _cache_dtype(k), k.data_ptr(), v.data_ptr(), sb, st, sh, s)
+                shape[1], self._dtype(k), k.data_ptr(), v.data_ptr(), strides[0], strides[1], strides[2], s)
         if guard is None:
-            _check(load_library().ravel_cache_append(*args))
+            _check(self._lib.ravel_cache_append(*args))
         else:
             with guard:
-                _check(load_library().ravel_cache_append(*args))
+                _check(self._lib.ravel_cache_append(*args))
 
     def attention(self, q, out, self_k=None, self_v=None, seq=None, scale=None, track=False, stream=None):
         """out = attention of q ``[batch, rows, n_q_heads, head_dim]`` over the sequences' tokens and the call's own
         ``self_k``, ``self_v`` ``[batch, n_self, n_kv_heads, head_dim]``; ``track``: add to the accumulated weights."""
-        c = self._c
-        if q.dim() != 4 or q.shape[3] != c.head_dim or out.shape != q.shape or out.dtype is not q.dtype:
-            raise ValueError(f"q and out must be [batch, rows, n_q_heads, {c.head_dim}] of one dtype")
-        B, rows, nq, hd = q.shape
-        qs, os = q.stride(), out.stride()
-        if (qs[3] != 1 or os[3] != 1) and q.numel():
+        shape, qs, os_, dtype = q.shape, q.stride(), out.stride(), q.dtype
+        nkv, hd = self._codes_shape
+        if len(shape) != 4 or shape[3] != hd or out.shape != shape or out.dtype is not dtype:
+            raise ValueError(f"q and out must be [batch, rows, n_q_heads, {hd}] of one dtype")
+        if (qs[3] != 1 or os_[3] != 1) and q.numel():
             raise ValueError("head_dim must be contiguous")
-        x = RavelCacheQuery(_cache_dtype(q), B, nq, rows, 0, 1 if track else 0, hd ** -0.5 if scale is None else scale, 0,
-                            self._index("seq", seq, B), q.data_ptr(), None, None, out.data_ptr(), qs[:3], (0, 0, 0), os[:3])
-        if (self_k is None) != (self_v is None):
-            raise ValueError("self_k and self_v must both be given or both None")
-        if self_k is not None:
-            if self_k.dim() != 4 or self_k.shape != self_v.shape or self_k.shape[0] != B or \
-                    self_k.shape[2] != c.n_kv_heads or self_k.shape[3] != hd or \
-                    self_k.dtype is not q.dtype or self_v.dtype is not q.dtype:
-                raise ValueError(f"self_k and self_v must be [{B}, n_self, {c.n_kv_heads}, {hd}] of the queries' dtype")
-            ss = self_k.stride()
+        B, rows, nq, _ = shape
+        n_self, kp, vp, ss = 0, 0, 0, (0, 0, 0)
+        if self_k is not None and self_v is not None:
+            n_self, ss = self_k.shape[1], self_k.stride()
+            if self_k.shape != (B, n_self, nkv, hd) or self_v.shape != self_k.shape or self_k.dtype is not dtype or \
+                    self_v.dtype is not dtype:
+                raise ValueError(f"self_k and self_v must be [{B}, n_self, {nkv}, {hd}] of the queries' dtype")
             if self_v.stride() != ss or (ss[3] != 1 and self_k.numel()):
                 raise ValueError("self_k and self_v must have the same strides, head_dim contiguous")
-            x.n_self, x.self_k, x.self_v, x.self_stride = self_k.shape[1], self_k.data_ptr(), self_v.data_ptr(), ss[:3]
+            kp, vp = self_k.data_ptr(), self_v.data_ptr()
+        elif self_k is not self_v:
+            raise ValueError("self_k and self_v must both be given or both None")
         guard, s = self._on(stream, q, out, self_k, self_v, seq)
+        sizes = (self._dtype(q), B, nq, rows, n_self, 1 if track else 0)
+        fields = (hd ** -0.5 if scale is None else scale, 0, self._index("seq", seq, B) or 0, q.data_ptr(), kp, vp,
+                  out.data_ptr(), *qs[:3], *ss[:3], *os_[:3])
         if guard is None:
-            self._attention(x, s)
+            self._attention(sizes, fields, s)
         else:
             with guard:
-                self._attention(x, s)
+                self._attention(sizes, fields, s)
 
-    def _attention(self, x, s):
-        import torch
-
-        lib, n = load_library(), ctypes.c_int64(0)
-        _check(lib.ravel_cache_attention_workspace(self._ref, ctypes.byref(x), ctypes.byref(n)))
-        if n.value:
+    def _attention(self, sizes, fields, s):
+        n = self._workspace.get(sizes)  # bytes that calls of these sizes need
+        if n is None:
+            need = ctypes.c_int64(0)
+            _check(self._lib.ravel_cache_attention_workspace(self._ref, _pack_query(*sizes, *fields, 0, 0), ctypes.byref(need)))
+            n = self._workspace[sizes] = need.value
+        ws = 0
+        if n:
             # of this call alone: torch keeps it from later calls on the stream until this one has run
-            ws = torch.empty(n.value, dtype=torch.uint8, device=self.device)
-            x.workspace, x.workspace_bytes = ws.data_ptr(), n.value
-        _check(lib.ravel_cache_attention(self._ref, ctypes.byref(x), s))
+            memory = self._torch.empty(n, dtype=self._torch.uint8, device=self.device)
+            ws = memory.data_ptr()
+        _check(self._lib.ravel_cache_attention(self._ref, _pack_query(*sizes, *fields, ws, n), s))
 
     def evict(self, keep: int, first: int = 0, seq=None, into: Optional["Cache"] = None, into_seq=None, kept=None,
               stream=None):
         """Keep the ``keep`` tokens of the largest accumulated weight per row and KV head, in place or in another cache;
         returns the index each place's token had, int32 ``[batch, n_kv_heads, keep]`` (``kept``, or a new tensor)."""
-        import torch
-
-        c = self._c
+        torch, c = self._torch, self._c
         B = seq.shape[0] if seq is not None else c.n_seq
         if into is not None and into.device != self.device:
             raise ValueError(f"every tensor of the call must be on {self.device}")
@@ -492,20 +505,10 @@ class Cache:
                 kept = torch.empty((B, c.n_kv_heads, max(keep, 0)), dtype=torch.int32, device=self.device)
             elif tuple(kept.shape) != (B, c.n_kv_heads, keep) or kept.dtype is not torch.int32 or not kept.is_contiguous():
                 raise ValueError(f"kept must be a contiguous int32 tensor [{B}, {c.n_kv_heads}, {keep}]")
-            lib, n = load_library(), ctypes.c_int64(0)
+            lib, n = self._lib, ctypes.c_int64(0)
             _check(lib.ravel_cache_evict_workspace(self._ref, B, keep, ctypes.byref(n)))
             ws = torch.empty(n.value, dtype=torch.uint8, device=self.device)
             _check(lib.ravel_cache_evict(self._ref, B, self._index("seq", seq, B), keep, first,
                                          None if into is None else into._ref, self._index("into_seq", into_seq, B),
                                          kept.data_ptr(), ws.data_ptr(), n.value, s))
         return kept
-
-
-def _cache_dtype(t) -> int:
-    import torch
-
-    if t.dtype is torch.bfloat16:
-        return BF16
-    if t.dtype is torch.float32:
-        return F32
-    raise ValueError(f"bf16 or float32 expected, got {t.dtype}")
