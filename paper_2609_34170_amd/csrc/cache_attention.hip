@@ -745,76 +745,79 @@ __global__ __launch_bounds__(64) void cache_join_kernel(CacheAttnArgs a, Part pa
     *(u32x2_t*)((bf16_t*)a.out + at) = u32x2_t{pack_bf16x2(num[0] * inv, num[1] * inv), pack_bf16x2(num[2] * inv, num[3] * inv)};
 }
 
-// Accumulated weights: a block owns 64 keys of a (sequence, kv head), forms their scores with
-// every row once more, 32 rows at a time dealt out to its waves, and adds 2^(score - lse).  Rows
-// are the first operand's here: a lane owns a key of each of two tiles and adds over its
-// registers.  Batch rows that name one sequence are added in row order by the first of them, so
-// that the sums have one order.
+// Accumulated weights: rw waves own 64 keys of a (sequence, kv head), form their scores with
+// every row once more, 32 rows at a time in turn, and add 2^(score - lse).  Rows are the first
+// operand's here: a lane owns a key of each of two tiles and adds over its registers.
+// Batch rows that name one sequence are added in row order by the first of them, so that the
+// sums have one order.  One wave, or all four of the block where there would be too few (they
+// read the same keys: one row of each of 16 heads over 8000 keys 7.5 us with one, 28 with more;
+// 400 rows of 256 dims over 16 x 816 keys 17 us with four).
 template <int HD, bool F32>
-__global__ __launch_bounds__(NW * 64) void cache_weight_kernel(CacheAttnArgs a, const float* lse) {
+__global__ __launch_bounds__(NW * 64) void cache_weight_kernel(CacheAttnArgs a, const float* lse, int rw) {
   constexpr int KS = HD / 16, NP = F32 ? 3 : 1;
   __shared__ float sum_s[NW][64];
   const CacheView& c = a.c;
-  const int bid = xcd_block(), nkt = (c.cap + 63) / 64;
+  const int bid = xcd_block(), bk = 64 * NW / rw, nkt = (c.cap + bk - 1) / bk;  // keys of a block
   const int g = bid / nkt % c.nkv, b0 = bid / nkt / c.nkv;
   const int id = __builtin_amdgcn_readfirstlane(cache_seq(c, a.seq, b0));
   if (id < 0 || cache_seq_before(c, a.seq, b0, id)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, h = lane >> 5;
-  const int n = cache_len(c, id), key0 = bid % nkt * 64;
-  if (key0 >= n) return;
+  const int n = cache_len(c, id), key0 = bid % nkt * bk + wave / rw * 64, sub = wave % rw;
   const int G = a.nq / c.nkv, R = G * a.rows;
   const long long head = (long long)id * c.nkv + g;
-  bf16x8_t kf[2][KS];
-#pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    const int key = min(key0 + 32 * u + l32, n - 1);
-    const float sc = c.ks[head * c.nblk + (key >> c.shift)];
-    const uint8_t* p = c.k + (head * c.cap + key) * HD + h * 16;
-#pragma unroll
-    for (int j = 0; j < KS / 2; ++j) {
-      const u32x4_t w = *(const u32x4_t*)(p + j * 32);
-      kf[u][2 * j] = scaled8(w[0], w[1], sc);
-      kf[u][2 * j + 1] = scaled8(w[2], w[3], sc);
-    }
-  }
-  const float sl2 = a.scale * kLog2e;
   float acc[2] = {0.f, 0.f};
-  for (int b = b0; b < a.batch; ++b) {
-    if (b != b0 && cache_seq(c, a.seq, b) != id) continue;
-    const float* lr = lse + ((long long)b * c.nkv + g) * R;
-    for (int r0 = wave * 32; r0 < R; r0 += NW * 32) {
-      const int r = min(r0 + l32, R - 1);
-      const long long at = b * a.qb + r % a.rows * a.qr + (g * G + r / a.rows) * a.qh + h * 16;
-      // 32 bits: planes are made fragment by fragment; bf16: every fragment on its way at once
-      bf16x8_t q[F32 ? 1 : KS][NP];
-      if constexpr (!F32) {
+  if (key0 < n && sub * 32 < R) {
+    bf16x8_t kf[2][KS];
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) load8<false>(a.q, at + (ks >> 1) * 32 + (ks & 1) * 8, q[ks]);
+    for (int u = 0; u < 2; ++u) {
+      const int key = min(key0 + 32 * u + l32, n - 1);
+      const float sc = c.ks[head * c.nblk + (key >> c.shift)];
+      const uint8_t* p = c.k + (head * c.cap + key) * HD + h * 16;
+#pragma unroll
+      for (int j = 0; j < KS / 2; ++j) {
+        const u32x4_t w = *(const u32x4_t*)(p + j * 32);
+        kf[u][2 * j] = scaled8(w[0], w[1], sc);
+        kf[u][2 * j + 1] = scaled8(w[2], w[3], sc);
       }
-      float ls[16];
+    }
+    const float sl2 = a.scale * kLog2e;
+    for (int b = b0; b < a.batch; ++b) {
+      if (b != b0 && cache_seq(c, a.seq, b) != id) continue;
+      const float* lr = lse + ((long long)b * c.nkv + g) * R;
+      for (int r0 = sub * 32; r0 < R; r0 += rw * 32) {
+        const int r = min(r0 + l32, R - 1);
+        const long long at = b * a.qb + r % a.rows * a.qr + (g * G + r / a.rows) * a.qh + h * 16;
+        // 32 bits: planes are made fragment by fragment; bf16: every fragment on its way at once
+        bf16x8_t q[F32 ? 1 : KS][NP];
+        if constexpr (!F32) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int rr = r0 + 8 * (i >> 2) + 4 * h + (i & 3);
-        ls[i] = rr < R ? lr[min(rr, R - 1)] : INFINITY;
-      }
-      f32x16_t s[2];
+          for (int ks = 0; ks < KS; ++ks) load8<false>(a.q, at + (ks >> 1) * 32 + (ks & 1) * 8, q[ks]);
+        }
+        float ls[16];
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[u][i] = 0.f;
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        if constexpr (F32) load8<true>(a.q, at + (ks >> 1) * 32 + (ks & 1) * 8, q[0]);
+        for (int i = 0; i < 16; ++i) {
+          const int rr = r0 + 8 * (i >> 2) + 4 * h + (i & 3);
+          ls[i] = rr < R ? lr[min(rr, R - 1)] : INFINITY;
+        }
+        f32x16_t s[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
-          for (int p = NP - 1; p >= 0; --p) s[u] = mfma32(q[F32 ? 0 : ks][p], kf[u][ks], s[u]);
+          for (int i = 0; i < 16; ++i) s[u][i] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          if constexpr (F32) load8<true>(a.q, at + (ks >> 1) * 32 + (ks & 1) * 8, q[0]);
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int p = NP - 1; p >= 0; --p) s[u] = mfma32(q[F32 ? 0 : ks][p], kf[u][ks], s[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[u] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i], sl2, -ls[i]));
       }
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) acc[u] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i], sl2, -ls[i]));
     }
   }
 #pragma unroll
@@ -823,11 +826,11 @@ __global__ __launch_bounds__(NW * 64) void cache_weight_kernel(CacheAttnArgs a, 
     if (h == 0) sum_s[wave][u * 32 + l32] = acc[u];
   }
   __syncthreads();
-  if (tid < 64 && key0 + tid < n) {
-    float v = sum_s[0][tid];
-#pragma unroll
-    for (int w = 1; w < NW; ++w) v += sum_s[w][tid];
-    c.weight[head * c.cap + key0 + tid] += v;
+  const int key = key0 + lane;
+  if (sub == 0 && key < n) {
+    float v = sum_s[wave][lane];
+    for (int w = 1; w < rw; ++w) v += sum_s[wave + w][lane];
+    c.weight[head * c.cap + key] += v;
   }
 }
 
@@ -876,9 +879,12 @@ hipError_t launch_hd(const CacheAttnArgs& a, hipStream_t s) {
   if (!p.tile)
     hipLaunchKernelGGL((cache_attn_kernel<HD, F32>), dim3((unsigned)blocks), dim3(NW * 64), 0, s, a, part, p.chunks);
   if (p.nsplit > 1) hipLaunchKernelGGL(cache_join_kernel<F32>, dim3((unsigned)joins), dim3(64), 0, s, a, part);
-  if (a.track)
-    hipLaunchKernelGGL((cache_weight_kernel<HD, F32>), dim3((unsigned)(heads * ((a.c.cap + 63) / 64))), dim3(NW * 64), 0, s, a,
-                       part.lse);
+  if (a.track) {
+    // one wave where its rows are few, or its keys alone give every SIMD a wave
+    const int rw = R <= 32 || heads * ((a.c.cap + 63) / 64) >= 1024 ? 1 : NW, bk = 64 * NW / rw;
+    hipLaunchKernelGGL((cache_weight_kernel<HD, F32>), dim3((unsigned)(heads * ((a.c.cap + bk - 1) / bk))), dim3(NW * 64), 0, s, a,
+                       part.lse, rw);
+  }
   return hipGetLastError();
 }
 
