@@ -23,7 +23,10 @@ constexpr float kLog2e = 1.4426950408889634f;
 // The running maximum of a row moves when a tile raises it by more than this (log2 units):
 // between moves the probabilities stay below 2^8 and nothing is rescaled.
 constexpr float kLazy = 8.f;
-constexpr int NW = 4;  // waves of a block; they take every fourth tile and are joined at the end
+// Waves of a block of few rows: as many as its registers take (8 of 256 dims instead of 4 and
+// key ranges to match: 400 rows over 866 keys 20 -> 15 us for 2 sequences, 30 -> 17 for 8; 16 heads
+// of 64 dims over 256 keys 7.1 -> 4.8, one launch instead of two).
+constexpr int few_row_waves(int hd, bool f32) { return hd <= 64 ? 16 : hd == 256 && f32 ? 4 : 8; }
 
 RAVEL_DEV f32x4_t mfma_bf16(bf16x8_t a, bf16x8_t b, f32x4_t c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
@@ -152,7 +155,11 @@ RAVEL_DEV bf16x8_t byte8(const uint32_t (&w)[8], int b) {
   return __builtin_bit_cast(bf16x8_t, (u32x4_t{codes2(a, false), codes2(c, false), codes2(d, false), codes2(e, false)}));
 }
 
-template <int HD, bool F32>
+// Few rows: a block owns 16 rows of a (batch row, kv head) and a range of its keys; its waves
+// take the range's tiles of 32 in turn and are joined at the end.  Nothing but the joining goes
+// through LDS: a wave loads its own keys as the first product's operand lies, and values 8 keys x
+// HD / 16 dims a lane, transposed by byte permutes (whole rows either way).
+template <int HD, bool F32, int NW = few_row_waves(HD, F32)>
 __global__ __launch_bounds__(NW * 64) void cache_attn_kernel(CacheAttnArgs a, Part part, int chunks) {
   constexpr int KS = HD / 32, NT = HD / 16, NP = F32 ? 3 : 1;
   __shared__ __attribute__((aligned(16))) float so[NW][16][HD + 4];
@@ -752,12 +759,13 @@ __global__ __launch_bounds__(64) void cache_join_kernel(CacheAttnArgs a, Part pa
 // sums have one order.  One wave, or all four of the block where there would be too few (they
 // read the same keys: one row of each of 16 heads over 8000 keys 7.5 us with one, 28 with more;
 // 400 rows of 256 dims over 16 x 816 keys 17 us with four).
+constexpr int WW = 4;  // waves of a block of keys
 template <int HD, bool F32>
-__global__ __launch_bounds__(NW * 64) void cache_weight_kernel(CacheAttnArgs a, const float* lse, int rw) {
+__global__ __launch_bounds__(WW * 64) void cache_weight_kernel(CacheAttnArgs a, const float* lse, int rw) {
   constexpr int KS = HD / 16, NP = F32 ? 3 : 1;
-  __shared__ float sum_s[NW][64];
+  __shared__ float sum_s[WW][64];
   const CacheView& c = a.c;
-  const int bid = xcd_block(), bk = 64 * NW / rw, nkt = (c.cap + bk - 1) / bk;  // keys of a block
+  const int bid = xcd_block(), bk = 64 * WW / rw, nkt = (c.cap + bk - 1) / bk;  // keys of a block
   const int g = bid / nkt % c.nkv, b0 = bid / nkt / c.nkv;
   const int id = __builtin_amdgcn_readfirstlane(cache_seq(c, a.seq, b0));
   if (id < 0 || cache_seq_before(c, a.seq, b0, id)) return;
@@ -782,41 +790,46 @@ __global__ __launch_bounds__(NW * 64) void cache_weight_kernel(CacheAttnArgs a, 
       }
     }
     const float sl2 = a.scale * kLog2e;
-    for (int b = b0; b < a.batch; ++b) {
-      if (b != b0 && cache_seq(c, a.seq, b) != id) continue;
-      const float* lr = lse + ((long long)b * c.nkv + g) * R;
-      for (int r0 = sub * 32; r0 < R; r0 += rw * 32) {
-        const int r = min(r0 + l32, R - 1);
-        const long long at = b * a.qb + r % a.rows * a.qr + (g * G + r / a.rows) * a.qh + h * 16;
-        // 32 bits: planes are made fragment by fragment; bf16: every fragment on its way at once
-        bf16x8_t q[F32 ? 1 : KS][NP];
-        if constexpr (!F32) {
+    // the rows that name this sequence, found 64 at a time; only b0 where all rows differ
+    const int b1 = !a.seq.idx || a.seq.row ? b0 + 1 : a.batch;
+    for (int bw = b0; bw < b1; bw += 64) {
+      unsigned long long same = __ballot(bw + lane < b1 && cache_seq(c, a.seq, bw + lane) == id);
+      for (; same; same &= same - 1) {
+        const int b = bw + __builtin_ctzll(same);
+        const float* lr = lse + ((long long)b * c.nkv + g) * R;
+        for (int r0 = sub * 32; r0 < R; r0 += rw * 32) {
+          const int r = min(r0 + l32, R - 1);
+          const long long at = b * a.qb + r % a.rows * a.qr + (g * G + r / a.rows) * a.qh + h * 16;
+          // 32 bits: planes are made fragment by fragment; bf16: every fragment on its way at once
+          bf16x8_t q[F32 ? 1 : KS][NP];
+          if constexpr (!F32) {
 #pragma unroll
-          for (int ks = 0; ks < KS; ++ks) load8<false>(a.q, at + (ks >> 1) * 32 + (ks & 1) * 8, q[ks]);
-        }
-        float ls[16];
+            for (int ks = 0; ks < KS; ++ks) load8<false>(a.q, at + (ks >> 1) * 32 + (ks & 1) * 8, q[ks]);
+          }
+          float ls[16];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int rr = r0 + 8 * (i >> 2) + 4 * h + (i & 3);
-          ls[i] = rr < R ? lr[min(rr, R - 1)] : INFINITY;
-        }
-        f32x16_t s[2];
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) s[u][i] = 0.f;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          if constexpr (F32) load8<true>(a.q, at + (ks >> 1) * 32 + (ks & 1) * 8, q[0]);
+          for (int i = 0; i < 16; ++i) {
+            const int rr = r0 + 8 * (i >> 2) + 4 * h + (i & 3);
+            ls[i] = rr < R ? lr[min(rr, R - 1)] : INFINITY;
+          }
+          f32x16_t s[2];
 #pragma unroll
           for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int p = NP - 1; p >= 0; --p) s[u] = mfma32(q[F32 ? 0 : ks][p], kf[u][ks], s[u]);
+            for (int i = 0; i < 16; ++i) s[u][i] = 0.f;
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) {
+            if constexpr (F32) load8<true>(a.q, at + (ks >> 1) * 32 + (ks & 1) * 8, q[0]);
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+              for (int p = NP - 1; p >= 0; --p) s[u] = mfma32(q[F32 ? 0 : ks][p], kf[u][ks], s[u]);
+          }
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[u] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i], sl2, -ls[i]));
         }
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) acc[u] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i], sl2, -ls[i]));
       }
     }
   }
@@ -846,17 +859,25 @@ Plan plan_of(const CacheAttnArgs& a) {
   const long long R = (long long)(a.nq / a.c.nkv) * a.rows, heads = (long long)a.batch * a.c.nkv;
   // 128-row blocks once the work is worth their start (13 us at 256 dims, 7 at 128): rows in
   // chunks of 16 times keys.  us, 16-row blocks / 128-row blocks: 400 rows of 256 dims over 866 keys,
-  // 8 sequences (1.7e5) 30 / 32, 16 (3.5e5) 34 / 34, 32 64 / 41; 400 rows of 128 dims over 2148
-  // keys, 4 heads (2.1e5) 17 / 21, 16 (8.6e5) 31 / 29, 64 97 / 46; 64 rows of 64 dims over 320 keys, 128
-  // heads (1.6e5) 7 / 14, 512 (6.6e5) 22 / 18.  Up to 32 rows they never win: 512 heads of
-  // 128 dims over 1024 keys, 32 rows 43 / 48, 48 rows 61 / 49.
+  // 8 sequences (1.7e5) 17 / 31, 16 (3.5e5) 32 / 34, 24 (5.2e5) 46 / 40, 64 103 / 42; 400 rows of 128
+  // dims over 2148 keys, 8 heads (4.3e5) 17 / 24, 16 (8.6e5) 33 / 28; 64 rows of 64 dims over 320
+  // keys, 128 heads (1.6e5) 9 / 14, 512 (6.6e5) 31 / 17.  Up to 32 rows they never win: 512 heads of
+  // 128 dims over 1024 keys, 32 rows 46.9 / 47.5, 48 rows 68 / 48.
   const long long work = (R + 15) / 16 * heads * (a.c.cap + a.n_self);
-  p.tile = !a.f32 && R > 32 && work >= 300000;
-  const int rows = p.tile ? 128 : 16, keys = !p.tile || a.c.hd < 256 ? 128 : 64;
+  p.tile = !a.f32 && R > 32 && work >= 500000;
+  const int rows = p.tile ? 128 : 16;
   p.chunks = (int)((R + rows - 1) / rows);
-  const long long blocks = p.chunks * heads, tiles = (a.c.cap + keys - 1) / keys + (a.n_self + keys - 1) / keys;
-  // key ranges: one (128 rows) or two blocks a CU, at least one tile a wave in every range
-  p.nsplit = (int)std::max(1ll, std::min({(p.tile ? 256 : 512) / std::max(blocks, 1ll), tiles, 64ll}));
+  const long long blocks = p.chunks * heads;
+  // Key ranges up to one block a CU.  128 rows: a stage at least.  16 rows: a tile a wave, but no
+  // ranges where a block has two for each of its waves (16 heads of 128 dims over 512 keys 7.3
+  // us so, 9.2 with two ranges; over 1024 11.0 and 9.3).
+  const int w = few_row_waves(a.c.hd, a.f32), keys = !p.tile ? 32 * w : a.c.hd < 256 ? 128 : 64;
+  long long steps = (a.c.cap + keys - 1) / keys + (a.n_self + keys - 1) / keys;
+  if (!p.tile) {
+    const long long tiles = (a.c.cap + 31) / 32 + (a.n_self + 31) / 32;
+    steps = tiles <= 2 * w ? 1 : (tiles + w - 1) / w;
+  }
+  p.nsplit = (int)std::max(1ll, std::min({256 / std::max(blocks, 1ll), steps, 64ll}));
   if (p.tile) p.nsplit = std::max(p.nsplit, (int)(((long long)a.c.cap * a.c.hd >> 30) + 1));  // 32-bit offsets in a range
   p.o_off = 0;
   p.ml_off = p.nsplit > 1 ? up256((size_t)p.nsplit * heads * R * a.c.hd * 4) : 0;
@@ -877,12 +898,13 @@ hipError_t launch_hd(const CacheAttnArgs& a, hipStream_t s) {
     if (p.tile) hipLaunchKernelGGL((cache_attn_tile_kernel<HD>), dim3((unsigned)blocks), dim3(512), 0, s, a, part, p.chunks);
   }
   if (!p.tile)
-    hipLaunchKernelGGL((cache_attn_kernel<HD, F32>), dim3((unsigned)blocks), dim3(NW * 64), 0, s, a, part, p.chunks);
+    hipLaunchKernelGGL((cache_attn_kernel<HD, F32>), dim3((unsigned)blocks), dim3(few_row_waves(HD, F32) * 64), 0, s, a, part,
+                       p.chunks);
   if (p.nsplit > 1) hipLaunchKernelGGL(cache_join_kernel<F32>, dim3((unsigned)joins), dim3(64), 0, s, a, part);
   if (a.track) {
     // one wave where its rows are few, or its keys alone give every SIMD a wave
-    const int rw = R <= 32 || heads * ((a.c.cap + 63) / 64) >= 1024 ? 1 : NW, bk = 64 * NW / rw;
-    hipLaunchKernelGGL((cache_weight_kernel<HD, F32>), dim3((unsigned)(heads * ((a.c.cap + bk - 1) / bk))), dim3(NW * 64), 0, s, a,
+    const int rw = R <= 32 || heads * ((a.c.cap + 63) / 64) >= 1024 ? 1 : WW, bk = 64 * WW / rw;
+    hipLaunchKernelGGL((cache_weight_kernel<HD, F32>), dim3((unsigned)(heads * ((a.c.cap + bk - 1) / bk))), dim3(WW * 64), 0, s, a,
                        part.lse, rw);
   }
   return hipGetLastError();

@@ -200,12 +200,16 @@ ATTEND = [
     (128, 4, 4, 16, 90, [90, 16, 17], 3, 40, "f32"),
     (64, 8, 8, 32, 257, [257, 0, 100], 16, 16, "f32"),
     (32, 4, 2, 64, 33, [33, 32, 1], 1, 0, "f32"),
-    # enough work for the blocks of 128 rows: every head dim, block, ragged stages, a last block of few rows
+    # many blocks of 16 rows, then enough work for those of 128: every head dim, ragged stages, a last block of few rows
     (256, 8, 1, 64, 2500, [2500, 0, 1999], 50, 50, "bf16"),
     (256, 8, 1, 16, 3001, [2977, 65, 64], 41, 0, "bf16"),
     (128, 16, 4, 128, 1100, [1100, 129, 1000], 100, 130, "bf16"),
     (64, 12, 3, 16, 900, [900, 899, 5], 100, 7, "bf16"),
     (32, 4, 4, 32, 2000, [2000, 1, 1025], 128, 8, "bf16"),
+    (256, 8, 1, 64, 4100, [4100, 0, 1999], 50, 50, "bf16"),
+    (256, 8, 1, 16, 5001, [4977, 65, 64], 41, 0, "bf16"),
+    (64, 12, 3, 16, 1400, [1400, 1399, 5], 100, 7, "bf16"),
+    (32, 4, 4, 32, 3200, [3200, 1, 1025], 128, 8, "bf16"),
 ]
 
 
@@ -224,7 +228,7 @@ def test_attention(hd, nq, nkv, block, cap, lens, rows, n_self, dtype):
     _same(g, c)
 
 
-@pytest.mark.parametrize("hd,nq,nkv,block,cap,lens,rows,n_self,dtype", ATTEND[:1] + ATTEND[2:9:2] + ATTEND[9:13] + ATTEND[13:16])
+@pytest.mark.parametrize("hd,nq,nkv,block,cap,lens,rows,n_self,dtype", ATTEND[:1] + ATTEND[2:9:2] + ATTEND[9:13] + ATTEND[13:16] + ATTEND[18::2])
 def test_accumulated_weights(hd, nq, nkv, block, cap, lens, rows, n_self, dtype):
     r = np.random.default_rng(hd + cap + rows + 1)
     c = _draw_cache(r, 4, nkv, cap, hd, block, lens + [cap])
