@@ -343,8 +343,8 @@ __global__ __launch_bounds__(NW * 64) void cache_attn_kernel(CacheAttnArgs a, Pa
 }
 
 // ---------------------------------------------------------------------------
-// Many rows: a block of 8 waves owns 128 rows of a (batch row, kv head) and walks stages of 64
-// keys; wave (rg, kh) takes the 32 rows of group rg over the half kh of every stage, and the two
+// Many rows: a block of 8 waves owns 128 rows of a (batch row, kv head) and walks stages of 64 (256
+// dims) or 128 keys; wave (rg, kh) takes the 32 rows of group rg over the half kh of every stage, and the two
 // waves of a group are joined at the end.  (One wave a group with twice the keys would need more
 // than the 256 registers that vector instructions reach; two also overlap one's exponentials with
 // the other's matrix instructions where a CU holds one block.)  On the 32 x 32 matrix
@@ -359,6 +359,10 @@ __global__ __launch_bounds__(NW * 64) void cache_attn_kernel(CacheAttnArgs a, Pa
 // dim's 4 keys.  The next stage's codes are on their way into registers while one is computed on,
 // by buffer loads, which leave the addresses to scalar registers and give 0 past the last token.
 // One barrier a stage.
+//
+// 64 sequences of 400 rows of 256 dims over 866 keys (22.7 GFLOP) take 41 us, 0.55 PFLOP/s.  Of a
+// stage's 2.2 us the matrix instructions take 0.96 and the LDS traffic (K and V once a row group,
+// 2 HD bytes a key and wave) 1.1; start and end of a block take 7.
 // ---------------------------------------------------------------------------
 typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16_t;
 typedef __attribute__((__vector_size__(4 * sizeof(short)))) short s16x4_t;
@@ -399,10 +403,9 @@ __global__ __launch_bounds__(512, 2) void cache_attn_tile_kernel(CacheAttnArgs a
   constexpr int RP = CH2 >= 16 ? 1 : 16 / CH2;    // tokens per 256 bytes (all banks)
   constexpr int XK = (CH2 < 16 ? CH2 : 16) - 1;   // swizzle masks: keys' fragments take 16 rows' same chunk,
   constexpr int XV = (CH2 < 16 ? CH2 : 16) / 4 - 1;  // values' four rows' same four chunks
-  // two buffers of keys and values; at the end half of a row group's accumulators, then a wave's
-  // output rows
+  // two buffers of keys and values; at the end half of each wave's accumulators, then its output rows
   __shared__ __attribute__((aligned(1024))) char buf[4 * TB];
-  __shared__ float ml_s[RB][2];
+  __shared__ float ml_s[2][RB][2];
   // at 256 dims the last QL query fragments live in LDS: with all of them in registers some
   // spill, and a reload waits for every load of the next stage
   constexpr int QL = HD == 256 ? 7 : 0;
@@ -452,15 +455,42 @@ __global__ __launch_bounds__(512, 2) void cache_attn_tile_kernel(CacheAttnArgs a
   // chunk ch of row r in LDS
   const auto k_at = [](int r, int ch) { return r * 2 * HD + ((ch ^ ((r / RP) & XK)) << 4); };
   const auto v_at = [](int r, int ch) { return TB + r * 2 * HD + ((ch ^ ((r / RP) & XV) << 2) << 4); };
+  // own tokens of stage t, through registers into LDS
+  const auto load_own = [&](int t, u32x4_t (&ok)[NL2], u32x4_t (&ov)[NL2]) {
+#pragma unroll
+    for (int i = 0; i < NL2; ++i) {
+      const int p = tid + i * 512, r = p / CH2, ch = p % CH2;
+      if (TB < 8192 && p >= TB / 16) break;
+      const long long at = b * a.sb + (long long)min(t * SK + r, S - 1) * a.st + g * a.sh + ch * 8;
+      ok[i] = *(const u32x4_t*)((const bf16_t*)a.sk + at);
+      ov[i] = *(const u32x4_t*)((const bf16_t*)a.sv + at);
+    }
+  };
+  const auto store_own = [&](int t, const u32x4_t (&ok)[NL2], const u32x4_t (&ov)[NL2]) {
+#pragma unroll
+    for (int i = 0; i < NL2; ++i) {
+      const int p = tid + i * 512, r = p / CH2, ch = p % CH2;
+      if (TB < 8192 && p >= TB / 16) break;
+      *(u32x4_t*)(buf + (t & 1) * 2 * TB + k_at(r, ch)) = ok[i];
+      *(u32x4_t*)(buf + (t & 1) * 2 * TB + v_at(r, ch)) = ov[i];
+    }
+  };
+  // the first stage's loads are all on their way before the first is waited for
+  u32x4_t ok0[NL2], ov0[NL2];
+  if (t0 < st) load_own(t0, ok0, ov0);
   if (c0 < c1 && t0 >= st) load(c0);
 
-  bf16x8_t q[KS - QL];
+  bf16x8_t q[KS - QL], qx[KS];
   {
     const int r = min(row, R - 1);  // rows past the group are computed and never stored
     const bf16_t* qr = (const bf16_t*)a.q + b * a.qb + r % a.rows * a.qr + (g * G + r / a.rows) * a.qh + h * 16;
 #pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qx[ks] = *(const bf16x8_t*)(qr + (ks >> 1) * 32 + (ks & 1) * 8);
+    __builtin_amdgcn_sched_barrier(0);
+    if (t0 < st) store_own(t0, ok0, ov0);
+#pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
-      const bf16x8_t x = *(const bf16x8_t*)(qr + (ks >> 1) * 32 + (ks & 1) * 8);
+      const bf16x8_t x = qx[ks];
       if (ks < KS - QL)
         q[ks] = x;
       else if (kh == 0)
@@ -480,35 +510,49 @@ __global__ __launch_bounds__(512, 2) void cache_attn_tile_kernel(CacheAttnArgs a
   const int ka0 = k_at(kh * 32 * NT + l32, h * 2);
   const int va0 = v_at(kh * 32 * NT + 4 * h + ((lane & 15) >> 2), ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) + (lane & 1) * 8;
 
+  const auto store = [&](int t) {  // the stage in registers, converted, into LDS
+    char* const kb = buf + (t & 1) * 2 * TB;
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int p = tid + i * 512, r = p / CH, ch = p % CH * 2;
+      if (CB < 8192 && p >= CB / 16) break;
+      const int ka = k_at(r, ch), va = v_at(r, ch);
+      *(bf16x8_t*)(kb + ka) = scaled8(kl[i][0], kl[i][1], kscale[i]);
+      *(bf16x8_t*)(kb + (ka ^ 16)) = scaled8(kl[i][2], kl[i][3], kscale[i]);
+      *(bf16x8_t*)(kb + va) = scaled8(vl[i][0], vl[i][1], vscale[i]);
+      *(bf16x8_t*)(kb + (va ^ 16)) = scaled8(vl[i][2], vl[i][3], vscale[i]);
+    }
+  };
+  const auto fetch = [&](int t) {
+    if (t >= st && t < t1) load(t - st);
+  };
+  if (t0 >= st && t0 < t1) store(t0);
+  // Of a SIMD's two waves one writes the next stage before it computes on this one, the other after,
+  // and matrix instructions go first: so one's conversions and exponentials fall into the
+  // other's products (256 / 128 dims 43.6 / 45.0 -> 41.2 / 41.9 us; 64 dims 17.1 and 18.4: not there).
+  constexpr bool kStagger = HD >= 128;
+  const bool early = kStagger && wave >= 4;
+  const auto first = [&](bool on) {
+    if constexpr (kStagger) {
+      if (on)
+        __builtin_amdgcn_s_setprio(1);
+      else
+        __builtin_amdgcn_s_setprio(0);
+    }
+  };
+  if (early) fetch(t0 + 1);
   for (int t = t0; t < t1; ++t) {
     char* const kb = buf + (t & 1) * 2 * TB;
-    int left;  // keys of this wave's part that are there; without any the probabilities are 0
-    if (t < st) {  // own tokens
-      left = S - t * SK - kh * 32 * NT;
-#pragma unroll
-      for (int i = 0; i < NL2; ++i) {
-        const int p = tid + i * 512, r = p / CH2, ch = p % CH2;
-        if (TB < 8192 && p >= TB / 16) break;
-        const long long at = b * a.sb + (long long)min(t * SK + r, S - 1) * a.st + g * a.sh + ch * 8;
-        *(u32x4_t*)(kb + k_at(r, ch)) = *(const u32x4_t*)((const bf16_t*)a.sk + at);
-        *(u32x4_t*)(kb + v_at(r, ch)) = *(const u32x4_t*)((const bf16_t*)a.sv + at);
-      }
-    } else {
-      left = n - (t - st) * SK - kh * 32 * NT;
-#pragma unroll
-      for (int i = 0; i < NL; ++i) {
-        const int p = tid + i * 512, r = p / CH, ch = p % CH * 2;
-        if (CB < 8192 && p >= CB / 16) break;
-        const int ka = k_at(r, ch), va = v_at(r, ch);
-        *(bf16x8_t*)(kb + ka) = scaled8(kl[i][0], kl[i][1], kscale[i]);
-        *(bf16x8_t*)(kb + (ka ^ 16)) = scaled8(kl[i][2], kl[i][3], kscale[i]);
-        *(bf16x8_t*)(kb + va) = scaled8(vl[i][0], vl[i][1], vscale[i]);
-        *(bf16x8_t*)(kb + (va ^ 16)) = scaled8(vl[i][2], vl[i][3], vscale[i]);
-      }
-    }
+    // keys of this wave's part that are there; without any the probabilities are 0
+    const int left = (t < st ? S - t * SK : n - (t - st) * SK) - kh * 32 * NT;
     __syncthreads();
-    if (t + 1 >= st && t + 1 < t1) load(t + 1 - st);
-
+    if (t + 1 < min(st, t1)) {
+      load_own(t + 1, ok0, ov0);
+      store_own(t + 1, ok0, ov0);
+    } else if (early && t + 1 < t1) {
+      store(t + 1);
+    }
+    fetch(early ? t + 2 : t + 1);
     // Fragments are read ahead, and the steps keep their order: with two tiles the exponentials of
     // the first lie between the matrix instructions of the second's scores, those of the
     // second between the first's of the second product.
@@ -606,96 +650,87 @@ __global__ __launch_bounds__(512, 2) void cache_attn_tile_kernel(CacheAttnArgs a
     };
 #pragma unroll
     for (int j = 0; j < PK; ++j) kf[j] = read_k(j);
+    first(true);
     scores(0);
+    first(false);
     if constexpr (NT == 2) {
       maximum(0);
+      first(true);
       scores(1);
+      first(false);
     }
     if constexpr (NT == 2) {
 #pragma unroll
       for (int j = 0; j < PV; ++j) vf[j] = read_v(j);
       __builtin_amdgcn_sched_barrier(0);
       maximum(1);
+      first(true);
       outputs(0);
       outputs(1);
+      first(false);
     } else {
       maximum(0);
       exponentials(0, 0, 16);
 #pragma unroll
       for (int j = 0; j < PV; ++j) vf[j] = read_v(j);
+      first(true);
       outputs(0);
+      first(false);
     }
+    if (!early && t + 1 >= st && t + 1 < t1) store(t + 1);
   }
 
-  // join the two waves of a row group (their lanes hold the same dims of the same rows), half of
-  // the accumulators at a time: each wave gives one half and keeps the other
+  // The two waves of a row group hold the same dims of the same rows in the same lanes: each gives
+  // the other one half of its accumulators and finishes the other half.
   l = half_sum(l);
   __syncthreads();  // the buffers are free
-  if (kh == 1 && h == 0) {
-    ml_s[rg * 32 + l32][0] = m;
-    ml_s[rg * 32 + l32][1] = l;
+  constexpr int HR = DT * 8;  // accumulators of half the dims
+  const auto acc = [&](int r) -> f32x4_t {
+    return f32x4_t{o[r / 16][r % 16], o[r / 16][r % 16 + 1], o[r / 16][r % 16 + 2], o[r / 16][r % 16 + 3]};
+  };
+  if (h == 0) {
+    ml_s[kh][rg * 32 + l32][0] = m;
+    ml_s[kh][rg * 32 + l32][1] = l;
   }
-  float* jb = (float*)buf + rg * DT * 8 * 64 + lane;  // (a group: 32 rows of 2 HD bytes)
-  constexpr int HR = DT * 16;  // accumulators of a lane
-  if (kh == 1) {
+  char* give = buf + wave * HR * 256 + lane * 16;
 #pragma unroll
-    for (int r = 0; r < HR / 2; ++r) jb[r * 64] = o[r / 16][r % 16];
-  }
+  for (int r = 0; r < HR; r += 4) *(f32x4_t*)(give + r * 256) = kh ? acc(r) : acc(HR + r);
   __syncthreads();
-  float mm = m, w0 = 1.f, w1 = 0.f, den = l;
-  if (kh == 0) {
-    const float m1 = ml_s[rg * 32 + l32][0], l1 = ml_s[rg * 32 + l32][1];
-    mm = fmaxf(m, m1);
-    const float ref = mm == -INFINITY ? 0.f : mm;
-    w0 = __builtin_amdgcn_exp2f(m - ref);
-    w1 = __builtin_amdgcn_exp2f(m1 - ref);
-    den = w0 * l + w1 * l1;
+  if (idle) return;
+  const float m1 = ml_s[kh ^ 1][rg * 32 + l32][0], l1 = ml_s[kh ^ 1][rg * 32 + l32][1], mm = fmaxf(m, m1);
+  const float ref = mm == -INFINITY ? 0.f : mm;
+  const float w0 = __builtin_amdgcn_exp2f(m - ref), w1 = __builtin_amdgcn_exp2f(m1 - ref), den = w0 * l + w1 * l1;
+  char* const ob = buf + (wave ^ 1) * HR * 256;  // what the other gave: read by this wave only
+  f32x4_t y[HR / 4];  // y[r]: dim HD / 2 * kh + 8 r + 4 h + ...
 #pragma unroll
-    for (int r = 0; r < HR / 2; ++r) o[r / 16][r % 16] = o[r / 16][r % 16] * w0 + jb[r * 64] * w1;
-  }
-  __syncthreads();
-  if (kh == 1) {
-#pragma unroll
-    for (int r = HR / 2; r < HR; ++r) jb[(r - HR / 2) * 64] = o[r / 16][r % 16];
-  }
-  __syncthreads();
-  if (kh == 1 || idle) return;
-#pragma unroll
-  for (int r = HR / 2; r < HR; ++r) o[r / 16][r % 16] = o[r / 16][r % 16] * w0 + jb[(r - HR / 2) * 64] * w1;
-  // o[d][r]: dim 32 d + 8 (r / 4) + 4 h + r % 4
+  for (int r = 0; r < HR; r += 4) y[r / 4] = (kh ? acc(HR + r) : acc(r)) * w0 + *(const f32x4_t*)(ob + lane * 16 + r * 256) * w1;
   if (part.nsplit > 1) {
     if (row >= R) return;
     const long long pr = (((long long)split * a.batch + b) * c.nkv + g) * R + row;
 #pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-      for (int r = 0; r < 16; r += 4)
-        *(f32x4_t*)(part.o + pr * HD + d * 32 + r * 2 + h * 4) = f32x4_t{o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]};
-    if (h == 0) {
+    for (int r = 0; r < HR / 4; ++r) *(f32x4_t*)(part.o + pr * HD + HD / 2 * kh + 8 * r + 4 * h) = y[r];
+    if (lane < 32 && kh == 0) {
       part.ml[pr * 2] = mm;
       part.ml[pr * 2 + 1] = den;
     }
     return;
   }
   const float inv = den == 0.f ? 0.f : 1.f / den;  // a row that sees nothing: 0
-  if (part.lse && h == 0 && row < R) part.lse[((long long)b * c.nkv + g) * R + row] = den == 0.f ? INFINITY : mm + log2f(den);
-  // through LDS (this group's part of the join's), so that whole rows are written: 8-byte pieces
-  // XOR-swizzled by row
-  constexpr int PX = HD / 4 - 1 < 31 ? HD / 4 - 1 : 31;
-  char* ob = buf + rg * 64 * HD;
+  if (part.lse && lane < 32 && kh == 0 && row < R)
+    part.lse[((long long)b * c.nkv + g) * R + row] = den == 0.f ? INFINITY : mm + log2f(den);
+  // through LDS, so that half rows are written whole: 8-byte pieces XOR-swizzled by row
+  constexpr int PX = (HD / 8 < 32 ? HD / 8 : 32) - 1;
 #pragma unroll
-  for (int d = 0; d < DT; ++d)
-#pragma unroll
-    for (int r = 0; r < 16; r += 4)
-      *(u32x2_t*)(ob + l32 * 2 * HD + (((8 * d + r / 2 + h) ^ (l32 * 2 & PX)) << 3)) =
-          u32x2_t{pack_bf16x2(o[d][r] * inv, o[d][r + 1] * inv), pack_bf16x2(o[d][r + 2] * inv, o[d][r + 3] * inv)};
-  constexpr int RS = 512 / HD;  // rows a store
-  int r = lane / (HD / 8), ix = (row0 + r) % a.rows, hx = (row0 + r) / a.rows;
-  const int x = lane % (HD / 8);
+  for (int r = 0; r < HR / 4; ++r)
+    *(u32x2_t*)(ob + l32 * HD + (((2 * r + h) ^ (l32 * 2 & PX)) << 3)) =
+        u32x2_t{pack_bf16x2(y[r][0] * inv, y[r][1] * inv), pack_bf16x2(y[r][2] * inv, y[r][3] * inv)};
+  constexpr int RS = 1024 / HD;  // rows a store
+  int r = lane / (HD / 16), ix = (row0 + r) % a.rows, hx = (row0 + r) / a.rows;
+  const int xc = lane % (HD / 16);
 #pragma unroll 4
-  for (int i = 0; i < HD / 16; ++i) {
-    const u32x4_t w = *(const u32x4_t*)(ob + r * 2 * HD + (((2 * x) ^ (r * 2 & PX)) << 3));
-    if (row0 + r < R) *(u32x4_t*)((bf16_t*)a.out + b * a.ob + ix * a.orow + (g * G + hx) * a.oh + x * 8) = w;
+  for (int i = 0; i < 32 / RS; ++i) {
+    const u32x4_t w = *(const u32x4_t*)(ob + r * HD + (((2 * xc) ^ (r * 2 & PX)) << 3));
+    if (row0 + r < R) *(u32x4_t*)((bf16_t*)a.out + b * a.ob + ix * a.orow + (g * G + hx) * a.oh + HD / 2 * kh + xc * 8) = w;
     r += RS;
     ix += RS;
     while (ix >= a.rows) {
