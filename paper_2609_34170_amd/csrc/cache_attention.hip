@@ -793,12 +793,27 @@ __global__ __launch_bounds__(64) void cache_join_kernel(CacheAttnArgs a, Part pa
 // Batch rows that name one sequence are added in row order by the first of them, so that the
 // sums have one order.  One wave, or all four of the block where there would be too few (they
 // read the same keys: one row of each of 16 heads over 8000 keys 7.5 us with one, 28 with more;
-// 400 rows of 256 dims over 16 x 816 keys 17 us with four).
+// 400 rows of 256 dims over 816 keys 13 us with four, 37 with one).
+//
+// Keys and rows come in whole lines and go through LDS: fragment by fragment from memory each load
+// touches 32 lines, and the rows, read once for every 64 keys, bind on that (400 rows of 128 dims over 64
+// heads of 2048 keys 44 us so, 25 through LDS; of 256 dims over 64 x 816 keys 40 and 30).
 constexpr int WW = 4;  // waves of a block of keys
+// order of a wave's own accesses to LDS, lane to lane
+RAVEL_DEV void wave_lds_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 template <int HD, bool F32>
-__global__ __launch_bounds__(WW * 64) void cache_weight_kernel(CacheAttnArgs a, const float* lse, int rw) {
+__global__ __launch_bounds__(WW * 64, 2) void cache_weight_kernel(CacheAttnArgs a, const float* lse, int rw) {
   constexpr int KS = HD / 16, NP = F32 ? 3 : 1;
+  constexpr int CK = HD / 16, CQ = HD / 8;  // 16-byte chunks of a key, of a bf16 row
+  constexpr int RS = 64 / CQ;               // rows of a load
+  constexpr bool kAhead = HD < 256;         // the next rows' loads in flight: 256 dims' do not fit the registers
   __shared__ float sum_s[WW][64];
+  __shared__ float ls_s[WW][32];
+  __shared__ __attribute__((aligned(128))) char stage_s[WW][64 * HD];  // a wave's keys, then 32 rows
   const CacheView& c = a.c;
   const int bid = xcd_block(), bk = 64 * WW / rw, nkt = (c.cap + bk - 1) / bk;  // keys of a block
   const int g = bid / nkt % c.nkv, b0 = bid / nkt / c.nkv;
@@ -809,21 +824,74 @@ __global__ __launch_bounds__(WW * 64) void cache_weight_kernel(CacheAttnArgs a, 
   const int n = cache_len(c, id), key0 = bid % nkt * bk + wave / rw * 64, sub = wave % rw;
   const int G = a.nq / c.nkv, R = G * a.rows;
   const long long head = (long long)id * c.nkv + g;
+  char* const sw = stage_s[wave];
+  // chunk ch of row r of C chunks: 8 neighbouring rows' same chunk fall on all banks
+  const auto at = [](int C, int r, int ch) {
+    return (r * C + (ch ^ (C < 8 ? r / (8 / C) & (C - 1) : r & 7))) * 16;
+  };
   float acc[2] = {0.f, 0.f};
   if (key0 < n && sub * 32 < R) {
+    u32x4_t raw[CK];
+#pragma unroll
+    for (int i = 0; i < CK; ++i) {
+      const int p = i * 64 + lane;
+      raw[i] = *(const u32x4_t*)(c.k + (head * c.cap + min(key0 + p / CK, n - 1)) * HD + p % CK * 16);
+    }
+    float sc[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) sc[u] = c.ks[head * c.nblk + (min(key0 + 32 * u + l32, n - 1) >> c.shift)];
+    // bf16 rows r0 to r0 + 31 and their sums, on their way into registers (rows past the group: row 0,
+    // with a sum that makes their weights 0)
+    u32x4_t qraw[CK];
+    float lraw;
+    // A step of some rows is di further on in rows and dh in heads, or one head more and a.rows back.
+    const long long wrap = a.qh - a.rows * a.qr, step = RS % a.rows * a.qr + RS / a.rows * a.qh;
+    const int skip = (rw - 1) * 32;
+    const long long leap = skip % a.rows * a.qr + skip / a.rows * a.qh;
+    const int r_first = sub * 32 + lane / CQ, i_first = r_first % a.rows;
+    const long long off_first = i_first * a.qr + r_first / a.rows * a.qh;
+    int qrow, qi;
+    long long off;
+    const auto move = [&](int rows, int i, long long by) {
+      qrow += rows;
+      qi += i;
+      off += by;
+      if (qi >= a.rows) {
+        qi -= a.rows;
+        off += wrap;
+      }
+    };
+    const auto fetch = [&](int b, int r0) {
+      if constexpr (!F32) {
+        const bf16_t* q = (const bf16_t*)a.q + b * a.qb + g * G * a.qh + lane % CQ * 8;
+        if (r0 == sub * 32) {
+          qrow = r_first;
+          qi = i_first;
+          off = off_first;
+        } else {
+          move(skip, skip % a.rows, leap);
+        }
+#pragma unroll
+        for (int i = 0; i < CK; ++i) {
+          qraw[i] = *(const u32x4_t*)(q + (qrow < R ? off : 0));
+          move(RS, RS % a.rows, step);
+        }
+        lraw = r0 + l32 < R ? lse[((long long)b * c.nkv + g) * R + r0 + l32] : INFINITY;
+      }
+    };
+    if (kAhead) fetch(b0, sub * 32);
+#pragma unroll
+    for (int i = 0; i < CK; ++i) *(u32x4_t*)(sw + at(CK, (i * 64 + lane) / CK, (i * 64 + lane) % CK)) = raw[i];
+    wave_lds_order();
     bf16x8_t kf[2][KS];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int key = min(key0 + 32 * u + l32, n - 1);
-      const float sc = c.ks[head * c.nblk + (key >> c.shift)];
-      const uint8_t* p = c.k + (head * c.cap + key) * HD + h * 16;
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int j = 0; j < KS / 2; ++j) {
-        const u32x4_t w = *(const u32x4_t*)(p + j * 32);
-        kf[u][2 * j] = scaled8(w[0], w[1], sc);
-        kf[u][2 * j + 1] = scaled8(w[2], w[3], sc);
+        const u32x4_t w = *(const u32x4_t*)(sw + at(CK, 32 * u + l32, 2 * j + h));
+        kf[u][2 * j] = scaled8(w[0], w[1], sc[u]);
+        kf[u][2 * j + 1] = scaled8(w[2], w[3], sc[u]);
       }
-    }
     const float sl2 = a.scale * kLog2e;
     // the rows that name this sequence, found 64 at a time; only b0 where all rows differ
     const int b1 = !a.seq.idx || a.seq.row ? b0 + 1 : a.batch;
@@ -832,38 +900,50 @@ __global__ __launch_bounds__(WW * 64) void cache_weight_kernel(CacheAttnArgs a, 
       for (; same; same &= same - 1) {
         const int b = bw + __builtin_ctzll(same);
         const float* lr = lse + ((long long)b * c.nkv + g) * R;
+        if (kAhead && b != b0) fetch(b, sub * 32);
         for (int r0 = sub * 32; r0 < R; r0 += rw * 32) {
-          const int r = min(r0 + l32, R - 1);
-          const long long at = b * a.qb + r % a.rows * a.qr + (g * G + r / a.rows) * a.qh + h * 16;
-          // 32 bits: planes are made fragment by fragment; bf16: every fragment on its way at once
-          bf16x8_t q[F32 ? 1 : KS][NP];
-          if constexpr (!F32) {
+          f32x4_t ls[4];
+          if constexpr (F32) {
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) load8<false>(a.q, at + (ks >> 1) * 32 + (ks & 1) * 8, q[ks]);
-          }
-          float ls[16];
+            for (int i = 0; i < 16; ++i) {
+              const int rr = r0 + 8 * (i >> 2) + 4 * h + (i & 3);
+              ls[i >> 2][i & 3] = rr < R ? lr[min(rr, R - 1)] : INFINITY;
+            }
+          } else {
+            wave_lds_order();
+            if (!kAhead) fetch(b, r0);
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int rr = r0 + 8 * (i >> 2) + 4 * h + (i & 3);
-            ls[i] = rr < R ? lr[min(rr, R - 1)] : INFINITY;
+            for (int i = 0; i < CK; ++i) *(u32x4_t*)(sw + at(CQ, (i * 64 + lane) / CQ, (i * 64 + lane) % CQ)) = qraw[i];
+            ls_s[wave][l32] = lraw;
+            wave_lds_order();
+            if (kAhead && r0 + rw * 32 < R) fetch(b, r0 + rw * 32);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) ls[i] = *(const f32x4_t*)&ls_s[wave][8 * i + 4 * h];
           }
           f32x16_t s[2];
 #pragma unroll
           for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[u][i] = 0.f;
+          // 32 bits: planes are made fragment by fragment
+          const int r = min(r0 + l32, R - 1);
+          const long long q0 = F32 ? b * a.qb + r % a.rows * a.qr + (g * G + r / a.rows) * a.qh + h * 16 : 0;
 #pragma unroll
           for (int ks = 0; ks < KS; ++ks) {
-            if constexpr (F32) load8<true>(a.q, at + (ks >> 1) * 32 + (ks & 1) * 8, q[0]);
+            bf16x8_t q[NP];
+            if constexpr (F32)
+              load8<true>(a.q, q0 + (ks >> 1) * 32 + (ks & 1) * 8, q);
+            else
+              q[0] = *(const bf16x8_t*)(sw + at(CQ, l32, (ks >> 1) * 4 + h * 2 + (ks & 1)));
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-              for (int p = NP - 1; p >= 0; --p) s[u] = mfma32(q[F32 ? 0 : ks][p], kf[u][ks], s[u]);
+              for (int p = NP - 1; p >= 0; --p) s[u] = mfma32(q[p], kf[u][ks], s[u]);
           }
 #pragma unroll
           for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) acc[u] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i], sl2, -ls[i]));
+            for (int i = 0; i < 16; ++i) acc[u] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i], sl2, -ls[i >> 2][i & 3]));
         }
       }
     }
