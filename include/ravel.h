@@ -418,8 +418,8 @@ typedef struct {
  *   of 8, or 4 in 32 bits).
  * A block that also holds older tokens keeps its scale, or, where the new tokens need a larger one,
  * has its older codes rounded to that.  Infinities become the largest code, NaN stays NaN; neither
- * counts for the scale.  Accumulated weights of the stored tokens start at 0.  pos and count must
- * not be the cache's len (but pos == len is taken as NULL).  A sequence that an earlier row names
+ * counts for the scale.  Accumulated weights of the stored tokens start at 0.  seq, pos and count
+ * must not lie in the cache's len (but pos == len is taken as NULL).  A sequence that an earlier row names
  * already is not written again.
  * Errors: E_INVALID (null pointer, alignment, dtype, block), E_SHAPE (sizes, strides). */
 ravel_status ravel_cache_append(const ravel_cache* cache, int32_t batch, const int32_t* seq, const int32_t* pos,
@@ -434,7 +434,8 @@ ravel_status ravel_cache_append(const ravel_cache* cache, int32_t batch, const i
  * products are as good as 32 bits.  A row that sees nothing (len 0 and no own tokens, or no
  * sequence) is 0.  With track, every cached token's softmax weights, summed over the rows and the
  * query heads of its KV head, are added to the cache's accumulated weight (batch rows that name one
- * sequence are added in row order).
+ * sequence are added in row order).  out shares no element with the inputs; scale is finite and not
+ * negative.
  * Strides in elements, (b, row or token, head); 16-byte aligned vectors (multiples of 8 elements, or
  * 4 in 32 bits).  workspace: ravel_cache_attention_workspace() bytes, 256-byte aligned, of this call
  * alone until it has run (NULL when that is 0). */

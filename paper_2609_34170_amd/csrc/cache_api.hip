@@ -1,6 +1,8 @@
 // C ABI of the 8-bit key/value cache: argument checks, then the launches of cache.hip and
 // cache_attention.hip.
+#include <array>
 #include <climits>
+#include <cmath>
 
 #include "cache.h"
 
@@ -11,6 +13,10 @@ namespace {
 ravel_status bad(const char* call, const std::string& msg) { return set_error(RAVEL_E_INVALID, std::string(call) + ": " + msg); }
 ravel_status bad_shape(const char* call, const std::string& msg) { return set_error(RAVEL_E_SHAPE, std::string(call) + ": " + msg); }
 bool aligned(const void* p, size_t n) { return (uintptr_t)p % n == 0; }
+
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+  return a && b && (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
+}
 
 #define CACHE_TRY(expr)              \
   do {                               \
@@ -86,6 +92,7 @@ ravel_status check_query_sizes(const char* call, const ravel_cache* c, const rav
   CACHE_TRY(check_dtype(call, q->dtype));
   CACHE_TRY(check_batch(call, q->batch, nullptr));
   if (q->reserved) return bad(call, "reserved must be 0");
+  if (!(q->scale >= 0.f && q->scale < INFINITY)) return bad(call, "scale must be finite and not negative");
   if (q->n_q_heads < 1 || q->n_q_heads % c->n_kv_heads) return bad_shape(call, "n_q_heads must be a multiple of n_kv_heads");
   if (q->rows < 1 || q->rows > 1 << 20) return bad_shape(call, "rows must be in 1..2^20");
   if (q->n_self < 0 || q->n_self > 1 << 20) return bad_shape(call, "n_self must be in 0..2^20");
@@ -131,7 +138,10 @@ ravel_status ravel_cache_append(const ravel_cache* c, int32_t batch, const int32
   if (!aligned(pos, 4) || !aligned(count, 4)) return bad(me, "pos and count must be 4-byte aligned");
   if (n > 0 && batch > 0 && (!k || !v)) return bad(me, "null keys or values");
   if (!aligned(k, 16) || !aligned(v, 16)) return bad(me, "keys and values must be 16-byte aligned");
-  if (count && count == c->len) return bad(me, "count must not be the cache's len");
+  // the call moves the lengths while other rows still read theirs
+  const size_t nl = (size_t)c->n_seq * 4, ni = (size_t)batch * 4;
+  if (overlap(seq, ni, c->len, nl) || overlap(count, ni, c->len, nl) || (pos != c->len && overlap(pos, ni, c->len, nl)))
+    return bad(me, "seq, pos and count must not lie in the cache's len");
   CacheAppendArgs a;
   a.c = view(c);
   a.seq = seq_map(seq);
@@ -174,6 +184,7 @@ ravel_status ravel_cache_attention(const ravel_cache* c, const ravel_cache_query
   if (need > 0 && (!q->workspace || q->workspace_bytes < 0 || (size_t)q->workspace_bytes < need))
     return bad(me, "needs a workspace of " + std::to_string(need) + " bytes");
   if (need > 0 && !aligned(q->workspace, 256)) return bad(me, "the workspace must be 256-byte aligned");
+  if (q->out == q->q) return bad(me, "out must not be the queries' memory");
   return launched(me, launch_cache_attention(a, (hipStream_t)stream));
 }
 
@@ -202,11 +213,19 @@ ravel_status ravel_cache_evict(const ravel_cache* c, int32_t batch, const int32_
     if (into->n_kv_heads != c->n_kv_heads || into->head_dim != c->head_dim || into->block != c->block)
       return bad_shape(me, "both caches must have the same KV heads, head_dim and block");
     if (into->capacity < (keep < c->capacity ? keep : c->capacity)) return bad_shape(me, "the destination holds fewer than keep tokens");
-    const size_t n1 = (size_t)c->n_seq * c->n_kv_heads * c->capacity * c->head_dim;
-    const size_t n2 = (size_t)into->n_seq * into->n_kv_heads * into->capacity * into->head_dim;
-    for (const void* p : {c->k, c->v})
-      for (const void* q : {into->k, into->v})
-        if ((uintptr_t)p < (uintptr_t)q + n2 && (uintptr_t)q < (uintptr_t)p + n1) return bad(me, "the caches share memory");
+    struct Piece {
+      const void* p;
+      size_t bytes;
+    };
+    const auto pieces = [](const ravel_cache* x) {
+      const size_t heads = (size_t)x->n_seq * x->n_kv_heads, tokens = heads * x->capacity;
+      const size_t scales = heads * ((x->capacity + x->block - 1) / x->block) * 4;
+      return std::array<Piece, 6>{{{x->k, tokens * x->head_dim}, {x->v, tokens * x->head_dim}, {x->k_scale, scales},
+                                   {x->v_scale, scales}, {x->len, (size_t)x->n_seq * 4}, {x->weight, tokens * 4}}};
+    };
+    for (const Piece& p : pieces(c))
+      for (const Piece& q : pieces(into))
+        if (overlap(p.p, p.bytes, q.p, q.bytes)) return bad(me, "the caches share memory");
   } else if (into_seq) {
     return bad(me, "into_seq without a destination");
   }

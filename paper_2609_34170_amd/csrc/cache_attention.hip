@@ -380,6 +380,11 @@ RAVEL_DEV f32x16_t mfma32(bf16x8_t a, bf16x8_t b, f32x16_t c) {
 }
 typedef __attribute__((address_space(3))) char lds_char;
 RAVEL_DEV lds_char* lds_ptr(void* p) { return (lds_char*)p; }
+// order of a wave's own accesses to LDS, lane to lane
+RAVEL_DEV void wave_lds_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
 RAVEL_DEV float half_max(float x) {  // over a lane and the one 32 further on
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
@@ -718,12 +723,13 @@ __global__ __launch_bounds__(512, 2) void cache_attn_tile_kernel(CacheAttnArgs a
   const float inv = den == 0.f ? 0.f : 1.f / den;  // a row that sees nothing: 0
   if (part.lse && lane < 32 && kh == 0 && row < R)
     part.lse[((long long)b * c.nkv + g) * R + row] = den == 0.f ? INFINITY : mm + log2f(den);
-  // through LDS, so that half rows are written whole: 8-byte pieces XOR-swizzled by row
+  // through LDS (the wave's own part), so that half rows are written whole: 8-byte pieces XOR-swizzled by row
   constexpr int PX = (HD / 8 < 32 ? HD / 8 : 32) - 1;
 #pragma unroll
   for (int r = 0; r < HR / 4; ++r)
     *(u32x2_t*)(ob + l32 * HD + (((2 * r + h) ^ (l32 * 2 & PX)) << 3)) =
         u32x2_t{pack_bf16x2(y[r][0] * inv, y[r][1] * inv), pack_bf16x2(y[r][2] * inv, y[r][3] * inv)};
+  wave_lds_order();
   constexpr int RS = 1024 / HD;  // rows a store
   int r = lane / (HD / 16), ix = (row0 + r) % a.rows, hx = (row0 + r) / a.rows;
   const int xc = lane % (HD / 16);
@@ -799,12 +805,6 @@ __global__ __launch_bounds__(64) void cache_join_kernel(CacheAttnArgs a, Part pa
 // touches 32 lines, and the rows, read once for every 64 keys, bind on that (400 rows of 128 dims over 64
 // heads of 2048 keys 44 us so, 25 through LDS; of 256 dims over 64 x 816 keys 40 and 30).
 constexpr int WW = 4;  // waves of a block of keys
-// order of a wave's own accesses to LDS, lane to lane
-RAVEL_DEV void wave_lds_order() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-}
-
 template <int HD, bool F32>
 __global__ __launch_bounds__(WW * 64, 2) void cache_weight_kernel(CacheAttnArgs a, const float* lse, int rw) {
   constexpr int KS = HD / 16, NP = F32 ? 3 : 1;
@@ -1008,7 +1008,7 @@ hipError_t launch_hd(const CacheAttnArgs& a, hipStream_t s) {
   char* ws = (char*)a.ws;
   const Part part{(float*)(ws + p.o_off), (float*)(ws + p.ml_off), a.track ? (float*)(ws + p.lse_off) : nullptr, p.nsplit};
   const long long blocks = p.chunks * heads * p.nsplit, joins = (heads * R * (HD / 4) + 63) / 64;
-  if (blocks > 0x7FFFFFFF || joins > 0x7FFFFFFF || heads * ((a.c.cap + 63) / 64) > 0x7FFFFFFF) return hipErrorInvalidValue;
+  if (blocks > 0x7FFFFFFF || joins > 0x7FFFFFFF || (a.track && heads * ((a.c.cap + 63) / 64) > 0x7FFFFFFF)) return hipErrorInvalidValue;
   if constexpr (!F32) {
     if (p.tile) hipLaunchKernelGGL((cache_attn_tile_kernel<HD>), dim3((unsigned)blocks), dim3(512), 0, s, a, part, p.chunks);
   }

@@ -407,6 +407,8 @@ class Cache:
         for t in tensors:
             if t is not None and t.get_device() != device:
                 raise ValueError(f"every tensor of the call must be on {self.device}")
+        if device < 0:
+            raise ValueError("a cache's calls need its tensors on a GPU")
         cuda = self._torch.cuda
         if stream is None:
             if device == cuda.current_device():
@@ -414,6 +416,8 @@ class Cache:
             return cuda.device(self.device), self._raw_stream(device)
         if isinstance(stream, int):
             stream = cuda.ExternalStream(stream, device=self.device)
+        elif stream.device != self.device:
+            raise ValueError(f"the stream must be one of {self.device}")
         return cuda.stream(stream), stream.cuda_stream
 
     def _index(self, name, t, batch):
