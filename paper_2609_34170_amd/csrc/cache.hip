@@ -74,8 +74,9 @@ struct Unit {
 // ---------------------------------------------------------------------------
 // Append: one block per (scale block that the row's tokens touch, kv head, K or V of a batch row).
 // The tokens are read once: their NU units a thread (of TH threads) wait in registers for the
-// scale that all of them together give (reading them again from the cache: 9.0 us for a context
-// of 18 x 816 tokens of 256 dims, 135 for 96 x 1250 tokens of 4 x 128 in 32 bits).
+// scale that all of them together give.  Memory binds: 7.4 us for a context of 18 x 816 tokens of
+// 256 dims, 117 for 96 x 1250 tokens of 4 x 128 in 32 bits, 5.2 TB/s (read again from the cache
+// instead: 9.0 and 135).
 // ---------------------------------------------------------------------------
 template <typename T, int NU, int TH>
 __global__ __launch_bounds__(TH) void cache_append_kernel(CacheAppendArgs a) {
@@ -225,7 +226,7 @@ RAVEL_DEV int block_scan(int v, int* lds, int& total) {  // exclusive; every thr
 // the first of those equal to it.  A thread holds KPT consecutive tokens' keys in registers (where
 // that is not all of them, 1024 KPT at a time), so that ranks in token order take two scans over
 // the threads' counts.  One workgroup for all of a (sequence, head): its vector instructions bind
-// (16384 tokens: 47 us with a scan for every 1024 of them and a pass over memory for every digit).
+// (16384 tokens: 18 us; 47 with a scan for every 1024 of them and a pass over memory for every digit).
 template <int KPT>
 __global__ __launch_bounds__(kSelThreads) void cache_select_kernel(CacheEvictArgs a, EvictInfo* info, int* holes) {
   constexpr int CHUNK = kSelThreads * KPT;

@@ -360,9 +360,9 @@ __global__ __launch_bounds__(NW * 64) void cache_attn_kernel(CacheAttnArgs a, Pa
 // by buffer loads, which leave the addresses to scalar registers and give 0 past the last token.
 // One barrier a stage.
 //
-// 64 sequences of 400 rows of 256 dims over 866 keys (22.7 GFLOP) take 41 us, 0.55 PFLOP/s.  Of a
-// stage's 2.2 us the matrix instructions take 0.96 and the LDS traffic (K and V once a row group,
-// 2 HD bytes a key and wave) 1.1; start and end of a block take 7.
+// 64 sequences of 400 rows of 256 dims over 866 keys (22.7 GFLOP) take 37 us, 0.62 PFLOP/s.  Of a
+// stage's 2.1 us the matrix instructions take 0.96 and the LDS traffic (K and V once a row group,
+// 2 HD bytes a key and wave) 1.1; start and end of a block take 6.
 // ---------------------------------------------------------------------------
 typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16_t;
 typedef __attribute__((__vector_size__(4 * sizeof(short)))) short s16x4_t;
