@@ -26,7 +26,9 @@ constexpr float kLazy = 8.f;
 // Waves of a block of few rows: as many as its registers take (8 of 256 dims instead of 4 and
 // key ranges to match: 400 rows over 866 keys 20 -> 15 us for 2 sequences, 30 -> 17 for 8; 16 heads
 // of 64 dims over 256 keys 7.1 -> 4.8, one launch instead of two).
-constexpr int few_row_waves(int hd, bool f32) { return hd <= 64 ? 16 : hd == 256 && f32 ? 4 : 8; }
+constexpr int few_row_waves(int hd, bool f32, int rt = 1) {
+  return hd <= 64 ? 16 : hd == 256 && (f32 || rt == 2) ? 4 : 8;
+}
 
 RAVEL_DEV f32x4_t mfma_bf16(bf16x8_t a, bf16x8_t b, f32x4_t c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
@@ -155,21 +157,22 @@ RAVEL_DEV bf16x8_t byte8(const uint32_t (&w)[8], int b) {
   return __builtin_bit_cast(bf16x8_t, (u32x4_t{codes2(a, false), codes2(c, false), codes2(d, false), codes2(e, false)}));
 }
 
-// Few rows: a block owns 16 rows of a (batch row, kv head) and a range of its keys; its waves
+// Few rows: a block owns 16 RT rows of a (batch row, kv head) and a range of its keys; its waves
 // take the range's tiles of 32 in turn and are joined at the end.  Nothing but the joining goes
 // through LDS: a wave loads its own keys as the first product's operand lies, and values 8 keys x
 // HD / 16 dims a lane, transposed by byte permutes (whole rows either way).
-template <int HD, bool F32, int NW = few_row_waves(HD, F32)>
+// Turning codes into operands binds where the codes are at hand: 32 rows share it.
+template <int HD, bool F32, int RT, int NW = few_row_waves(HD, F32, RT)>
 __global__ __launch_bounds__(NW * 64) void cache_attn_kernel(CacheAttnArgs a, Part part, int chunks) {
   constexpr int KS = HD / 32, NT = HD / 16, NP = F32 ? 3 : 1;
-  __shared__ __attribute__((aligned(16))) float so[NW][16][HD + 4];
-  __shared__ float sml[NW][16][2];
+  __shared__ __attribute__((aligned(16))) float so[NW][16 * RT][HD + 4];
+  __shared__ float sml[NW][16 * RT][2];
   const CacheView& c = a.c;
   const int split = blockIdx.x % part.nsplit, chunk = blockIdx.x / part.nsplit % chunks;
   const int bg = blockIdx.x / (part.nsplit * chunks), g = bg % c.nkv, b = bg / c.nkv;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, grp = lane >> 4;
-  const int G = a.nq / c.nkv, R = G * a.rows, row = chunk * 16 + l16;
+  const int G = a.nq / c.nkv, R = G * a.rows;
   const int id = cache_seq(c, a.seq, b), n = id < 0 ? 0 : cache_len(c, id), S = id < 0 ? 0 : a.n_self;
   const int ct = (n + 31) >> 5, tiles = ct + ((S + 31) >> 5);
   const int t0 = tiles * split / part.nsplit, t1 = tiles * (split + 1) / part.nsplit;  // (at most 64 splits)
@@ -177,41 +180,44 @@ __global__ __launch_bounds__(NW * 64) void cache_attn_kernel(CacheAttnArgs a, Pa
   const uint8_t *kc = c.k + head * c.cap * HD, *vc = c.v + head * c.cap * HD;
   const float *ksc = c.ks + head * c.nblk, *vsc = c.vs + head * c.nblk;
 
-  bf16x8_t q[KS][NP];
-  {
-    const int r = min(row, R - 1);  // rows past the group are computed and never stored
+  bf16x8_t q[RT][KS][NP];
+  f32x4_t o[RT][NT];
+  float m[RT], l[RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int r = min(chunk * 16 * RT + rt * 16 + l16, R - 1);  // rows past the group are computed and never stored
     const long long at = b * a.qb + r % a.rows * a.qr + (g * G + r / a.rows) * a.qh;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) load8<F32>(a.q, at + kdim<HD>(ks, grp), q[ks]);
-  }
-  f32x4_t o[NT];
+    for (int ks = 0; ks < KS; ++ks) load8<F32>(a.q, at + kdim<HD>(ks, grp), q[rt][ks]);
 #pragma unroll
-  for (int t = 0; t < NT; ++t) o[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  float m = -INFINITY, l = 0.f;
+    for (int t = 0; t < NT; ++t) o[rt][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    m[rt] = -INFINITY;
+    l[rt] = 0.f;
+  }
   const float sl2 = a.scale * kLog2e;
 
   // x: this lane's scores (log2 units, -inf where masked) of keys 16 u + 4 grp + r; leaves
   // the probabilities times vs[u] in pl, the operand planes
-  const auto softmax = [&](float (&x)[8], const float (&vs)[2], bf16x8_t (&pl)[NP]) {
+  const auto softmax = [&](int rt, float (&x)[8], const float (&vs)[2], bf16x8_t (&pl)[NP]) {
     float mx = x[0];
 #pragma unroll
     for (int i = 1; i < 8; ++i) mx = fmaxf(mx, x[i]);
-    if (__any(mx > m + kLazy)) {
+    if (__any(mx > m[rt] + kLazy)) {
       mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
       mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-      const float mnew = mx > m + kLazy ? mx : m;
-      const float corr = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mnew);
-      m = mnew;
-      l *= corr;
+      const float mnew = mx > m[rt] + kLazy ? mx : m[rt];
+      const float corr = m[rt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[rt] - mnew);
+      m[rt] = mnew;
+      l[rt] *= corr;
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) o[t][r] *= corr;
+        for (int r = 0; r < 4; ++r) o[rt][t][r] *= corr;
     }
-    const float mref = m == -INFINITY ? 0.f : m;
+    const float mref = m[rt] == -INFINITY ? 0.f : m[rt];
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = __builtin_amdgcn_exp2f(x[i] - mref);
-    l += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+    l[rt] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] *= vs[i >> 2];
     planes<NP>(x, pl);
@@ -227,21 +233,28 @@ __global__ __launch_bounds__(NW * 64) void cache_attn_kernel(CacheAttnArgs a, Pa
     const int key0 = t * 32;
     const int blk0 = key0 >> c.shift, blk1 = min(key0 + 16, n - 1) >> c.shift;
     const float k2[2] = {ksc[blk0] * sl2, ksc[blk1] * sl2}, vs[2] = {vsc[blk0], vsc[blk1]};
-    float x[8];
+    float x[RT][8];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+      f32x4_t s[RT];
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) s[rt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         const bf16x8_t kf = key_operand<HD>(cur, u, ks);
 #pragma unroll
-        for (int p = NP - 1; p >= 0; --p) s = mfma_bf16(kf, q[ks][p], s);
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+          for (int p = NP - 1; p >= 0; --p) s[rt] = mfma_bf16(kf, q[rt][ks][p], s[rt]);
       }
 #pragma unroll
-      for (int r = 0; r < 4; ++r) x[4 * u + r] = key0 + 16 * u + 4 * grp + r < n ? s[r] * k2[u] : -INFINITY;
+      for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[rt][4 * u + r] = key0 + 16 * u + 4 * grp + r < n ? s[rt][r] * k2[u] : -INFINITY;
     }
-    bf16x8_t pl[NP];
-    softmax(x, vs, pl);
+    bf16x8_t pl[RT][NP];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) softmax(rt, x[rt], vs, pl[rt]);
 #pragma unroll
     for (int i = 0; i < NT; ++i) {  // dim tile i: dims l16 * NT + i
       uint32_t w[8];
@@ -249,32 +262,41 @@ __global__ __launch_bounds__(NW * 64) void cache_attn_kernel(CacheAttnArgs a, Pa
       for (int j = 0; j < 8; ++j) w[j] = cur.v[j][i >> 2];
       const bf16x8_t vf = byte8(w, i & 3);
 #pragma unroll
-      for (int p = NP - 1; p >= 0; --p) o[i] = mfma_bf16(vf, pl[p], o[i]);
+      for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int p = NP - 1; p >= 0; --p) o[rt][i] = mfma_bf16(vf, pl[rt][p], o[rt][i]);
     }
   }
   // the call's own tokens
   for (int t = max(t0 + wave, ct + ((t0 + wave - ct) & (NW - 1))); t < t1; t += NW) {
     const int key0 = (t - ct) * 32;
-    float x[8];
+    float x[RT][8];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const long long at = b * a.sb + (long long)min(key0 + 16 * u + l16, S - 1) * a.st + g * a.sh;
-      f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+      f32x4_t s[RT];
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) s[rt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         bf16x8_t kf[NP];
         load8<F32>(a.sk, at + kdim<HD>(ks, grp), kf);
 #pragma unroll
-        for (int i = NP - 1; i >= 0; --i)
+        for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-          for (int p = NP - 1 - i; p >= 0; --p) s = mfma_bf16(kf[i], q[ks][p], s);
+          for (int i = NP - 1; i >= 0; --i)
+#pragma unroll
+            for (int p = NP - 1 - i; p >= 0; --p) s[rt] = mfma_bf16(kf[i], q[rt][ks][p], s[rt]);
       }
 #pragma unroll
-      for (int r = 0; r < 4; ++r) x[4 * u + r] = key0 + 16 * u + 4 * grp + r < S ? s[r] * sl2 : -INFINITY;
+      for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[rt][4 * u + r] = key0 + 16 * u + 4 * grp + r < S ? s[rt][r] * sl2 : -INFINITY;
     }
-    bf16x8_t pl[NP];
+    bf16x8_t pl[RT][NP];
     const float one[2] = {1.f, 1.f};
-    softmax(x, one, pl);
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) softmax(rt, x[rt], one, pl[rt]);
     long long va[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j)
@@ -288,27 +310,32 @@ __global__ __launch_bounds__(NW * 64) void cache_attn_kernel(CacheAttnArgs a, Pa
         y[j] = F32 ? ((const float*)a.sv)[va[j] + i] : bf16_to_f32(((const bf16_t*)a.sv)[va[j] + i]);
       planes<NP>(y, vf);
 #pragma unroll
-      for (int k = NP - 1; k >= 0; --k)
+      for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-        for (int p = NP - 1 - k; p >= 0; --p) o[i] = mfma_bf16(vf[k], pl[p], o[i]);
+        for (int k = NP - 1; k >= 0; --k)
+#pragma unroll
+          for (int p = NP - 1 - k; p >= 0; --p) o[rt][i] = mfma_bf16(vf[k], pl[rt][p], o[rt][i]);
     }
   }
 
   // join the waves: o[t][r] is dim (4 grp + r) NT + t of row l16
-  l += __shfl_xor(l, 16, 64);
-  l += __shfl_xor(l, 32, 64);
 #pragma unroll
-  for (int r = 0; r < 4; ++r)
+  for (int rt = 0; rt < RT; ++rt) {
+    l[rt] += __shfl_xor(l[rt], 16, 64);
+    l[rt] += __shfl_xor(l[rt], 32, 64);
 #pragma unroll
-    for (int t = 0; t < NT; ++t) so[wave][l16][(4 * grp + r) * NT + t] = o[t][r];
-  if (grp == 0) {
-    sml[wave][l16][0] = m;
-    sml[wave][l16][1] = l;
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) so[wave][16 * rt + l16][(4 * grp + r) * NT + t] = o[rt][t][r];
+    if (grp == 0) {
+      sml[wave][16 * rt + l16][0] = m[rt];
+      sml[wave][16 * rt + l16][1] = l[rt];
+    }
   }
   __syncthreads();
   constexpr int Q4 = HD / 4;
-  for (int i = tid; i < 16 * Q4; i += NW * 64) {
-    const int r = i / Q4, d = i % Q4 * 4, rr = chunk * 16 + r;
+  for (int i = tid; i < 16 * RT * Q4; i += NW * 64) {
+    const int r = i / Q4, d = i % Q4 * 4, rr = chunk * 16 * RT + r;
     if (rr >= R) break;
     float mm = sml[0][r][0];
 #pragma unroll
@@ -964,6 +991,7 @@ __global__ __launch_bounds__(WW * 64, 2) void cache_weight_kernel(CacheAttnArgs 
 
 struct Plan {
   bool tile;
+  int rt;  // few rows: 16 rt rows of a block
   int chunks, nsplit;
   size_t o_off, ml_off, lse_off, bytes;
 };
@@ -972,21 +1000,25 @@ size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 Plan plan_of(const CacheAttnArgs& a) {
   Plan p;
   const long long R = (long long)(a.nq / a.c.nkv) * a.rows, heads = (long long)a.batch * a.c.nkv;
-  // 128-row blocks once the work is worth their start (13 us at 256 dims, 7 at 128): rows in
-  // chunks of 16 times keys.  us, 16-row blocks / 128-row blocks: 400 rows of 256 dims over 866 keys,
-  // 8 sequences (1.7e5) 17 / 31, 16 (3.5e5) 32 / 34, 24 (5.2e5) 46 / 40, 64 103 / 42; 400 rows of 128
-  // dims over 2148 keys, 8 heads (4.3e5) 17 / 24, 16 (8.6e5) 33 / 28; 64 rows of 64 dims over 320
-  // keys, 128 heads (1.6e5) 9 / 14, 512 (6.6e5) 31 / 17.  Up to 32 rows they never win: 512 heads of
-  // 128 dims over 1024 keys, 32 rows 46.9 / 47.5, 48 rows 68 / 48.
-  const long long work = (R + 15) / 16 * heads * (a.c.cap + a.n_self);
-  p.tile = !a.f32 && R > 32 && work >= 500000;
-  const int rows = p.tile ? 128 : 16;
+  // Rows of a block, by how often its blocks fill the 256 CUs (one of them a CU): 32 rows take 1.4 times
+  // as long as 16 and half the blocks, 128 some 1.8 times as long as 32, and their start and the sum
+  // of their key ranges cost 9 us and more.  us with 16 / 32 / 128 rows:
+  //   400 rows of 256 dims over 866 keys, 8 sequences 17 / 24 / 31, 16 32 / 25 / 33, 24 47 / 47 / 38
+  //   400 rows of 128 dims over 2148 keys, 8 heads 17 / 21 / 23, 16 33 / 23 / 27, 24 48 / 41 / 34
+  //   64 rows of 64 dims over 320 keys, 128 heads 9.4 / 7.3 / 13, 256 18 / 12 / 9
+  //   128 heads of 128 dims over 4096 keys, 32 rows 41 / 30 / 47, 64 77 / 44 / 48
+  //   512 heads of 128 dims over 1024 keys, 32 rows 47 / 30 / 45, 33 66 / 54 / 45
+  //   16 heads of 128 dims over 8192 keys, 64 rows 22 / 19 / 21, 128 33 / 26 / 24
+  const long long b16 = (R + 15) / 16 * heads, b32 = (R + 31) / 32 * heads, keys_all = (long long)a.c.cap + a.n_self;
+  p.tile = !a.f32 && R > 32 && (b32 > 256 || (R >= 96 && b32 * keys_all >= 500000));
+  p.rt = !a.f32 && R > 16 && (5 * ((b16 + 255) / 256) > 7 * ((b32 + 255) / 256) || (b16 > 128 && keys_all >= 4096)) ? 2 : 1;
+  const int rows = p.tile ? 128 : 16 * p.rt;
   p.chunks = (int)((R + rows - 1) / rows);
   const long long blocks = p.chunks * heads;
   // Key ranges up to one block a CU.  128 rows: a stage at least.  16 rows: a tile a wave, but no
   // ranges where a block has two for each of its waves (16 heads of 128 dims over 512 keys 7.3
   // us so, 9.2 with two ranges; over 1024 11.0 and 9.3).
-  const int w = few_row_waves(a.c.hd, a.f32), keys = !p.tile ? 32 * w : a.c.hd < 256 ? 128 : 64;
+  const int w = few_row_waves(a.c.hd, a.f32, p.rt), keys = !p.tile ? 32 * w : a.c.hd < 256 ? 128 : 64;
   long long steps = (a.c.cap + keys - 1) / keys + (a.n_self + keys - 1) / keys;
   if (!p.tile) {
     const long long tiles = (a.c.cap + 31) / 32 + (a.n_self + 31) / 32;
@@ -1012,8 +1044,13 @@ hipError_t launch_hd(const CacheAttnArgs& a, hipStream_t s) {
   if constexpr (!F32) {
     if (p.tile) hipLaunchKernelGGL((cache_attn_tile_kernel<HD>), dim3((unsigned)blocks), dim3(512), 0, s, a, part, p.chunks);
   }
-  if (!p.tile)
-    hipLaunchKernelGGL((cache_attn_kernel<HD, F32>), dim3((unsigned)blocks), dim3(few_row_waves(HD, F32) * 64), 0, s, a, part,
+  if constexpr (!F32) {
+    if (!p.tile && p.rt == 2)
+      hipLaunchKernelGGL((cache_attn_kernel<HD, F32, 2>), dim3((unsigned)blocks), dim3(few_row_waves(HD, F32, 2) * 64), 0, s, a,
+                         part, p.chunks);
+  }
+  if (!p.tile && p.rt == 1)
+    hipLaunchKernelGGL((cache_attn_kernel<HD, F32, 1>), dim3((unsigned)blocks), dim3(few_row_waves(HD, F32) * 64), 0, s, a, part,
                        p.chunks);
   if (p.nsplit > 1) hipLaunchKernelGGL(cache_join_kernel<F32>, dim3((unsigned)joins), dim3(64), 0, s, a, part);
   if (a.track) {

@@ -210,6 +210,18 @@ ATTEND = [
     (256, 8, 1, 16, 5001, [4977, 65, 64], 41, 0, "bf16"),
     (64, 12, 3, 16, 1400, [1400, 1399, 5], 100, 7, "bf16"),
     (32, 4, 4, 32, 3200, [3200, 1, 1025], 128, 8, "bf16"),
+    # and more keys than blocks of 32 rows would walk
+    (256, 8, 1, 64, 7800, [7800, 0, 1999], 50, 50, "bf16"),
+    (256, 8, 1, 16, 9201, [9177, 65, 64], 41, 0, "bf16"),
+    (64, 12, 3, 16, 2601, [2601, 2599, 5], 100, 7, "bf16"),
+    (32, 4, 4, 32, 6300, [6300, 1, 1025], 128, 8, "bf16"),
+    # blocks of 32 rows: every head dim, an odd last block, two key ranges
+    (256, 8, 1, 128, 300, [300, 0, 77], 120, 33, "bf16"),
+    (128, 16, 4, 32, 333, [333, 31, 200], 60, 0, "bf16"),
+    (64, 12, 3, 64, 301, [301, 299, 1], 85, 85, "bf16"),
+    (32, 6, 3, 16, 129, [129, 0, 128], 130, 7, "bf16"),
+    (128, 4, 4, 64, 4100, [4100, 0, 4099], 100, 1, "bf16"),
+    (64, 8, 8, 16, 4097, [4097, 33, 2000], 65, 16, "bf16"),
 ]
 
 
