@@ -535,7 +535,9 @@ __global__ __launch_bounds__(512, 2) void cache_attn_tile_kernel(CacheAttnArgs a
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
   float m = -INFINITY, l = 0.f;
-  const float sl2 = a.scale * kLog2e;
+  // masked scores are -inf before the scale multiplies them: a scale of 0 is the smallest positive number
+  // here (-inf * 0 is NaN), which still rounds every finite score to 2^-21 and less
+  const float sl2 = fmaxf(a.scale * kLog2e, 0x1p-149f);
 
   // LDS addresses of this lane's first fragments; the others' differ in bits that the swizzle
   // leaves alone or only flips
