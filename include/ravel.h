@@ -387,7 +387,9 @@ ravel_status ravel_profile_step(ravel_buffer* buf, const void* fop_tokens, float
  * device; the struct may be copied and is read during the call only.  k and v must be 16-byte
  * aligned.  The calls are enqueued on `stream` and allocate nothing; they may be captured into a
  * graph, and read lengths, indices and positions from device memory when they run.  Calls that
- * write one sequence must be ordered with every other call on it.
+ * write one sequence must be ordered with every other call on it.  Codes, scales and weights behind
+ * a sequence's length are no part of any result and need not be initialised (unless an append skips
+ * them: tokens between the length and its pos become the sequence's as they are).
  *
  *   seq  [batch] device int32: the sequence of each batch row; NULL: row b is sequence b.  A row
  *        whose index is outside 0..n_seq-1 (say -1, for padding) takes no part in the call.

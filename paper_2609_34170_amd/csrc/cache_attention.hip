@@ -469,7 +469,9 @@ __global__ __launch_bounds__(512, 2) void cache_attn_tile_kernel(CacheAttnArgs a
   // (a key range holds less than 2^31 bytes)
   const auto rk = buffer_of(kc + (long long)c0 * SK * HD, min(cn, (c1 - c0) * SK) * HD);
   const auto rv = buffer_of(vc + (long long)c0 * SK * HD, min(cn, (c1 - c0) * SK) * HD);
-  const auto rks = buffer_of(ksc + sblk, (c.nblk - sblk) * 4), rvs = buffer_of(vsc + sblk, (c.nblk - sblk) * 4);
+  // (blocks behind the last token give a scale of 0: what lies there need not be a number)
+  const int sbytes = max(((n - 1) >> c.shift) + 1 - sblk, 0) * 4;
+  const auto rks = buffer_of(ksc + sblk, sbytes), rvs = buffer_of(vsc + sblk, sbytes);
   // a thread's loads lie 8 KB apart: LR tokens, whole scale blocks or inside one
   constexpr int LR = 512 / CH;
   const int voff = CB < 8192 && tid >= CB / 16 ? 0x7FFFFFF0 : tid * 16;  // (past the end: nothing is read)
