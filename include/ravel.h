@@ -482,7 +482,10 @@ ravel_status ravel_cache_attention(const ravel_cache* cache, const ravel_cache_q
  *   beyond the tokens kept (all of them for a row without a sequence).
  * workspace: ravel_cache_evict_workspace() bytes, 256-byte aligned, of this call alone until it has
  * run.  A destination that an earlier row names already is not written again.
- * Errors: E_INVALID (null pointer, no weights, workspace too small), E_SHAPE (sizes, first > keep). */
+ * kept and the workspace lie in neither cache, seq and into_seq not in the cache that is written
+ * (its len, say), kept or the workspace.
+ * Errors: E_INVALID (null pointer, no weights, workspace too small, shared memory), E_SHAPE (sizes,
+ * first > keep). */
 ravel_status ravel_cache_evict_workspace(const ravel_cache* cache, int32_t batch, int32_t keep, int64_t* bytes);
 ravel_status ravel_cache_evict(const ravel_cache* cache, int32_t batch, const int32_t* seq, int32_t keep, int32_t first,
                                const ravel_cache* into, const int32_t* into_seq, int32_t* kept, void* workspace,

@@ -18,6 +18,18 @@ bool overlap(const void* a, size_t na, const void* b, size_t nb) {
   return a && b && (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
 }
 
+struct Piece {
+  const void* p;
+  size_t bytes;
+};
+bool overlap(const Piece& a, const Piece& b) { return overlap(a.p, a.bytes, b.p, b.bytes); }
+std::array<Piece, 6> pieces(const ravel_cache* x) {  // a cache's memory
+  const size_t heads = (size_t)x->n_seq * x->n_kv_heads, tokens = heads * x->capacity;
+  const size_t scales = heads * ((x->capacity + x->block - 1) / x->block) * 4;
+  return {{{x->k, tokens * x->head_dim}, {x->v, tokens * x->head_dim}, {x->k_scale, scales},
+           {x->v_scale, scales}, {x->len, (size_t)x->n_seq * 4}, {x->weight, tokens * 4}}};
+}
+
 #define CACHE_TRY(expr)              \
   do {                               \
     const ravel_status s_ = (expr);  \
@@ -213,19 +225,9 @@ ravel_status ravel_cache_evict(const ravel_cache* c, int32_t batch, const int32_
     if (into->n_kv_heads != c->n_kv_heads || into->head_dim != c->head_dim || into->block != c->block)
       return bad_shape(me, "both caches must have the same KV heads, head_dim and block");
     if (into->capacity < (keep < c->capacity ? keep : c->capacity)) return bad_shape(me, "the destination holds fewer than keep tokens");
-    struct Piece {
-      const void* p;
-      size_t bytes;
-    };
-    const auto pieces = [](const ravel_cache* x) {
-      const size_t heads = (size_t)x->n_seq * x->n_kv_heads, tokens = heads * x->capacity;
-      const size_t scales = heads * ((x->capacity + x->block - 1) / x->block) * 4;
-      return std::array<Piece, 6>{{{x->k, tokens * x->head_dim}, {x->v, tokens * x->head_dim}, {x->k_scale, scales},
-                                   {x->v_scale, scales}, {x->len, (size_t)x->n_seq * 4}, {x->weight, tokens * 4}}};
-    };
     for (const Piece& p : pieces(c))
       for (const Piece& q : pieces(into))
-        if (overlap(p.p, p.bytes, q.p, q.bytes)) return bad(me, "the caches share memory");
+        if (overlap(p, q)) return bad(me, "the caches share memory");
   } else if (into_seq) {
     return bad(me, "into_seq without a destination");
   }
@@ -235,6 +237,20 @@ ravel_status ravel_cache_evict(const ravel_cache* c, int32_t batch, const int32_
   if (!workspace || workspace_bytes < 0 || (size_t)workspace_bytes < need)
     return bad(me, "needs a workspace of " + std::to_string(need) + " bytes");
   if (!aligned(workspace, 256)) return bad(me, "the workspace must be 256-byte aligned");
+  // The selection writes kept and the workspace, the moves read both back; the moves write the
+  // destination while other blocks still read their indices and the first cache.
+  const size_t ni = (size_t)batch * 4;
+  const Piece ids{seq, ni}, into_ids{into_seq, ni}, ks{kept, (size_t)batch * c->n_kv_heads * keep * 4}, ws{workspace, need};
+  if (overlap(ks, ws)) return bad(me, "kept must not lie in the workspace");
+  if (overlap(ids, ks) || overlap(ids, ws) || overlap(into_ids, ks) || overlap(into_ids, ws))
+    return bad(me, "seq and into_seq must not lie in kept or the workspace");
+  for (const ravel_cache* x : {c, into ? into : c})
+    for (const Piece& p : pieces(x)) {
+      if (overlap(ks, p)) return bad(me, "kept must not lie in a cache");
+      if (overlap(ws, p)) return bad(me, "the workspace must not lie in a cache");
+      if (x == (into ? into : c) && (overlap(ids, p) || overlap(into_ids, p)))
+        return bad(me, "seq and into_seq must not lie in the cache that is written");
+    }
   CacheEvictArgs a;
   a.src = view(c);
   a.dst = view(into ? into : c);
