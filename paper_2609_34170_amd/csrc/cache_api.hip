@@ -1,7 +1,7 @@
 // C ABI of the 8-bit key/value cache: argument checks, then the launches of cache.hip and
 // cache_attention.hip.
+#include <algorithm>
 #include <array>
-#include <climits>
 #include <cmath>
 
 #include "cache.h"
@@ -67,11 +67,17 @@ ravel_status check_dtype(const char* call, int32_t dtype) {
   return dtype == RAVEL_F32 || dtype == RAVEL_BF16 ? RAVEL_OK : bad(call, "dtype must be RAVEL_F32 or RAVEL_BF16");
 }
 
-// vectors of 16 bytes wherever an index and a head lead
-ravel_status check_strides(const char* call, int32_t dtype, std::initializer_list<int64_t> st) {
+// vectors of 16 bytes wherever an index and a head lead; (stride, extent) of each dimension
+struct Dim {
+  int64_t stride, extent;
+};
+ravel_status check_strides(const char* call, int32_t dtype, std::initializer_list<Dim> dims) {
   const int64_t v = dtype == RAVEL_F32 ? 4 : 8;
-  for (int64_t x : st)
-    if (x < 0 || x % v || x > INT64_MAX / (1ll << 33)) return bad_shape(call, "strides must be multiples of 16 bytes, not negative");
+  for (const Dim& d : dims) {
+    if (d.stride < 0 || d.stride % v) return bad_shape(call, "strides must be multiples of 16 bytes, not negative");
+    // the sum of three such offsets, in bytes, stays within 64 bits
+    if (d.stride > (1ll << 59) / std::max<int64_t>(d.extent, 1)) return bad_shape(call, "strides reach past 64-bit addresses");
+  }
   return RAVEL_OK;
 }
 
@@ -146,7 +152,7 @@ ravel_status ravel_cache_append(const ravel_cache* c, int32_t batch, const int32
   CACHE_TRY(check_batch(me, batch, seq));
   CACHE_TRY(check_dtype(me, dtype));
   if (n < 0 || n > c->capacity) return bad_shape(me, "n must be in 0..capacity");
-  CACHE_TRY(check_strides(me, dtype, {batch_stride, token_stride, head_stride}));
+  CACHE_TRY(check_strides(me, dtype, {{batch_stride, batch}, {token_stride, n}, {head_stride, c->n_kv_heads}}));
   if (!aligned(pos, 4) || !aligned(count, 4)) return bad(me, "pos and count must be 4-byte aligned");
   if (n > 0 && batch > 0 && (!k || !v)) return bad(me, "null keys or values");
   if (!aligned(k, 16) || !aligned(v, 16)) return bad(me, "keys and values must be 16-byte aligned");
@@ -188,8 +194,10 @@ ravel_status ravel_cache_attention(const ravel_cache* c, const ravel_cache_query
   if (q->n_self > 0 && (!q->self_k || !q->self_v)) return bad(me, "null own keys or values");
   for (const void* p : {q->q, q->self_k, q->self_v, (const void*)q->out})
     if (!aligned(p, 16)) return bad(me, "q, self_k, self_v and out must be 16-byte aligned");
-  for (const int64_t* st : {q->q_stride, q->self_stride, q->out_stride})
-    CACHE_TRY(check_strides(me, q->dtype, {st[0], st[1], st[2]}));
+  for (const int64_t* st : {q->q_stride, q->out_stride})
+    CACHE_TRY(check_strides(me, q->dtype, {{st[0], q->batch}, {st[1], q->rows}, {st[2], q->n_q_heads}}));
+  const int64_t* ss = q->self_stride;
+  CACHE_TRY(check_strides(me, q->dtype, {{ss[0], q->batch}, {ss[1], q->n_self}, {ss[2], c->n_kv_heads}}));
   if (q->track && !c->weight) return bad(me, "track needs a cache with weights");
   const CacheAttnArgs a = attn_args(c, q);
   const size_t need = cache_attn_workspace(a);
