@@ -370,7 +370,7 @@ struct ravel_buffer {
   void* qws = nullptr;           // attention workspace
   void* qevict_ws = nullptr;     // eviction workspace and its indices
   int* qkept = nullptr;
-  void* qstage = nullptr;        // a context's keys and values given in host memory
+  void* qstage = nullptr;        // a context's keys and values that the append kernel cannot read where they are
   hipEvent_t stage_free = nullptr;
   // activations
   float* x = nullptr;
@@ -1150,9 +1150,11 @@ ravel_status apply_publishes(ravel_buffer* b, hipStream_t s) {
   return RAVEL_OK;
 }
 
-bool on_device(const void* p) {
+// Whether the append kernel can read p as it lies: memory of `device`, in vectors of 16 bytes.
+bool readable(const void* p, int device) {
+  if ((uintptr_t)p % 16) return false;
   hipPointerAttribute_t at;
-  if (hipPointerGetAttributes(&at, p) == hipSuccess) return at.type == hipMemoryTypeDevice;
+  if (hipPointerGetAttributes(&at, p) == hipSuccess) return at.type == hipMemoryTypeDevice && at.device == device;
   (void)hipGetLastError();  // plain host memory
   return false;
 }
@@ -1161,9 +1163,9 @@ bool on_device(const void* p) {
 ravel_status store_context(ravel_buffer* b, int env, const void* k, const void* v, hipStream_t producer) {
   const ravel_config& c = b->m->cfg;
   const size_t bytes = b->ctx_elems * b->m->elt;
-  const bool staged = !on_device(k) || !on_device(v);
+  const bool staged = !readable(k, b->m->device) || !readable(v, b->m->device);
   if (staged) {
-    // the staging rows are free once the last context given in host memory is stored
+    // the staging rows are free once the last context that went through them is stored
     HIP_TRY(hipStreamWaitEvent(producer, b->stage_free, 0));
     HIP_TRY(hipMemcpyAsync(b->qstage, k, bytes, hipMemcpyDefault, producer));
     HIP_TRY(hipMemcpyAsync((char*)b->qstage + bytes, v, bytes, hipMemcpyDefault, producer));
@@ -2571,8 +2573,6 @@ ravel_status ravel_set_context(ravel_buffer* b, int32_t env, const void* k, cons
   if ((k == nullptr) != (v == nullptr)) return fail(RAVEL_E_INVALID, "k and v must both be given or both NULL");
   if (env == -1 && !k) return fail(RAVEL_E_INVALID, "env = -1 needs k and v ([B, L, P, n_kv, hd])");
   if (b->quant_block && !k) return fail(RAVEL_E_STATE, "quantized contexts need k and v");
-  if (b->quant_block && ((uintptr_t)k % 16 || (uintptr_t)v % 16))
-    return fail(RAVEL_E_INVALID, "quantized contexts: k and v must be 16-byte aligned");
   hipStream_t ps = (hipStream_t)producer;
   std::lock_guard<std::mutex> lk(b->mu);
   const int e0 = env < 0 ? 0 : env, e1 = env < 0 ? b->B : env + 1;
