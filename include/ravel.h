@@ -363,7 +363,9 @@ ravel_status ravel_train_loss(ravel_buffer* buf, const float* target, const floa
  * record "phase/<index>/<phase class>" per phase in launch order; neither kind
  * is an additional launch.  Launches whose row count is decided on the device
  * (the modulation GEMMs run on the rows of distinct offset conditionings,
- * class "gemm_rows") carry bytes = flops = 0.  On input *n is the
+ * class "gemm_rows") carry bytes = flops = 0.  Contexts in 8 bits count the
+ * tokens that they hold: "cache_attn", "cache_join" (the join of its key ranges)
+ * and, while tracking, "cache_weight".  On input *n is the
  * capacity; on output the number of records. */
 typedef struct {
   char name[48];

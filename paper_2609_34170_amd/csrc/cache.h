@@ -61,7 +61,10 @@ struct CacheAttnArgs {
   void* ws;  // cache_attn_workspace() bytes, 16-byte aligned
 };
 size_t cache_attn_workspace(const CacheAttnArgs& a);  // c.nkv, hd, cap and the sizes of the call are read
-hipError_t launch_cache_attention(const CacheAttnArgs& a, hipStream_t s);
+int cache_attn_ranges(const CacheAttnArgs& a);            // key ranges, joined by a launch of their own where there are several
+// A call's launches: the attention, the join of its key ranges (if there are several), the weights (track).
+enum { CACHE_ATTEND = 1, CACHE_JOIN = 2, CACHE_WEIGHTS = 4, CACHE_ALL = 7 };
+hipError_t launch_cache_attention(const CacheAttnArgs& a, hipStream_t s, int launches = CACHE_ALL);
 
 struct CacheEvictArgs {
   CacheView src, dst;  // dst the same as src: in place

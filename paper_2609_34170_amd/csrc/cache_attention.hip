@@ -1038,26 +1038,29 @@ Plan plan_of(const CacheAttnArgs& a) {
 }
 
 template <int HD, bool F32>
-hipError_t launch_hd(const CacheAttnArgs& a, hipStream_t s) {
+hipError_t launch_hd(const CacheAttnArgs& a, hipStream_t s, int launches) {
   const Plan p = plan_of(a);
   const long long heads = (long long)a.batch * a.c.nkv, R = (long long)(a.nq / a.c.nkv) * a.rows;
   char* ws = (char*)a.ws;
   const Part part{(float*)(ws + p.o_off), (float*)(ws + p.ml_off), a.track ? (float*)(ws + p.lse_off) : nullptr, p.nsplit};
   const long long blocks = p.chunks * heads * p.nsplit, joins = (heads * R * (HD / 4) + 63) / 64;
   if (blocks > 0x7FFFFFFF || joins > 0x7FFFFFFF || (a.track && heads * ((a.c.cap + 63) / 64) > 0x7FFFFFFF)) return hipErrorInvalidValue;
-  if constexpr (!F32) {
-    if (p.tile) hipLaunchKernelGGL((cache_attn_tile_kernel<HD>), dim3((unsigned)blocks), dim3(512), 0, s, a, part, p.chunks);
+  if (launches & CACHE_ATTEND) {
+    if constexpr (!F32) {
+      if (p.tile) hipLaunchKernelGGL((cache_attn_tile_kernel<HD>), dim3((unsigned)blocks), dim3(512), 0, s, a, part, p.chunks);
+    }
+    if constexpr (!F32) {
+      if (!p.tile && p.rt == 2)
+        hipLaunchKernelGGL((cache_attn_kernel<HD, F32, 2>), dim3((unsigned)blocks), dim3(few_row_waves(HD, F32, 2) * 64), 0, s, a,
+                           part, p.chunks);
+    }
+    if (!p.tile && p.rt == 1)
+      hipLaunchKernelGGL((cache_attn_kernel<HD, F32, 1>), dim3((unsigned)blocks), dim3(few_row_waves(HD, F32) * 64), 0, s, a, part,
+                         p.chunks);
   }
-  if constexpr (!F32) {
-    if (!p.tile && p.rt == 2)
-      hipLaunchKernelGGL((cache_attn_kernel<HD, F32, 2>), dim3((unsigned)blocks), dim3(few_row_waves(HD, F32, 2) * 64), 0, s, a,
-                         part, p.chunks);
-  }
-  if (!p.tile && p.rt == 1)
-    hipLaunchKernelGGL((cache_attn_kernel<HD, F32, 1>), dim3((unsigned)blocks), dim3(few_row_waves(HD, F32) * 64), 0, s, a, part,
-                       p.chunks);
-  if (p.nsplit > 1) hipLaunchKernelGGL(cache_join_kernel<F32>, dim3((unsigned)joins), dim3(64), 0, s, a, part);
-  if (a.track) {
+  if ((launches & CACHE_JOIN) && p.nsplit > 1)
+    hipLaunchKernelGGL(cache_join_kernel<F32>, dim3((unsigned)joins), dim3(64), 0, s, a, part);
+  if ((launches & CACHE_WEIGHTS) && a.track) {
     // one wave where its rows are few, or its keys alone give every SIMD a wave
     const int rw = R <= 32 || heads * ((a.c.cap + 63) / 64) >= 1024 ? 1 : WW, bk = 64 * WW / rw;
     hipLaunchKernelGGL((cache_weight_kernel<HD, F32>), dim3((unsigned)(heads * ((a.c.cap + bk - 1) / bk))), dim3(WW * 64), 0, s, a,
@@ -1070,13 +1073,15 @@ hipError_t launch_hd(const CacheAttnArgs& a, hipStream_t s) {
 
 size_t cache_attn_workspace(const CacheAttnArgs& a) { return a.batch == 0 ? 0 : plan_of(a).bytes; }
 
-hipError_t launch_cache_attention(const CacheAttnArgs& a, hipStream_t s) {
+int cache_attn_ranges(const CacheAttnArgs& a) { return a.batch == 0 ? 1 : plan_of(a).nsplit; }
+
+hipError_t launch_cache_attention(const CacheAttnArgs& a, hipStream_t s, int launches) {
   if (a.batch == 0) return hipSuccess;
   switch (a.c.hd) {
-    case 32: return a.f32 ? launch_hd<32, true>(a, s) : launch_hd<32, false>(a, s);
-    case 64: return a.f32 ? launch_hd<64, true>(a, s) : launch_hd<64, false>(a, s);
-    case 128: return a.f32 ? launch_hd<128, true>(a, s) : launch_hd<128, false>(a, s);
-    case 256: return a.f32 ? launch_hd<256, true>(a, s) : launch_hd<256, false>(a, s);
+    case 32: return a.f32 ? launch_hd<32, true>(a, s, launches) : launch_hd<32, false>(a, s, launches);
+    case 64: return a.f32 ? launch_hd<64, true>(a, s, launches) : launch_hd<64, false>(a, s, launches);
+    case 128: return a.f32 ? launch_hd<128, true>(a, s, launches) : launch_hd<128, false>(a, s, launches);
+    case 256: return a.f32 ? launch_hd<256, true>(a, s, launches) : launch_hd<256, false>(a, s, launches);
     default: return hipErrorInvalidValue;
   }
 }

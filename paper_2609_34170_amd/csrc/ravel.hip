@@ -77,6 +77,7 @@ struct KernelRecorder {
     hipEvent_t a, b;
   };
   std::vector<Rec> recs;
+  std::vector<double> ctx_tokens;  // contexts in 8 bits: tokens that a layer's hold, over the envs
   void begin(const char* name, double bytes, double flops) {
     Rec r{name, bytes, flops, nullptr, nullptr};
     (void)hipEventCreate(&r.a);
@@ -613,13 +614,30 @@ CacheAttnArgs cache_attn_args(const ravel_buffer* b, int l) {
 }
 
 ravel_status run_cache_attn(ravel_buffer* b, hipStream_t s, KernelRecorder* rec, int l) {
+  const CacheAttnArgs a = cache_attn_args(b, l);
+  if (!rec) {
+    HIP_TRY(launch_cache_attention(a, s));
+    return RAVEL_OK;
+  }
   const ravel_config& c = b->m->cfg;
-  const double elt = (double)b->m->elt, row = (double)c.n_kv_heads * c.head_dim, H = c.horizon;
-  const double bytes = b->B * (H * c.n_q_heads * c.head_dim * 2 * elt + (c.prefix_len + H * elt) * row * 2);
-  const double flops = 4.0 * b->B * c.n_q_heads * H * (c.prefix_len + H) * c.head_dim;
-  if (rec) rec->begin("cache_attn", bytes, flops);
-  HIP_TRY(launch_cache_attention(cache_attn_args(b, l), s));
-  if (rec) rec->end();
+  const double elt = (double)b->m->elt, row = (double)c.n_kv_heads * c.head_dim, H = c.horizon, tokens = rec->ctx_tokens[l];
+  const double rows = b->B * H * c.n_q_heads, scales = tokens / b->quant_block * c.n_kv_heads * 4;  // (a share of a block's)
+  rec->begin("cache_attn", rows * c.head_dim * 2 * elt + (tokens + b->B * H * elt) * row * 2 + 2 * scales,
+             4.0 * c.n_q_heads * H * (tokens + b->B * H) * c.head_dim);
+  HIP_TRY(launch_cache_attention(a, s, CACHE_ATTEND));
+  rec->end();
+  const int ranges = cache_attn_ranges(a);
+  if (ranges > 1) {
+    rec->begin("cache_join", rows * (ranges * (c.head_dim + 2.0) * 4 + c.head_dim * elt), 2.0 * rows * ranges * c.head_dim);
+    HIP_TRY(launch_cache_attention(a, s, CACHE_JOIN));
+    rec->end();
+  }
+  if (a.track) {  // keys' codes, rows, their sums, weights there and back
+    rec->begin("cache_weight", tokens * row + scales + rows * (c.head_dim * elt + 4) + 8 * tokens * c.n_kv_heads,
+               2.0 * c.n_q_heads * H * tokens * c.head_dim);
+    HIP_TRY(launch_cache_attention(a, s, CACHE_WEIGHTS));
+    rec->end();
+  }
   return RAVEL_OK;
 }
 
@@ -3186,6 +3204,15 @@ ravel_status ravel_profile_step(ravel_buffer* b, const void* fop, float* action,
   if (b->relative) return fail(RAVEL_E_STATE, "profiling covers absolute actions only");
   KernelRecorder rec;
   rec.stream = s;
+  if (b->quant_block) {  // an eviction leaves the lengths on the device
+    const int L = m->cfg.layers;
+    std::vector<int> len(b->qc.n_seq);
+    HIP_TRY(hipStreamSynchronize(s));
+    HIP_TRY(hipMemcpy(len.data(), b->qc.len, len.size() * 4, hipMemcpyDeviceToHost));
+    rec.ctx_tokens.assign(L, 0.0);
+    for (int e = 0; e < b->B; ++e)
+      for (int l = 0; l < L; ++l) rec.ctx_tokens[l] += len[((size_t)b->active[e] * b->B + e) * L + l];
+  }
   ravel_status st = b->persistent ? enqueue_persistent_step(b, fop, nullptr, action, s, &rec)
                                   : enqueue_step(b, fop, nullptr, action, s, &rec);
   b->t_host += 1;
