@@ -438,8 +438,7 @@ ravel_status ravel_cache_append(const ravel_cache* cache, int32_t batch, const i
  * products are as good as 32 bits.  A row that sees nothing (len 0 and no own tokens, or no
  * sequence) is 0.  With track, every cached token's softmax weights, summed over the rows and the
  * query heads of its KV head, are added to the cache's accumulated weight (batch rows that name one
- * sequence are added in row order).  out shares no element with the inputs; scale is finite and not
- * negative.
+ * sequence are added in row order).  out shares no element with the inputs; scale is in 0..2^100.
  * Strides in elements, (b, row or token, head); 16-byte aligned vectors (multiples of 8 elements, or
  * 4 in 32 bits).  workspace: ravel_cache_attention_workspace() bytes, 256-byte aligned, of this call
  * alone until it has run (NULL when that is 0). */

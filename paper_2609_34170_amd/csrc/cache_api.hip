@@ -2,7 +2,6 @@
 // cache_attention.hip.
 #include <algorithm>
 #include <array>
-#include <cmath>
 
 #include "cache.h"
 
@@ -110,7 +109,8 @@ ravel_status check_query_sizes(const char* call, const ravel_cache* c, const rav
   CACHE_TRY(check_dtype(call, q->dtype));
   CACHE_TRY(check_batch(call, q->batch, nullptr));
   if (q->reserved) return bad(call, "reserved must be 0");
-  if (!(q->scale >= 0.f && q->scale < INFINITY)) return bad(call, "scale must be finite and not negative");
+  // (times log2 e and a block's scale it has to stay finite: 0 times infinity is not 0)
+  if (!(q->scale >= 0.f && q->scale <= 0x1p100f)) return bad(call, "scale must be in 0..2^100");
   if (q->n_q_heads < 1 || q->n_q_heads % c->n_kv_heads) return bad_shape(call, "n_q_heads must be a multiple of n_kv_heads");
   if (q->rows < 1 || q->rows > 1 << 20) return bad_shape(call, "rows must be in 1..2^20");
   if (q->n_self < 0 || q->n_self > 1 << 20) return bad_shape(call, "n_self must be in 0..2^20");
