@@ -422,7 +422,7 @@ typedef struct {
  *   of 8, or 4 in 32 bits).
  * A block that also holds older tokens keeps its scale, or, where the new tokens need a larger one,
  * has its older codes rounded to that.  Infinities become the largest code, NaN stays NaN; neither
- * counts for the scale.  Accumulated weights of the stored tokens start at 0.  seq, pos and count
+ * counts for the scale.  Magnitudes from 1.9375 * 2^127 on round to 2^128, which is infinite in 32 bits.  Accumulated weights of the stored tokens start at 0.  seq, pos and count
  * must not lie in the cache's len (but pos == len is taken as NULL).  A sequence that an earlier row names
  * already is not written again.
  * Errors: E_INVALID (null pointer, alignment, dtype, block), E_SHAPE (sizes, strides). */
@@ -434,9 +434,10 @@ ravel_status ravel_cache_append(const ravel_cache* cache, int32_t batch, const i
  * sequence's len tokens, then the n_self tokens whose keys and values come with the call in the
  * queries' dtype (every row sees all of both; query head j uses KV head j / (n_q_heads /
  * n_kv_heads)).  out = softmax(scale q k) v; scores, softmax and sums in 32 bits, in a bf16 call the
- * probabilities are rounded to bf16 for the second product and out at the end; in a 32-bit call
- * products are as good as 32 bits.  A row that sees nothing (len 0 and no own tokens, or no
- * sequence) is 0.  With track, every cached token's softmax weights, summed over the rows and the
+ * probabilities are rounded to bf16 for the second product (with many rows of up to 128 dims those of
+ * 32 keys a second time, where the next 32 raise the row's maximum far) and out at the end; in a 32-bit call products are
+ * as good as 32 bits.  Values of magnitudes up to 2^100 leave the sums finite.  A row that sees nothing
+ * (len 0 and no own tokens, or no sequence) is 0.  With track, every cached token's softmax weights, summed over the rows and the
  * query heads of its KV head, are added to the cache's accumulated weight (batch rows that name one
  * sequence are added in row order).  out shares no element with the inputs; scale is in 0..2^100.
  * Strides in elements, (b, row or token, head); 16-byte aligned vectors (multiples of 8 elements, or

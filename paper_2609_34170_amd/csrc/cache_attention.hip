@@ -372,9 +372,9 @@ __global__ __launch_bounds__(NW * 64) void cache_attn_kernel(CacheAttnArgs a, Pa
 // ---------------------------------------------------------------------------
 // Many rows: a block of 8 waves owns 128 rows of a (batch row, kv head) and walks stages of 64 (256
 // dims) or 128 keys; wave (rg, kh) takes the 32 rows of group rg over the half kh of every stage, and the two
-// waves of a group are joined at the end.  (One wave a group with twice the keys would need more
-// than the 256 registers that vector instructions reach; two also overlap one's exponentials with
-// the other's matrix instructions where a CU holds one block.)  On the 32 x 32 matrix
+// waves of a group are joined at the end: of a SIMD's two waves one's exponentials overlap the
+// other's matrix instructions.  (Not tried: one wave a SIMD with 64 rows and its outputs in
+// accumulation registers, which would halve the fragments' LDS reads.)  On the 32 x 32 matrix
 // instruction a lane owns one row of S^T and O^T, and 16 of each 32 keys (the other 16 the lane
 // 32 further on).
 //
@@ -389,7 +389,8 @@ __global__ __launch_bounds__(NW * 64) void cache_attn_kernel(CacheAttnArgs a, Pa
 //
 // 64 sequences of 400 rows of 256 dims over 866 keys (22.7 GFLOP) take 37 us, 0.62 PFLOP/s.  Of a
 // stage's 2.1 us the matrix instructions take 0.96 and the LDS traffic (K and V once a row group,
-// 2 HD bytes a key and wave) 1.1; start and end of a block take 6.
+// 2 HD bytes a key and wave) 1.1, one after the other more than beside each other; start and end of a
+// block take 6.  400 rows are 13 groups of 32: three of the fourth block's four are idle.
 // ---------------------------------------------------------------------------
 typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16_t;
 typedef __attribute__((__vector_size__(4 * sizeof(short)))) short s16x4_t;
@@ -1004,6 +1005,8 @@ size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 Plan plan_of(const CacheAttnArgs& a) {
   Plan p;
   const long long R = (long long)(a.nq / a.c.nkv) * a.rows, heads = (long long)a.batch * a.c.nkv;
+  // All by the capacity: the host does not know the lengths, and a long cache of short contents is
+  // planned as if it were full.
   // Rows of a block, by how often its blocks fill the 256 CUs (one of them a CU): 32 rows take 1.4 times
   // as long as 16 and half the blocks, 128 some 1.8 times as long as 32, and their start and the sum
   // of their key ranges cost 9 us and more.  us with 16 / 32 / 128 rows:
