@@ -435,11 +435,12 @@ ravel_status ravel_cache_append(const ravel_cache* cache, int32_t batch, const i
  * queries' dtype (every row sees all of both; query head j uses KV head j / (n_q_heads /
  * n_kv_heads)).  out = softmax(scale q k) v; scores, softmax and sums in 32 bits, in a bf16 call the
  * probabilities are rounded to bf16 for the second product (with many rows of up to 128 dims those of
- * 32 keys a second time, where the next 32 raise the row's maximum far) and out at the end; in a 32-bit call products are
- * as good as 32 bits.  Values of magnitudes up to 2^100 leave the sums finite.  A row that sees nothing
- * (len 0 and no own tokens, or no sequence) is 0.  With track, every cached token's softmax weights, summed over the rows and the
- * query heads of its KV head, are added to the cache's accumulated weight (batch rows that name one
- * sequence are added in row order).  out shares no element with the inputs; scale is in 0..2^100.
+ * 32 keys a second time, where the next 32 raise the row's maximum far) and out at the end; in a 32-bit
+ * call products are as good as 32 bits.  Values of magnitudes up to 2^90 leave the sums finite.  A row
+ * that sees nothing (len 0 and no own tokens, or no sequence) is 0.  With track, every cached token's
+ * softmax weights, summed over the rows and the query heads of its KV head, are added to the cache's
+ * accumulated weight (batch rows that name one sequence are added in row order).  out shares no element
+ * with the inputs; scale is in 0..2^100.
  * Strides in elements, (b, row or token, head); 16-byte aligned vectors (multiples of 8 elements, or
  * 4 in 32 bits).  workspace: ravel_cache_attention_workspace() bytes, 256-byte aligned, of this call
  * alone until it has run (NULL when that is 0). */
