@@ -529,6 +529,181 @@ ravel_status ravel_context_evict(ravel_buffer* buf, int32_t env, int32_t keep, i
  * quantized contexts, no applied context), E_INVALID (null pointer, env). */
 ravel_status ravel_context_cache(ravel_buffer* buf, int32_t env, ravel_cache* cache);
 
+/* -------------------------------------------------------------------------
+ * A layer's operators, with their gradients: gated residual and norm, cross attention, gated MLP.
+ *
+ * What an expert layer computes between its linear layers, as calls of their own, for programs that
+ * train on the loss above or run adapters of their own.  All memory is the caller's device memory on
+ * the current device; the structs are read during the call only.  The calls are enqueued on `stream`,
+ * allocate nothing and may be captured into a graph.  Elements of a tensor's innermost dimension are
+ * adjacent; other strides are in elements.  Tensors of RAVEL_BF16 and RAVEL_F32 are 16-byte aligned
+ * with strides of whole 16 bytes; vectors of 32-bit numbers that modulate rows likewise.  Inputs and
+ * outputs share no memory unless a call says so.  A workspace is ...workspace() bytes, 256-byte
+ * aligned, of this call alone until it has run (NULL when that is 0); the sizes come from the
+ * struct's sizes and from which of its pointers are NULL.  No result depends on the order in which
+ * blocks run: sums over rows are formed in one order, with no atomics.
+ *
+ * 1. Gated residual and norm.  For rows r of `width` elements:
+ *
+ *      F = f, or f / rms(f) * (1 + post) with post           rms(z) = sqrt(mean z^2 + eps)
+ *      t = x + alpha * gate * F                              (x without f)
+ *      y = t / rms(t) * (1 + scale) + shift
+ *
+ * x and t (x_out) have stream_dtype, f and y dtype; post, alpha, gate, scale and shift are 32-bit,
+ * each NULL where it is not there.  gate, scale and shift are vectors of `width` with stride 0, or
+ * hold `mods` rows, of which row r uses (r / group) % mods: rows of their own (group 1, mods =
+ * rows), one for each environment (group = its rows), one for each slot (group 1, mods = slots).
+ * The norm is that of t as x_out holds it.  Sums are in 32 bits: the squares of a row have to be
+ * finite there.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+  int32_t stream_dtype; /* of x, x_out and their gradients                    */
+  int32_t dtype;        /* of f, y and their gradients; RAVEL_BF16 with a
+                           RAVEL_BF16 stream                                  */
+  int32_t rows;         /* >= 0                                               */
+  int32_t width;        /* multiple of 8, <= 8192                             */
+  int32_t mods;         /* rows of gate, scale and shift, >= 1                */
+  int32_t group;        /* neighbouring rows that share one, >= 1             */
+  float eps;            /* > 0                                                */
+  int32_t reserved;     /* 0 */
+  const void* x;        /* [rows, width]                                      */
+  const void* f;        /* [rows, width], the block's output, or NULL         */
+  const float* post;    /* [width], or NULL: f is taken as it is              */
+  const float* alpha;   /* one number, or NULL: 1                             */
+  const float* gate;    /* or NULL: 1                                         */
+  const float* scale;   /* or NULL: 0                                         */
+  const float* shift;   /* or NULL: 0                                         */
+  void* x_out;          /* [rows, width]; NULL without f; may be x            */
+  void* y;              /* [rows, width], or NULL: only the residual          */
+  int64_t x_stride, f_stride, x_out_stride, y_stride, gate_stride, scale_stride, shift_stride;
+} ravel_norm;
+
+/* Errors: E_INVALID (null pointer, alignment, dtype, eps), E_SHAPE (sizes, strides). */
+ravel_status ravel_norm_residual(const ravel_norm* norm, void* stream);
+
+/* Its gradients: dy and d_out are those of y and x_out (either may be NULL: zero), every output may be
+ * NULL.  Of the struct above, x_out is read (x without f), f, post, alpha, gate and scale; x (with f),
+ * y and shift are not.  A vector's gradient is summed over all rows, a modulation row's over the rows
+ * that use it (0 if none does).  dx may be d_out. */
+typedef struct {
+  const void* dy;    /* [rows, width], dtype               */
+  const void* d_out; /* [rows, width], stream_dtype        */
+  void* dx;          /* [rows, width], stream_dtype        */
+  void* df;          /* [rows, width], dtype; needs f      */
+  float* dpost;      /* [width]; needs post                */
+  float* dalpha;     /* one number; needs alpha            */
+  float* dgate;      /* as gate; needs gate                */
+  float* dscale;     /* as scale; needs scale              */
+  float* dshift;     /* [mods, width], or [width] with stride 0 */
+  int64_t dy_stride, d_out_stride, dx_stride, df_stride;
+  int64_t dgate_stride, dscale_stride, dshift_stride; /* 0 where the vector's is (dshift: where it is summed over all rows) */
+  void* workspace;
+  int64_t workspace_bytes;
+} ravel_norm_grad;
+ravel_status ravel_norm_residual_grad_workspace(const ravel_norm* norm, const ravel_norm_grad* grad, int64_t* bytes);
+/* Errors: as above; E_INVALID also for a workspace too small or a gradient of what is not there. */
+ravel_status ravel_norm_residual_grad(const ravel_norm* norm, const ravel_norm_grad* grad, void* stream);
+
+/* 2. Cross attention: `rows` query rows per batch row over `keys` states of another length.
+ *
+ *      out = softmax(scale q k^T) v      over the first k_len[b] keys, for the first q_len[b] rows
+ *
+ * Query head j uses KV head j / (n_q_heads / n_kv_heads); every row sees all of its batch row's keys.
+ * Keys behind k_len and rows behind q_len take no part, whatever they hold: out is 0 for such rows and
+ * for all rows of a batch row without keys.  lse, if given, is the logarithm of each row's sum of
+ * exp(scale q k), -infinity for rows that are 0.  Scores, softmax and sums are in 32 bits; in bf16
+ * calls probabilities (and in the gradients the scores') are rounded to bf16 before they are
+ * multiplied, outputs at the end.  scale is in 0..2^100. */
+typedef struct {
+  int32_t dtype; /* RAVEL_F32 or RAVEL_BF16: q, k, v, out and their gradients */
+  int32_t batch;
+  int32_t n_q_heads;  /* at most 256                            */
+  int32_t n_kv_heads; /* divides n_q_heads                      */
+  int32_t head_dim;   /* 32, 64, 128 or 256                     */
+  int32_t rows;       /* 0 .. 2^20                              */
+  int32_t keys;       /* 0 .. 2^24                              */
+  float scale;        /* of the scores, e.g. 1 / sqrt(head_dim) */
+  const int32_t* q_len; /* [batch] or NULL: rows; outside 0..rows: the nearer bound */
+  const int32_t* k_len; /* [batch] or NULL: keys; likewise                          */
+  const void* q;
+  const void* k;
+  const void* v;
+  void* out;
+  float* lse;           /* [batch, n_q_heads, rows], or NULL (the gradients need it) */
+  int64_t q_stride[3];  /* (batch row, row or key, head); the latter two at most 2^22 bytes */
+  int64_t k_stride[3];
+  int64_t v_stride[3];
+  int64_t out_stride[3];
+  void* workspace;      /* of ravel_cross_attention */
+  int64_t workspace_bytes;
+} ravel_cross;
+
+ravel_status ravel_cross_attention_workspace(const ravel_cross* cross, int64_t* bytes);
+/* Errors: E_INVALID (null pointer, alignment, dtype, scale, workspace too small), E_SHAPE (sizes,
+ * strides, head counts). */
+ravel_status ravel_cross_attention(const ravel_cross* cross, void* stream);
+
+/* Its gradients from dout, with out and lse as the call above left them.  dk and dv sum over the query
+ * heads of their KV head; gradients of keys behind k_len and of rows behind q_len are 0.  dq may be
+ * NULL, and so may dk and dv together.  dout behind q_len is not read. */
+typedef struct {
+  const void* dout;
+  void* dq;
+  void* dk;
+  void* dv;
+  int64_t dout_stride[3];
+  int64_t dq_stride[3];
+  int64_t dk_stride[3];
+  int64_t dv_stride[3];
+  void* workspace;
+  int64_t workspace_bytes;
+} ravel_cross_grad;
+ravel_status ravel_cross_attention_grad_workspace(const ravel_cross* cross, const ravel_cross_grad* grad, int64_t* bytes);
+ravel_status ravel_cross_attention_grad(const ravel_cross* cross, const ravel_cross_grad* grad, void* stream);
+
+/* 3. Gated MLP, up to its hidden values: h = act(x Wg^T) * (x Wu^T), products and activation in 32 bits.
+ * gate and up, if given, receive x Wg^T and x Wu^T in dtype, for the gradients. */
+enum { RAVEL_GELU_TANH = 0, RAVEL_SILU = 1 };
+typedef struct {
+  int32_t dtype;    /* RAVEL_F32 or RAVEL_BF16, of all tensors      */
+  int32_t act;      /* RAVEL_GELU_TANH or RAVEL_SILU                */
+  int32_t rows;     /* >= 0                                         */
+  int32_t width;    /* of x: multiple of 8                          */
+  int32_t hidden;   /* of h: multiple of 8                          */
+  int32_t reserved; /* 0 */
+  const void* x;    /* [rows, width]                                */
+  const void* wg;   /* [hidden, width]                              */
+  const void* wu;   /* [hidden, width]                              */
+  void* h;          /* [rows, hidden]                               */
+  void* gate;       /* [rows, hidden], or NULL; with up             */
+  void* up;         /* [rows, hidden], or NULL; with gate           */
+  int64_t x_stride, w_stride, h_stride, gate_stride; /* of a row; w_stride of wg and wu, gate_stride of gate and up;
+                                                       at most 2^22 bytes */
+  void* workspace;  /* of ravel_gated_mlp */
+  int64_t workspace_bytes;
+} ravel_mlp;
+
+ravel_status ravel_gated_mlp_workspace(const ravel_mlp* mlp, int64_t* bytes);
+/* Errors: E_INVALID (null pointer, alignment, dtype, workspace too small), E_SHAPE (sizes, strides). */
+ravel_status ravel_gated_mlp(const ravel_mlp* mlp, void* stream);
+
+/* Its gradients from dh, with gate and up as the call above left them; h is not read.  dx may be NULL,
+ * and so may dwg and dwu together.  The gradients of gate and up, dh * up * act'(gate) and dh *
+ * act(gate), are rounded to dtype before they are multiplied. */
+typedef struct {
+  int32_t weight_dtype; /* of dwg and dwu: dtype or RAVEL_F32 */
+  int32_t reserved;     /* 0 */
+  const void* dh;       /* [rows, hidden], dtype  */
+  void* dx;             /* [rows, width], dtype   */
+  void* dwg;            /* [hidden, width]        */
+  void* dwu;            /* [hidden, width]        */
+  int64_t dh_stride, dx_stride, dw_stride; /* of a row; dw_stride of dwg and dwu */
+  void* workspace;
+  int64_t workspace_bytes;
+} ravel_mlp_grad;
+ravel_status ravel_gated_mlp_grad_workspace(const ravel_mlp* mlp, const ravel_mlp_grad* grad, int64_t* bytes);
+ravel_status ravel_gated_mlp_grad(const ravel_mlp* mlp, const ravel_mlp_grad* grad, void* stream);
+
 /* Message of the calling thread's last non-OK status ("" if none). */
 const char* ravel_last_error(void);
 

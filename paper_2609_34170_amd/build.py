@@ -20,7 +20,8 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libravel.so")
 SOURCES = ["gemm.hip", "gemm_tile.hip", "f32.hip", "attention.hip", "adapter.hip", "cache.hip", "cache_attention.hip",
-           "cache_api.hip", "elementwise.hip", "persistent.hip", "ravel.hip"]
+           "cache_api.hip", "norm_residual.hip", "cross_attention.hip", "gated_mlp.hip", "layer_api.hip", "elementwise.hip",
+           "persistent.hip", "ravel.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -1,0 +1,840 @@
+// Cross attention, out = softmax(scale q k^T) v over k_len keys, and its gradients.
+//
+// No row masks another's keys, so the query heads of a KV head are one row space: row r of (batch row, KV head) is
+// query row r / G of its G heads' head r % G, and every key and value tile is used by all of them.
+//
+// Rows are the columns of every result: s^T = K q^T leaves each lane 4 keys of one row, which is the operand of
+// o^T = V^T p^T as it stands (lds_tile.h), with V's fragments read along columns.  Probabilities never leave
+// registers, a row's maximum is one lane's business and two exchanges, and the running maximum and sum take one pass.
+//
+// The gradients are two passes over the same tiles, each writing what it owns, so that nothing is added by atomics:
+// rows against all keys (dq; also each row's D = sum dout out), then keys against all rows (dk, dv).  That forms
+// s and dout v^T twice, 7 products for 5.
+#include "gemm_epilogue.h"
+#include "layer.h"
+#include "lds_tile.h"
+
+namespace ravel {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+struct CrossArgs {
+  ravel_cross c;
+  ravel_cross_grad g;
+  int G, tiles, splits;  // query heads of a KV head; tiles of what the blocks own; ranges of what they walk
+  int padded;            // rows of stat (and of a partial) per (batch row, KV head)
+  float* part;           // partial results [split][batch][KV head][row or key][head_dim], or null
+  float* part_ml;        // forward: [split][batch][KV head][row][2], maximum (log2 units) and sum
+  float* stat;           // gradients: [2][batch][KV head][padded]: lse (log2 units), D
+  float* part2;          // dv's partials
+};
+
+RAVEL_DEV int live_len(const int* len, int b, int most) { return len ? min(max(len[b], 0), most) : most; }
+
+template <typename T> RAVEL_DEV void store_row4(T* p, f32x4_t v);
+template <> RAVEL_DEV void store_row4<float>(float* p, f32x4_t v) { *(f32x4_t*)p = v; }
+template <> RAVEL_DEV void store_row4<bf16_t>(bf16_t* p, f32x4_t v) {
+  *(u32x2_t*)p = u32x2_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+}
+RAVEL_DEV float dot16(f32x4_t a, f32x4_t b) { return (a[0] * b[0] + a[1] * b[1]) + (a[2] * b[2] + a[3] * b[3]); }
+RAVEL_DEV float dot16(bf16x8_t a, bf16x8_t b) {
+  const u32x4_t x = __builtin_bit_cast(u32x4_t, a), y = __builtin_bit_cast(u32x4_t, b);
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    s += __uint_as_float(x[i] << 16) * __uint_as_float(y[i] << 16) +
+         __uint_as_float(x[i] & 0xFFFF0000u) * __uint_as_float(y[i] & 0xFFFF0000u);
+  return s;
+}
+
+// Block `id` of a launch: its tile, KV head, batch row and range, neighbours sharing a batch row and head (and their XCD's
+// L2).
+struct Work {
+  int tile, h, b, split;
+};
+RAVEL_DEV Work work_of(const CrossArgs& a) {
+  int id = xcd_tile(blockIdx.x, gridDim.x);
+  Work w;
+  w.tile = id % a.tiles, id /= a.tiles;
+  w.split = id % a.splits, id /= a.splits;
+  w.h = id % a.c.n_kv_heads, w.b = id / a.c.n_kv_heads;
+  return w;
+}
+
+// K and V tiles (or q and dout): sizes and what a wave loads.
+template <typename T, int HD, int ROWS>
+struct Tiles {
+  static constexpr int RB = HD * sizeof(T), BYTES = ROWS * RB, SEGS = BYTES / 1024 / 4;  // segments per wave
+  static_assert(BYTES % 4096 == 0, "segments of four waves");
+};
+
+// Keys [first, first + TK) of one head into a tile; keys behind `end` (the last live key's end) are zeros.
+template <typename T, int HD, int TK>
+RAVEL_DEV void load_keys(const Segments<T, HD * sizeof(T)>& at, const T* head, const T* end, int stride, int first, char* tile, int wave) {
+  typedef Tiles<T, HD, TK> Z;
+  const unsigned row = __umul24(at.row, stride * (unsigned)sizeof(T));
+#pragma unroll
+  for (int i = 0; i < Z::SEGS; ++i) {
+    const int seg = wave * Z::SEGS + i;
+    const T* const from = head + (int64_t)(first + seg * at.ROWS) * stride;
+    load_segment(buffer_until((const char*)from, (const char*)end), tile, seg, row + at.byte_of(seg));
+  }
+}
+// Rows [first, first + TR) of a (batch row, KV head)'s row space; rows from `end` on are zeros.  head: row 0 of the first
+// query head.  Quotients by G through its reciprocal `inv` = ceil(2^23 / G), exact for what is below 2^23 / G.
+struct RowSpace {
+  int G, inv;
+};
+template <typename T, int HD, int TR>
+RAVEL_DEV void load_rows(const Segments<T, HD * sizeof(T)>& at, const T* head, int64_t row_stride, int head_stride, RowSpace sp, int first,
+                         int end, char* tile, int wave) {
+  typedef Tiles<T, HD, TR> Z;
+  const int i0 = first / sp.G, rest = first - i0 * sp.G;
+  const rsrc_t from = buffer_from(head + i0 * row_stride);
+#pragma unroll
+  for (int i = 0; i < Z::SEGS; ++i) {
+    const int seg = wave * Z::SEGS + i, r = seg * at.ROWS + at.row;
+    const unsigned x = rest + r, q = __umul24(x, sp.inv) >> 23, g = x - __umul24(q, sp.G);
+    const unsigned off = __umul24(q, (unsigned)row_stride * (unsigned)sizeof(T)) + __umul24(g, head_stride * (unsigned)sizeof(T));
+    load_segment(from, tile, seg, first + r < end ? off + at.byte_of(seg) : kOutside);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// forward
+// ---------------------------------------------------------------------------
+// Four waves: KW of them share 16 MI rows and split a tile's keys between them (few rows), 4 / KW groups of rows.
+template <typename T, int HD, int MI, int KW, int TK>
+__global__ __launch_bounds__(256, (4 * Tiles<T, HD, TK>::BYTES <= 65536 ? 2 : 1)) void cross_kernel(CrossArgs a) {
+  typedef Tiles<T, HD, TK> Z;
+  typedef Mat<T> M;
+  typedef typename M::frag frag;
+  constexpr int RB = Z::RB, STEPS = RB / 64, DF = HD / 16, TKW = TK / KW, NF = TKW / 16, NP = TKW / M::CK;
+  static_assert(TKW % M::CK == 0, "whole contraction steps");
+  constexpr int JOIN = KW > 1 ? 16 * MI * (HD + 2) * 4 : 0;  // bytes of a wave's results
+  static_assert(JOIN <= Z::BYTES, "a wave's results in a tile");
+  // Four arrays: reads along columns of one buffer wait for the loads in flight into another unless the compiler sees
+  // that they are apart.
+  __shared__ __attribute__((aligned(1024))) char k0[Z::BYTES], v0[Z::BYTES], k1[Z::BYTES], v1[Z::BYTES];
+
+  const int lane = threadIdx.x & 63, wave = wave_index(), l16 = lane & 15, grp = lane >> 4;
+  const int wk = wave % KW, wr = wave / KW;
+  const ravel_cross& c = a.c;
+  const Work w = work_of(a);
+  const int live = live_len(c.q_len, w.b, c.rows) * a.G, all = c.rows * a.G;
+  const int klen = live_len(c.k_len, w.b, c.keys);
+  const int row0 = w.tile * (16 * MI * (4 / KW)) + wr * 16 * MI;  // this wave's rows
+  const int ktiles = (klen + TK - 1) / TK, per = (ktiles + a.splits - 1) / a.splits;
+  const int t0 = min(ktiles, w.split * per), t1 = min(ktiles, t0 + per);
+
+  const T* const q = (const T*)c.q + w.b * c.q_stride[0] + (int64_t)w.h * a.G * c.q_stride[2];
+  const T* const k = (const T*)c.k + w.b * c.k_stride[0] + w.h * c.k_stride[2];
+  const T* const v = (const T*)c.v + w.b * c.v_stride[0] + w.h * c.v_stride[2];
+  const T *const k_end = k + (int64_t)(klen - 1) * (int)c.k_stride[1] + HD, *const v_end = v + (int64_t)(klen - 1) * (int)c.v_stride[1] + HD;
+  const Segments<T, RB> seg0(lane);
+  const auto issue = [&](int t, char* kt, char* vt) {
+    const auto seg = seg0.fresh();
+    load_keys<T, HD, TK>(seg, k, k_end, (int)c.k_stride[1], t * TK, kt, wave);
+    load_keys<T, HD, TK>(seg, v, v_end, (int)c.v_stride[1], t * TK, vt, wave);
+  };
+  if (t0 < t1) issue(t0, k0, v0);
+
+  frag qf[MI][STEPS];
+#pragma unroll
+  for (int i = 0; i < MI; ++i) {
+    const int r = row0 + i * 16 + l16, qr = r / a.G;
+    const T* const p = q + qr * c.q_stride[1] + (r - qr * a.G) * c.q_stride[2];
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) qf[i][s] = r < live && c.scale > 0.f ? *(const frag*)(p + (s * 4 + grp) * (16 / sizeof(T))) : frag{};
+  }
+  const float cs = c.scale > 0.f ? c.scale * kLog2e : 1.f;  // (a scale of 0: rows of zeros, so that -infinity stays)
+  f32x4_t o[MI][DF];
+  float m[MI], l[MI];
+#pragma unroll
+  for (int i = 0; i < MI; ++i) {
+    m[i] = -INFINITY, l[i] = 0.f;
+#pragma unroll
+    for (int d = 0; d < DF; ++d) o[i][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  const TileLane<T, RB> at0(lane);
+
+  // Keys that do not exist start from -infinity: the last tile's, whose rows are zeros.  (A select behind the products,
+  // under a branch, read them too early: the compiler leaves out wait states where a branch skips a few instructions
+  // between matrix instructions and their results' use.)
+  f32x4_t start[NF];
+#pragma unroll
+  for (int f = 0; f < NF; ++f) start[f] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  const auto step = [&](int t, const char* kc, const char* vc, char* kn, char* vn) {
+    tile_barrier<0>();
+    if (t + 1 < t1) issue(t + 1, kn, vn);
+    lds_char_t* const kt = (lds_char_t*)kc + wk * TKW * RB;
+    lds_char_t* const vt = (lds_char_t*)vc + wk * TKW * RB;
+    if (t == ktiles - 1) {
+      const int left = klen - t * TK - wk * TKW - grp * 4;
+#pragma unroll
+      for (int f = 0; f < NF; ++f)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) start[f][r] = f * 16 + r < left ? 0.f : -INFINITY;
+    }
+    auto at = at0.fresh();
+    f32x4_t s[MI][NF];
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int f = 0; f < NF; ++f) s[i][f] = start[f];
+#pragma unroll
+    for (int f = 0; f < NF; ++f)
+#pragma unroll
+      for (int st = 0; st < STEPS; ++st) {
+        const frag kf = at.along_row(kt, f, st);
+#pragma unroll
+        for (int i = 0; i < MI; ++i) s[i][f] = M::mma(kf, qf[i][st], s[i][f]);
+      }
+    frag pf[MI][NP];
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      float top = -INFINITY;
+#pragma unroll
+      for (int f = 0; f < NF; ++f) {
+        s[i][f] *= cs;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) top = fmaxf(top, s[i][f][r]);
+      }
+      top = fmaxf(top, __shfl_xor(top, 16, 64));
+      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      top = fmaxf(top, m[i]);
+      const float ref = top == -INFINITY ? 0.f : top, fall = __builtin_amdgcn_exp2f(m[i] - ref);
+      if (__any(top != m[i])) {
+        l[i] *= fall;
+#pragma unroll
+        for (int d = 0; d < DF; ++d) o[i][d] *= fall;
+      }
+      m[i] = top;
+#pragma unroll
+      for (int f = 0; f < NF; ++f)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          s[i][f][r] = __builtin_amdgcn_exp2f(s[i][f][r] - ref);
+          l[i] += s[i][f][r];
+        }
+#pragma unroll
+      for (int p = 0; p < NP; ++p) pf[i][p] = M::operand(&s[i][p * (NF / NP)]);
+    }
+    at = at0.fresh();
+#pragma unroll
+    for (int d = 0; d < DF; ++d)
+#pragma unroll
+      for (int p = 0; p < NP; ++p) {
+        const frag vf = at.along_col(vt, p, d);
+#pragma unroll
+        for (int i = 0; i < MI; ++i) o[i][d] = M::mma(vf, pf[i][p], o[i][d]);
+      }
+  };
+  for (int t = t0; t < t1; t += 2) {
+    step(t, k0, v0, k1, v1);
+    if (t + 1 < t1) step(t + 1, k1, v1, k0, v0);
+  }
+#pragma unroll
+  for (int i = 0; i < MI; ++i) {
+    l[i] += __shfl_xor(l[i], 16, 64);
+    l[i] += __shfl_xor(l[i], 32, 64);
+  }
+  if constexpr (KW > 1) {  // the waves that share rows: wave wk = 0 takes their sum
+    __syncthreads();
+    const auto results = [&](int w) { return (float*)(w == 0 ? k0 : w == 1 ? v0 : w == 2 ? k1 : v1); };
+    float* const mine = results(wave);
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      float* const p = mine + (i * 16 + l16) * (HD + 2);
+      if (wk > 0) {
+#pragma unroll
+        for (int d = 0; d < DF; ++d)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) p[d * 16 + grp * 4 + r] = o[i][d][r];
+        if (grp == 0) p[HD] = m[i], p[HD + 1] = l[i];
+      }
+    }
+    __syncthreads();
+    if (wk > 0) return;
+#pragma unroll
+    for (int j = 1; j < KW; ++j)
+#pragma unroll
+      for (int i = 0; i < MI; ++i) {
+        const float* const p = results(wave + j) + (i * 16 + l16) * (HD + 2);
+        const float mj = p[HD], top = fmaxf(m[i], mj), ref = top == -INFINITY ? 0.f : top;
+        const float fa = __builtin_amdgcn_exp2f(m[i] - ref), fb = __builtin_amdgcn_exp2f(mj - ref);
+        m[i] = top;
+        l[i] = l[i] * fa + p[HD + 1] * fb;
+#pragma unroll
+        for (int d = 0; d < DF; ++d)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) o[i][d][r] = o[i][d][r] * fa + p[d * 16 + grp * 4 + r] * fb;
+      }
+  }
+#pragma unroll
+  for (int i = 0; i < MI; ++i) {
+    const int r = row0 + i * 16 + l16;
+    if (r >= all) continue;
+    if (a.part) {
+      const size_t at = (((size_t)w.split * c.batch + w.b) * c.n_kv_heads + w.h) * all + r;
+#pragma unroll
+      for (int d = 0; d < DF; ++d) *(f32x4_t*)(a.part + at * HD + d * 16 + grp * 4) = o[i][d];
+      if (grp == 0) a.part_ml[at * 2] = m[i], a.part_ml[at * 2 + 1] = l[i];
+      continue;
+    }
+    const int qr = r / a.G, g = r - qr * a.G;
+    const bool any = r < live && klen > 0;
+    const float f = any ? 1.f / l[i] : 0.f;
+    T* const out = (T*)c.out + w.b * c.out_stride[0] + qr * c.out_stride[1] + (int64_t)(w.h * a.G + g) * c.out_stride[2];
+#pragma unroll
+    for (int d = 0; d < DF; ++d) store_row4<T>(out + d * 16 + grp * 4, any ? o[i][d] * f : f32x4_t{0.f, 0.f, 0.f, 0.f});
+    if (c.lse && grp == 0)
+      c.lse[((size_t)w.b * c.n_q_heads + w.h * a.G + g) * c.rows + qr] = any ? m[i] * kLn2 + logf(l[i]) : -INFINITY;
+  }
+}
+
+// Key ranges joined: a thread takes 4 dims of a row.
+template <typename T>
+__global__ __launch_bounds__(256) void cross_join_kernel(CrossArgs a) {
+  const ravel_cross& c = a.c;
+  const int hd4 = c.head_dim / 4, all = c.rows * a.G;
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, n = (int64_t)c.batch * c.n_kv_heads * all;
+  if (id >= n * hd4) return;
+  const int64_t at = id / hd4;
+  const int d = (int)(id - at * hd4) * 4, r = (int)(at % all), h = (int)(at / all % c.n_kv_heads);
+  const int b = (int)(at / all / c.n_kv_heads);
+  const int qr = r / a.G, g = r - qr * a.G;
+  const bool any = r < live_len(c.q_len, b, c.rows) * a.G && live_len(c.k_len, b, c.keys) > 0;
+  float m = -INFINITY, l = 0.f;
+  f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+  if (any) {
+    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.part_ml[(s * n + at) * 2]);
+    const float ref = m == -INFINITY ? 0.f : m;
+    for (int s = 0; s < a.splits; ++s) {
+      const float f = __builtin_amdgcn_exp2f(a.part_ml[(s * n + at) * 2] - ref);
+      l += f * a.part_ml[(s * n + at) * 2 + 1];
+      o += f * *(const f32x4_t*)(a.part + (s * n + at) * c.head_dim + d);
+    }
+    o *= 1.f / l;
+  }
+  store_row4<T>((T*)c.out + b * c.out_stride[0] + qr * c.out_stride[1] + (int64_t)(h * a.G + g) * c.out_stride[2] + d, o);
+  if (c.lse && d == 0) c.lse[((size_t)b * c.n_q_heads + h * a.G + g) * c.rows + qr] = any ? m * kLn2 + logf(l) : -INFINITY;
+}
+
+// ---------------------------------------------------------------------------
+// dq (and D): a wave owns 16 MI rows, the block walks the keys
+// ---------------------------------------------------------------------------
+template <typename T, int HD, int MI, int TK>
+__global__ __launch_bounds__(256, (4 * Tiles<T, HD, TK>::BYTES <= 65536 ? 2 : 1)) void cross_dq_kernel(CrossArgs a) {
+  typedef Tiles<T, HD, TK> Z;
+  typedef Mat<T> M;
+  typedef typename M::frag frag;
+  constexpr int RB = Z::RB, STEPS = RB / 64, DF = HD / 16, NP = TK / M::CK, FP = M::CK / 16;
+  __shared__ __attribute__((aligned(1024))) char k0[Z::BYTES], v0[Z::BYTES], k1[Z::BYTES], v1[Z::BYTES];
+
+  const int lane = threadIdx.x & 63, wave = wave_index(), l16 = lane & 15, grp = lane >> 4;
+  const ravel_cross& c = a.c;
+  const ravel_cross_grad& g = a.g;
+  const Work w = work_of(a);
+  const int live = live_len(c.q_len, w.b, c.rows) * a.G, all = c.rows * a.G;
+  const int klen = live_len(c.k_len, w.b, c.keys);
+  const int row0 = w.tile * (64 * MI) + wave * 16 * MI;
+  const int ktiles = g.dq ? (klen + TK - 1) / TK : 0, per = (ktiles + a.splits - 1) / a.splits;
+  const int t0 = min(ktiles, w.split * per), t1 = min(ktiles, t0 + per);
+
+  const T* const k = (const T*)c.k + w.b * c.k_stride[0] + w.h * c.k_stride[2];
+  const T* const v = (const T*)c.v + w.b * c.v_stride[0] + w.h * c.v_stride[2];
+  const T *const k_end = k + (int64_t)(klen - 1) * (int)c.k_stride[1] + HD, *const v_end = v + (int64_t)(klen - 1) * (int)c.v_stride[1] + HD;
+  const Segments<T, RB> seg0(lane);
+  const auto issue = [&](int t, char* kt, char* vt) {
+    const auto seg = seg0.fresh();
+    load_keys<T, HD, TK>(seg, k, k_end, (int)c.k_stride[1], t * TK, kt, wave);
+    load_keys<T, HD, TK>(seg, v, v_end, (int)c.v_stride[1], t * TK, vt, wave);
+  };
+  if (t0 < t1) issue(t0, k0, v0);
+
+  frag qf[MI][STEPS], of[MI][STEPS];  // of: dout
+  float lse[MI], D[MI];
+#pragma unroll
+  for (int i = 0; i < MI; ++i) {
+    const int r = row0 + i * 16 + l16, qr = r / a.G, gh = w.h * a.G + r - qr * a.G;
+    const bool in = r < live;
+    const T* const pq = (const T*)c.q + w.b * c.q_stride[0] + qr * c.q_stride[1] + gh * c.q_stride[2];
+    const T* const po = (const T*)c.out + w.b * c.out_stride[0] + qr * c.out_stride[1] + gh * c.out_stride[2];
+    const T* const pd = (const T*)g.dout + w.b * g.dout_stride[0] + qr * g.dout_stride[1] + gh * g.dout_stride[2];
+    D[i] = 0.f;
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+      const int e = (s * 4 + grp) * (16 / sizeof(T));
+      qf[i][s] = in && c.scale > 0.f ? *(const frag*)(pq + e) : frag{};
+      of[i][s] = in ? *(const frag*)(pd + e) : frag{};
+      D[i] += dot16(of[i][s], in ? *(const frag*)(po + e) : frag{});
+    }
+    D[i] += __shfl_xor(D[i], 16, 64);
+    D[i] += __shfl_xor(D[i], 32, 64);
+    lse[i] = in ? c.lse[((size_t)w.b * c.n_q_heads + gh) * c.rows + qr] * kLog2e : INFINITY;
+    if (a.stat && grp == 0 && w.split == 0) {
+      float* const p = a.stat + ((size_t)w.b * c.n_kv_heads + w.h) * a.padded + r;
+      p[0] = lse[i];
+      p[(size_t)c.batch * c.n_kv_heads * a.padded] = D[i];
+    }
+  }
+  if (!g.dq) return;
+  const float cs = c.scale > 0.f ? c.scale * kLog2e : 1.f;
+  f32x4_t dq[MI][DF];
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int d = 0; d < DF; ++d) dq[i][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  const TileLane<T, RB> at0(lane);
+
+  f32x4_t start[TK / 16];  // as in the forward: keys that do not exist
+#pragma unroll
+  for (int f = 0; f < TK / 16; ++f) start[f] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  const auto step = [&](int t, const char* kc, const char* vc, char* kn, char* vn) {
+    tile_barrier<0>();
+    if (t + 1 < t1) issue(t + 1, kn, vn);
+    lds_char_t* const kt = (lds_char_t*)kc;
+    lds_char_t* const vt = (lds_char_t*)vc;
+    if (t == ktiles - 1) {
+      const int left = klen - t * TK - grp * 4;
+#pragma unroll
+      for (int f = 0; f < TK / 16; ++f)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) start[f][r] = f * 16 + r < left ? 0.f : -INFINITY;
+    }
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      const auto at = at0.fresh();
+      f32x4_t s[MI][FP], dp[MI][FP];
+#pragma unroll
+      for (int f = 0; f < FP; ++f) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i) s[i][f] = start[p * FP + f], dp[i][f] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int st = 0; st < STEPS; ++st) {
+          const frag kf = at.along_row(kt, p * FP + f, st), vf = at.along_row(vt, p * FP + f, st);
+#pragma unroll
+          for (int i = 0; i < MI; ++i) {
+            s[i][f] = M::mma(kf, qf[i][st], s[i][f]);
+            dp[i][f] = M::mma(vf, of[i][st], dp[i][f]);
+          }
+        }
+      }
+      frag ds[MI];
+#pragma unroll
+      for (int i = 0; i < MI; ++i) {
+#pragma unroll
+        for (int f = 0; f < FP; ++f)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float pr = __builtin_amdgcn_exp2f(s[i][f][r] * cs - lse[i]);
+            s[i][f][r] = pr * (dp[i][f][r] - D[i]);
+          }
+        ds[i] = M::operand(s[i]);
+      }
+#pragma unroll
+      for (int d = 0; d < DF; ++d) {
+        const frag kf = at.along_col(kt, p, d);
+#pragma unroll
+        for (int i = 0; i < MI; ++i) dq[i][d] = M::mma(kf, ds[i], dq[i][d]);
+      }
+    }
+  };
+  for (int t = t0; t < t1; t += 2) {
+    step(t, k0, v0, k1, v1);
+    if (t + 1 < t1) step(t + 1, k1, v1, k0, v0);
+  }
+#pragma unroll
+  for (int i = 0; i < MI; ++i) {
+    const int r = row0 + i * 16 + l16;
+    if (r >= all) continue;
+    if (a.part) {
+      const size_t to = (((size_t)w.split * c.batch + w.b) * c.n_kv_heads + w.h) * all + r;
+#pragma unroll
+      for (int d = 0; d < DF; ++d) *(f32x4_t*)(a.part + to * HD + d * 16 + grp * 4) = dq[i][d];
+      continue;
+    }
+    const int qr = r / a.G, gh = w.h * a.G + r - qr * a.G;
+    T* const to = (T*)g.dq + w.b * g.dq_stride[0] + qr * g.dq_stride[1] + gh * g.dq_stride[2];
+#pragma unroll
+    for (int d = 0; d < DF; ++d) store_row4<T>(to + d * 16 + grp * 4, r < live ? dq[i][d] * c.scale : f32x4_t{0.f, 0.f, 0.f, 0.f});
+  }
+}
+
+// ---------------------------------------------------------------------------
+// dk, dv: RW waves share 16 KI keys and split a tile's rows between them, the block walks the rows
+// ---------------------------------------------------------------------------
+template <typename T, int HD, int KI, int RW, int TR>
+__global__ __launch_bounds__(256, (4 * Tiles<T, HD, TR>::BYTES <= 65536 && Tiles<T, HD, TR>::RB < 1024 ? 2 : 1)) void cross_dkv_kernel(CrossArgs a) {
+  typedef Tiles<T, HD, TR> Z;
+  typedef Mat<T> M;
+  typedef typename M::frag frag;
+  constexpr int RB = Z::RB, STEPS = RB / 64, DF = HD / 16, TRW = TR / RW, NP = TRW / M::CK, FP = M::CK / 16;
+  static_assert(TRW % M::CK == 0, "whole contraction steps");
+  static_assert(RW == 1 || 16 * KI * HD * 4 <= Z::BYTES, "a wave's sums in a tile");
+  constexpr int TS = TR < 64 ? 64 : TR;  // a tile's lse and D, 64 a load
+  __shared__ __attribute__((aligned(1024))) char q0[Z::BYTES], o0[Z::BYTES], q1[Z::BYTES], o1[Z::BYTES];  // o: dout
+  __shared__ __attribute__((aligned(1024))) float s0[2 * TS], s1[2 * TS];
+
+  const int lane = threadIdx.x & 63, wave = wave_index(), l16 = lane & 15, grp = lane >> 4;
+  const int wr = wave % RW, wk = wave / RW;
+  const ravel_cross& c = a.c;
+  const ravel_cross_grad& g = a.g;
+  const Work w = work_of(a);
+  const int live = live_len(c.q_len, w.b, c.rows) * a.G;
+  const int klen = live_len(c.k_len, w.b, c.keys);
+  const int first = w.tile * (16 * KI * (4 / RW)), key0 = first + wk * 16 * KI;
+  const int rtiles = first < klen ? (live + TR - 1) / TR : 0, per = (rtiles + a.splits - 1) / a.splits;
+  const int t0 = min(rtiles, w.split * per), t1 = min(rtiles, t0 + per);
+
+  const T* const q = (const T*)c.q + w.b * c.q_stride[0] + (int64_t)w.h * a.G * c.q_stride[2];
+  const T* const dout = (const T*)g.dout + w.b * g.dout_stride[0] + (int64_t)w.h * a.G * g.dout_stride[2];
+  const float* const stat = a.stat + ((size_t)w.b * c.n_kv_heads + w.h) * a.padded;
+  const size_t apart = (size_t)c.batch * c.n_kv_heads * a.padded;  // from lse to D
+  const RowSpace space{a.G, ((1 << 23) + a.G - 1) / a.G};
+  const Segments<T, RB> seg0(lane);
+  const auto issue = [&](int t, char* qt, char* ot, float* st) {
+    const auto seg = seg0.fresh();
+    if (wave < 2) {  // one of lse and D (through LDS: loads into registers would wait for the tiles issued before them)
+      const rsrc_t from = buffer_from(stat + wave * apart + t * TR);
+#pragma unroll
+      for (int i = 0; i < TS / 64; ++i)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_dst_t*)(st + wave * TS + i * 64), 4,
+                                                 (int)(lane < TR ? (i * 64 + lane) * 4 : kOutside), 0, 0, 0);
+    }
+    load_rows<T, HD, TR>(seg, q, c.q_stride[1], (int)c.q_stride[2], space, t * TR, live, qt, wave);
+    load_rows<T, HD, TR>(seg, dout, g.dout_stride[1], (int)g.dout_stride[2], space, t * TR, live, ot, wave);
+  };
+  if (t0 < t1) issue(t0, q0, o0, s0);
+
+  frag kf[KI][STEPS], vf[KI][STEPS];
+#pragma unroll
+  for (int i = 0; i < KI; ++i) {
+    const int key = key0 + i * 16 + l16;
+    const T* const pk = (const T*)c.k + w.b * c.k_stride[0] + key * c.k_stride[1] + w.h * c.k_stride[2];
+    const T* const pv = (const T*)c.v + w.b * c.v_stride[0] + key * c.v_stride[1] + w.h * c.v_stride[2];
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+      const int e = (s * 4 + grp) * (16 / sizeof(T));
+      kf[i][s] = key < klen && c.scale > 0.f ? *(const frag*)(pk + e) : frag{};
+      vf[i][s] = key < klen ? *(const frag*)(pv + e) : frag{};
+    }
+  }
+  const float cs = c.scale > 0.f ? c.scale * kLog2e : 1.f;
+  f32x4_t dk[KI][DF], dv[KI][DF];
+#pragma unroll
+  for (int i = 0; i < KI; ++i)
+#pragma unroll
+    for (int d = 0; d < DF; ++d) dk[i][d] = dv[i][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  const TileLane<T, RB> at0(lane);
+
+  const auto step = [&](int t, const char* qc, const char* oc, const float* sc, char* qn, char* on, float* sn) {
+    tile_barrier<0>();
+    if (t + 1 < t1) issue(t + 1, qn, on, sn);
+    RAVEL_LDS const float* const st = (RAVEL_LDS const float*)sc + wr * TRW + grp * 4;
+    lds_char_t* const qt = (lds_char_t*)qc + wr * TRW * RB;
+    lds_char_t* const ot = (lds_char_t*)oc + wr * TRW * RB;
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      const auto at = at0.fresh();
+      f32x4_t s[KI][FP], dp[KI][FP], le[FP], Dr[FP];
+#pragma unroll
+      for (int f = 0; f < FP; ++f) {
+        le[f] = *(RAVEL_LDS const f32x4_t*)(st + (p * FP + f) * 16);
+        Dr[f] = *(RAVEL_LDS const f32x4_t*)(st + TS + (p * FP + f) * 16);
+#pragma unroll
+        for (int i = 0; i < KI; ++i) s[i][f] = dp[i][f] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int st = 0; st < STEPS; ++st) {
+          const frag qf = at.along_row(qt, p * FP + f, st), of = at.along_row(ot, p * FP + f, st);
+#pragma unroll
+          for (int i = 0; i < KI; ++i) {
+            s[i][f] = M::mma(qf, kf[i][st], s[i][f]);
+            dp[i][f] = M::mma(of, vf[i][st], dp[i][f]);
+          }
+        }
+      }
+      frag pf[KI], ds[KI];
+#pragma unroll
+      for (int i = 0; i < KI; ++i) {
+#pragma unroll
+        for (int f = 0; f < FP; ++f)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float pr = __builtin_amdgcn_exp2f(s[i][f][r] * cs - le[f][r]);
+            s[i][f][r] = pr;
+            dp[i][f][r] = pr * (dp[i][f][r] - Dr[f][r]);
+          }
+        pf[i] = M::operand(s[i]);
+        ds[i] = M::operand(dp[i]);
+      }
+#pragma unroll
+      for (int d = 0; d < DF; ++d) {
+        const frag of = at.along_col(ot, p, d), qf = at.along_col(qt, p, d);
+#pragma unroll
+        for (int i = 0; i < KI; ++i) {
+          dv[i][d] = M::mma(of, pf[i], dv[i][d]);
+          dk[i][d] = M::mma(qf, ds[i], dk[i][d]);
+        }
+      }
+    }
+  };
+  for (int t = t0; t < t1; t += 2) {
+    step(t, q0, o0, s0, q1, o1, s1);
+    if (t + 1 < t1) step(t + 1, q1, o1, s1, q0, o0, s0);
+  }
+  if constexpr (RW > 1) {  // the waves that share keys: wave wr = 0 takes their sum, dv first, then dk
+    const auto sums = [&](int w) { return (float*)(w == 0 ? q0 : w == 1 ? o0 : w == 2 ? q1 : o1); };
+    float* const mine = sums(wave);
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+      f32x4_t(&x)[KI][DF] = which ? dk : dv;
+      __syncthreads();
+      if (wr > 0)
+#pragma unroll
+        for (int i = 0; i < KI; ++i)
+#pragma unroll
+          for (int d = 0; d < DF; ++d) *(f32x4_t*)(mine + (i * DF + d) * 256 + lane * 4) = x[i][d];
+      __syncthreads();
+      if (wr == 0)
+#pragma unroll
+        for (int j = 1; j < RW; ++j)
+#pragma unroll
+          for (int i = 0; i < KI; ++i)
+#pragma unroll
+            for (int d = 0; d < DF; ++d) x[i][d] += *(const f32x4_t*)(sums(wave + j) + (i * DF + d) * 256 + lane * 4);
+    }
+    if (wr > 0) return;
+  }
+#pragma unroll
+  for (int i = 0; i < KI; ++i) {
+    const int key = key0 + i * 16 + l16;
+    if (key >= c.keys) continue;
+    if (a.part) {
+      const size_t to = (((size_t)w.split * c.batch + w.b) * c.n_kv_heads + w.h) * c.keys + key;
+#pragma unroll
+      for (int d = 0; d < DF; ++d) {
+        *(f32x4_t*)(a.part + to * HD + d * 16 + grp * 4) = dk[i][d];
+        *(f32x4_t*)(a.part2 + to * HD + d * 16 + grp * 4) = dv[i][d];
+      }
+      continue;
+    }
+    T* const pk = (T*)g.dk + w.b * g.dk_stride[0] + key * g.dk_stride[1] + w.h * g.dk_stride[2];
+    T* const pv = (T*)g.dv + w.b * g.dv_stride[0] + key * g.dv_stride[1] + w.h * g.dv_stride[2];
+    const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int d = 0; d < DF; ++d) {
+      store_row4<T>(pk + d * 16 + grp * 4, key < klen ? dk[i][d] * c.scale : zero);
+      store_row4<T>(pv + d * 16 + grp * 4, key < klen ? dv[i][d] : zero);
+    }
+  }
+}
+
+// Partial sums of ranges added in order: to (b, i, h, d) of a tensor whose index i takes the G heads of a KV head (dq) or
+// is a key (dk, dv: G = 1).
+struct SumArgs {
+  const float* part;
+  void* to;
+  int64_t stride[3];
+  int splits, batch, heads, n, G, hd;  // n = indices of a (batch row, KV head) in part
+  const int* len;
+  int most;
+  float scale;
+};
+template <typename T>
+__global__ __launch_bounds__(256) void cross_sum_kernel(SumArgs x0, SumArgs x1) {
+  const SumArgs a = blockIdx.y ? x1 : x0;
+  const int hd4 = a.hd / 4;
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, n = (int64_t)a.batch * a.heads * a.n;
+  if (id >= n * hd4) return;
+  const int64_t at = id / hd4;
+  const int d = (int)(id - at * hd4) * 4, i = (int)(at % a.n), h = (int)(at / a.n % a.heads), b = (int)(at / a.n / a.heads);
+  f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+  const int qr = i / a.G, g = i - qr * a.G;
+  if (qr < live_len(a.len, b, a.most)) {
+    for (int j = 0; j < a.splits; ++j) s += *(const f32x4_t*)(a.part + (j * n + at) * a.hd + d);
+    s *= a.scale;
+  }
+  store_row4<T>((T*)a.to + b * a.stride[0] + qr * a.stride[1] + (int64_t)(h * a.G + g) * a.stride[2] + d, s);
+}
+
+// ---------------------------------------------------------------------------
+// plans
+// ---------------------------------------------------------------------------
+// Rows of a few-row block (its waves split the keys) and of a many-row block; tile heights.
+template <typename T, int HD>
+struct Shape {
+  static constexpr int RB = HD * sizeof(T);
+  static constexpr int MI = RB >= 1024 ? 1 : 2, TK = RB >= 256 ? 16384 / RB : 64;       // many rows: 128 a block
+  static constexpr int KW = RB >= 512 ? 2 : 4, TF = RB >= 256 ? 32768 / RB : 128;  // few: 16 * 4 / KW a block
+  static constexpr int BI = RB >= 512 ? 1 : 2;                          // gradients: 16-row (or -key) fragments of a wave
+};
+constexpr int kFill = 512;  // blocks that fill the chip, two a CU
+
+int ranges(int64_t blocks, int tiles, int least) {  // of `tiles` tiles, at least `least` each
+  int64_t s = kFill / (blocks < 1 ? 1 : blocks);
+  if (s > tiles / least) s = tiles / least;
+  return s < 1 ? 1 : (int)(s > 64 ? 64 : s);
+}
+
+struct Plan {
+  bool few;
+  int tiles, splits;
+  size_t bytes;
+};
+size_t round256(size_t n) { return (n + 255) / 256 * 256; }
+
+template <typename T, int HD>
+Plan plan_forward(const ravel_cross& c) {
+  typedef Shape<T, HD> S;
+  const int all = c.rows * (c.n_q_heads / c.n_kv_heads);
+  Plan p;
+  p.few = all <= 32;
+  const int per = p.few ? 16 * (4 / S::KW) : 64 * S::MI, tk = p.few ? S::TF : S::TK;
+  p.tiles = (all + per - 1) / per;
+  const int64_t heads = (int64_t)c.batch * c.n_kv_heads;
+  p.splits = ranges(heads * p.tiles, (c.keys + tk - 1) / tk, p.few ? 2 : 4);
+  p.bytes = p.splits > 1 ? round256((size_t)p.splits * heads * all * (HD + 2) * 4) : 0;
+  return p;
+}
+
+template <typename T, int HD>
+hipError_t forward(const ravel_cross& c, hipStream_t s) {
+  typedef Shape<T, HD> S;
+  const Plan p = plan_forward<T, HD>(c);
+  CrossArgs a{};
+  a.c = c;
+  a.G = c.n_q_heads / c.n_kv_heads;
+  a.tiles = p.tiles;
+  a.splits = p.splits;
+  const int64_t heads = (int64_t)c.batch * c.n_kv_heads, all = (int64_t)c.rows * a.G;
+  if (p.splits > 1) {
+    a.part = (float*)c.workspace;
+    a.part_ml = a.part + p.splits * heads * all * HD;
+  }
+  const dim3 grid((unsigned)(heads * p.tiles * p.splits));
+  if (p.few)
+    cross_kernel<T, HD, 1, S::KW, S::TF><<<grid, 256, 0, s>>>(a);
+  else
+    cross_kernel<T, HD, S::MI, 1, S::TK><<<grid, 256, 0, s>>>(a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.splits == 1) return e;
+  cross_join_kernel<T><<<(unsigned)((heads * all * (HD / 4) + 255) / 256), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+struct GradPlan {
+  int qtiles, qsplits, ktiles, ksplits, padded;
+  bool few;  // keys
+  size_t stat, part;
+};
+template <typename T, int HD>
+GradPlan plan_grad(const ravel_cross& c, const ravel_cross_grad& g) {
+  typedef Shape<T, HD> S;
+  const int all = c.rows * (c.n_q_heads / c.n_kv_heads);
+  const int64_t heads = (int64_t)c.batch * c.n_kv_heads;
+  GradPlan p{};
+  const int per = 64 * S::BI;
+  p.padded = (all + 127) / 128 * 128;  // whole tiles of either pass: every row that one reads has its lse and D
+  p.qtiles = p.padded / per;
+  p.qsplits = g.dq ? ranges(heads * p.qtiles, (c.keys + S::TK - 1) / S::TK, 4) : 1;
+  if (p.qsplits > 1) p.part = (size_t)p.qsplits * heads * all * HD * 4;
+  if (g.dk) {
+    p.few = c.keys <= 16 * (4 / S::KW);
+    const int kper = p.few ? 16 * (4 / S::KW) : per, tr = p.few ? S::TF : S::TK;
+    p.ktiles = (c.keys + kper - 1) / kper;
+    p.ksplits = ranges(heads * p.ktiles, (all + tr - 1) / tr, p.few ? 1 : 4);
+    p.stat = round256((size_t)heads * p.padded * 2 * 4);
+    if (p.ksplits > 1) {
+      const size_t n = (size_t)p.ksplits * heads * c.keys * HD * 4 * 2;
+      if (n > p.part) p.part = n;
+    }
+  }
+  p.part = round256(p.part);
+  return p;
+}
+
+template <typename T, int HD>
+hipError_t gradients(const ravel_cross& c, const ravel_cross_grad& g, hipStream_t s) {
+  typedef Shape<T, HD> S;
+  const GradPlan p = plan_grad<T, HD>(c, g);
+  CrossArgs a{};
+  a.c = c;
+  a.g = g;
+  a.G = c.n_q_heads / c.n_kv_heads;
+  a.padded = p.padded;
+  a.stat = p.stat ? (float*)g.workspace : nullptr;
+  float* const part = (float*)((char*)g.workspace + p.stat);
+  const int64_t heads = (int64_t)c.batch * c.n_kv_heads, all = (int64_t)c.rows * a.G;
+  hipError_t e;
+  if (all > 0) {
+    a.tiles = p.qtiles;
+    a.splits = p.qsplits;
+    a.part = p.qsplits > 1 ? part : nullptr;
+    cross_dq_kernel<T, HD, S::BI, S::TK><<<dim3((unsigned)(heads * a.tiles * a.splits)), 256, 0, s>>>(a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    if (a.part) {
+      const SumArgs x{part, g.dq, {g.dq_stride[0], g.dq_stride[1], g.dq_stride[2]}, p.qsplits, c.batch, c.n_kv_heads,
+                      (int)all, a.G, HD, c.q_len, c.rows, c.scale};
+      cross_sum_kernel<T><<<dim3((unsigned)((heads * all * (HD / 4) + 255) / 256), 1), 256, 0, s>>>(x, x);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+  }
+  if (!g.dk || c.keys == 0) return hipSuccess;
+  a.tiles = p.ktiles;
+  a.splits = p.ksplits;
+  a.part = p.ksplits > 1 ? part : nullptr;
+  a.part2 = part + (size_t)p.ksplits * heads * c.keys * HD;
+  const dim3 grid((unsigned)(heads * a.tiles * a.splits));
+  if (p.few)
+    cross_dkv_kernel<T, HD, 1, S::KW, S::TF><<<grid, 256, 0, s>>>(a);
+  else
+    cross_dkv_kernel<T, HD, S::BI, 1, S::TK><<<grid, 256, 0, s>>>(a);
+  if ((e = hipGetLastError()) != hipSuccess || !a.part) return e;
+  SumArgs x{part, g.dk, {g.dk_stride[0], g.dk_stride[1], g.dk_stride[2]}, p.ksplits, c.batch, c.n_kv_heads, c.keys, 1, HD,
+            c.k_len, c.keys, c.scale};
+  SumArgs y = x;
+  y.part = a.part2;
+  y.to = g.dv;
+  for (int i = 0; i < 3; ++i) y.stride[i] = g.dv_stride[i];
+  y.scale = 1.f;
+  cross_sum_kernel<T><<<dim3((unsigned)((heads * c.keys * (HD / 4) + 255) / 256), 2), 256, 0, s>>>(x, y);
+  return hipGetLastError();
+}
+
+template <typename F>
+auto by_shape(const ravel_cross& c, F f) {
+  const auto dims = [&](auto t) {
+    switch (c.head_dim) {
+      case 32: return f(t, std::integral_constant<int, 32>());
+      case 64: return f(t, std::integral_constant<int, 64>());
+      case 128: return f(t, std::integral_constant<int, 128>());
+      default: return f(t, std::integral_constant<int, 256>());
+    }
+  };
+  return c.dtype == RAVEL_F32 ? dims(float()) : dims(bf16_t());
+}
+
+}  // namespace
+
+size_t cross_workspace(const ravel_cross& c) {
+  return by_shape(c, [&](auto t, auto hd) { return plan_forward<decltype(t), hd.value>(c).bytes; });
+}
+hipError_t launch_cross_attention(const ravel_cross& c, hipStream_t s) {
+  if (c.batch == 0 || c.rows == 0) return hipSuccess;
+  return by_shape(c, [&](auto t, auto hd) { return forward<decltype(t), hd.value>(c, s); });
+}
+size_t cross_grad_workspace(const ravel_cross& c, const ravel_cross_grad& g) {
+  return by_shape(c, [&](auto t, auto hd) {
+    const GradPlan p = plan_grad<decltype(t), hd.value>(c, g);
+    return p.stat + p.part;
+  });
+}
+hipError_t launch_cross_attention_grad(const ravel_cross& c, const ravel_cross_grad& g, hipStream_t s) {
+  if (c.batch == 0) return hipSuccess;
+  return by_shape(c, [&](auto t, auto hd) { return gradients<decltype(t), hd.value>(c, g, s); });
+}
+
+}  // namespace ravel

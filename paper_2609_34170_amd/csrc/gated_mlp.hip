@@ -1,0 +1,398 @@
+// Gated MLP up to its hidden values, h = act(x Wg^T) * (x Wu^T), and its gradients.
+//
+// One matrix kernel serves the forward and both gradient products.  Its operands come as rows along the contraction (x
+// and the weights of the forward) or as rows across it (the weights for dx, x and the hidden gradients for dw): either
+// kind goes from memory to LDS as it lies and is read from there as fragments along rows or along columns (lds_tile.h),
+// so nothing is transposed in memory.  The forward's blocks take the gate and up weights of the same hidden units, 16 and 16 in
+// turn, so that a wave holds both products of a unit and the activation, the product and the one rounding are its
+// epilogue.
+#include "gemm_epilogue.h"
+#include "layer.h"
+#include "lds_tile.h"
+
+namespace ravel {
+namespace {
+
+struct MatArgs {
+  // C[m, n] = sum over pairs p and k < K of A[p](m, k) B[p](n, k)
+  const void *A[2], *B[2];
+  int64_t lda, ldb;
+  int M, N, K, pairs;
+  int splits, per;  // ranges of the contraction's tiles (all pairs'), and tiles of a range
+  // FORWARD: B[0] gate and B[1] up weights, N = 2 hidden; C[0] h, C[1] and C[2] x Wg^T and x Wu^T or null
+  // BOTH: two products C[0] = A[0] B[0], C[1] = A[1] B[0], one behind the other in the grid
+  void* C[3];
+  int64_t ldc, ldg;
+  int act;
+  float* part;  // splits > 1: [split][M][N]
+};
+enum { STORE = 0, FORWARD = 1, BOTH = 2 };
+
+RAVEL_DEV float act_f(float x, int kind) { return kind == RAVEL_SILU ? silu_f(x) : gelu_tanh_f(x); }
+
+RAVEL_DEV void put4(float* p, f32x4_t v) { *(f32x4_t*)p = v; }
+RAVEL_DEV void put4(bf16_t* p, f32x4_t v) { *(u32x2_t*)p = u32x2_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])}; }
+
+// BM x BN outputs a block of WM x WN waves.  AC, BC: A, B lie as rows across the contraction.  O: type of the outputs.
+template <typename T, typename O, int BM, int BN, int WM, int WN, bool AC, bool BC, int MODE>
+__global__ __launch_bounds__(64 * WM * WN) void mlp_matrix_kernel(MatArgs a) {
+  typedef Mat<T> M;
+  typedef typename M::frag frag;
+  constexpr int E = sizeof(T), BK = 128 / E, NW = WM * WN;
+  constexpr int TM = BM / (16 * WM), TN = BN / (16 * WN);
+  constexpr int RA = AC ? BM * E : 128, RBB = BC ? BN * E : 128;  // bytes of a tile's row
+  constexpr int SA = BM * 128 / 1024 / NW, SB = BN * 128 / 1024 / NW;
+  static_assert(SA >= 1 && SB >= 1 && BM % (16 * WM) == 0 && BN % (16 * WN) == 0, "tiles");
+  static_assert(MODE != FORWARD || TN % 2 == 0, "a gate block and its up block in one wave");
+  // Four arrays: reads along columns of one buffer wait for the loads in flight into another unless the compiler sees
+  // that they are apart.
+  __shared__ __attribute__((aligned(1024))) char As0[BM * 128], As1[BM * 128], Bs0[BN * 128], Bs1[BN * 128];
+
+  const int lane = threadIdx.x & 63, wave = wave_index(), l16 = lane & 15, grp = lane >> 4;
+  const int wm = wave / WN, wn = wave % WN;
+  const int tiles_m = (a.M + BM - 1) / BM, tiles_n = (a.N + BN - 1) / BN, tiles_k = (a.K + BK - 1) / BK;
+  const int all_m = MODE == BOTH ? 2 * tiles_m : tiles_m;
+  int tr, tc, z;
+  item_rcz(xcd_tile(blockIdx.x, gridDim.x), all_m, tiles_n, a.splits, tr, tc, z);
+  const int which = MODE == BOTH && tr >= tiles_m ? 1 : 0;
+  const int m0 = (tr - which * tiles_m) * BM, n0 = tc * BN;
+  const int k0 = z * a.per, k1 = min(tiles_k * a.pairs, k0 + a.per);
+
+  // An operand's rows are its own (AC false) or the contraction's; its end is its last element's, rows behind it are
+  // zeros.  Columns behind a row's end read the next row: across the contraction they are outputs that are not
+  // stored, along it (the last tile) they are cut off.
+  const Segments<T, RA> sa0(lane);
+  const Segments<T, RBB> sb0(lane);
+  const int lda = (int)a.lda * E, ldb = (int)a.ldb * E;
+  const auto issue = [&](int t, char* Ad, char* Bd) {
+    const auto sa = sa0.fresh();
+    const auto sb = sb0.fresh();
+    const unsigned ra = __umul24(sa.row, lda), rb = __umul24(sb.row, ldb);
+    const int pair = t >= tiles_k ? 1 : 0, k = (t - pair * tiles_k) * BK, left = (a.K - k) * E;
+    const char* const A = (const char*)a.A[MODE == BOTH ? which : pair];
+    const char* const A_end = A + (AC ? (int64_t)(a.K - 1) * lda + a.M * E : (int64_t)(a.M - 1) * lda + a.K * E);
+#pragma unroll
+    for (int i = 0; i < SA; ++i) {
+      const int seg = wave * SA + i, r = seg * sa.ROWS, c = sa.byte_of(seg);
+      const rsrc_t from = buffer_until(A + (AC ? (int64_t)(k + r) * lda + m0 * E : (int64_t)(m0 + r) * lda + k * E), A_end);
+      load_segment(from, Ad, seg, AC || c < left ? ra + c : kOutside);
+    }
+    const char* const B = (const char*)a.B[MODE == STORE ? pair : 0];
+#pragma unroll
+    for (int i = 0; i < SB; ++i) {
+      const int seg = wave * SB + i, c = sb.byte_of(seg);
+      if constexpr (MODE == FORWARD) {  // rows 32 j .. + 15 of the tile: gate, the next 16: up weights of the same units
+        const char* const W = (const char*)a.B[(seg >> 1) & 1];
+        const int u = n0 / 2 + (seg >> 2) * 16 + (seg & 1) * 8;
+        const rsrc_t from = buffer_until(W + (int64_t)u * ldb + k * E, W + (int64_t)(a.N / 2 - 1) * ldb + a.K * E);
+        load_segment(from, Bd, seg, c < left ? rb + c : kOutside);
+      } else {
+        const int r = seg * sb.ROWS;
+        const char* const B_end = B + (BC ? (int64_t)(a.K - 1) * ldb + a.N * E : (int64_t)(a.N - 1) * ldb + a.K * E);
+        const rsrc_t from = buffer_until(B + (BC ? (int64_t)(k + r) * ldb + n0 * E : (int64_t)(n0 + r) * ldb + k * E), B_end);
+        load_segment(from, Bd, seg, BC || c < left ? rb + c : kOutside);
+      }
+    }
+  };
+
+  f32x4_t acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  TileLane<T, RA, true> la(lane);
+  TileLane<T, RBB, true> lb(lane);
+  la.advance(AC ? 0 : wm * TM, AC ? wm * TM : 0);
+  lb.advance(BC ? 0 : wn * TN, BC ? wn * TN : 0);
+  const auto compute = [&](const char* Ad, const char* Bd) {
+    lds_char_t* const as = (lds_char_t*)Ad;
+    lds_char_t* const bs = (lds_char_t*)Bd;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const auto ta = la.fresh();
+      const auto tb = lb.fresh();
+      frag af[TM], bf[TN];
+#pragma unroll
+      for (int j = 0; j < TN; ++j) bf[j] = BC ? tb.along_col(bs, s, j) : tb.along_row(bs, j, s);
+#pragma unroll
+      for (int i = 0; i < TM; ++i) af[i] = AC ? ta.along_col(as, s, i) : ta.along_row(as, i, s);
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = M::mma(bf[j], af[i], acc[i][j]);
+      __builtin_amdgcn_sched_barrier(0);  // the next step's fragments have no registers before these are used
+    }
+  };
+  if (k0 < k1) issue(k0, As0, Bs0);
+  for (int t = k0; t < k1; t += 2) {  // two buffers: the next tile is in flight while one is multiplied
+    tile_barrier<0>();
+    if (t + 1 < k1) issue(t + 1, As1, Bs1);
+    compute(As0, Bs0);
+    if (t + 1 < k1) {
+      tile_barrier<0>();
+      if (t + 2 < k1) issue(t + 2, As0, Bs0);
+      compute(As1, Bs1);
+    }
+  }
+
+  // acc[i][j] is row l16, columns 4 grp .. + 3 of its 16 x 16 block
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int m = m0 + (wm * TM + i) * 16 + l16;
+    if (m >= a.M) continue;
+    if constexpr (MODE == FORWARD) {
+#pragma unroll
+      for (int j = 0; j < TN; j += 2) {
+        const int u = n0 / 2 + (wn * TN + j) * 8 + grp * 4;
+        if (u >= a.N / 2) continue;
+        f32x4_t h;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) h[r] = act_f(acc[i][j][r], a.act) * acc[i][j + 1][r];
+        put4((O*)a.C[0] + m * a.ldc + u, h);
+        if (a.C[1]) {
+          put4((O*)a.C[1] + m * a.ldg + u, acc[i][j]);
+          put4((O*)a.C[2] + m * a.ldg + u, acc[i][j + 1]);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < TN; ++j) {
+        const int n = n0 + (wn * TN + j) * 16 + grp * 4;
+        if (n >= a.N) continue;
+        if (a.part)
+          put4(a.part + (((size_t)z * (MODE == BOTH ? 2 : 1) + which) * a.M + m) * a.N + n, acc[i][j]);
+        else
+          put4((O*)a.C[which] + m * a.ldc + n, acc[i][j]);
+      }
+    }
+  }
+}
+
+// Ranges of the contraction added in order.
+template <typename O>
+__global__ __launch_bounds__(256) void mlp_sum_kernel(const float* part, int splits, int64_t range, O* c0, O* c1, int64_t ldc,
+                                                      int M, int N) {
+  const int n4 = N / 4;
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (id >= (int64_t)M * n4) return;
+  const int64_t m = id / n4;
+  const int n = (int)(id - m * n4) * 4;
+  part += (size_t)blockIdx.y * M * N;
+  f32x4_t s = *(const f32x4_t*)(part + m * N + n);
+  for (int z = 1; z < splits; ++z) s += *(const f32x4_t*)(part + z * range + m * N + n);
+  put4((blockIdx.y ? c1 : c0) + m * ldc + n, s);
+}
+
+// The hidden gradients, dg = dh u act'(g) and du = dh act(g), [rows, hidden] each.
+RAVEL_DEV void act_grad(float x, int kind, float& y, float& slope) {
+  if (kind == RAVEL_SILU) {
+    const float s = 1.f / (1.f + __expf(-x));
+    y = x * s;
+    slope = s * (1.f + x * (1.f - s));
+  } else {
+    // gelu_tanh_f's form: s = 1 / (1 + exp(-2 u)), y = x s, slope = s + x s (1 - s) 2 u'
+    const float c = 0.7978845608028654f, x2 = x * x;
+    const float s = 1.f / (1.f + __expf(-2.f * c * x * (1.f + 0.044715f * x2)));
+    y = x * s;
+    // (far out s (1 - s) is 0, and must not meet an infinite x^2)
+    const float z = fminf(fmaxf(x, -64.f), 64.f);
+    slope = s + z * s * (1.f - s) * (2.f * c) * (1.f + 3.f * 0.044715f * z * z);
+  }
+}
+template <typename T> RAVEL_DEV void get8(const T* p, float (&v)[8]);
+template <> RAVEL_DEV void get8<float>(const float* p, float (&v)[8]) {
+  const f32x4_t a = *(const f32x4_t*)p, b = *(const f32x4_t*)(p + 4);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = a[i], v[i + 4] = b[i];
+}
+template <> RAVEL_DEV void get8<bf16_t>(const bf16_t* p, float (&v)[8]) {
+  const u32x4_t w = *(const u32x4_t*)p;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(w[i] << 16), v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+}
+RAVEL_DEV void put8(float* p, const float (&v)[8]) {
+  *(f32x4_t*)p = f32x4_t{v[0], v[1], v[2], v[3]};
+  *(f32x4_t*)(p + 4) = f32x4_t{v[4], v[5], v[6], v[7]};
+}
+RAVEL_DEV void put8(bf16_t* p, const float (&v)[8]) {
+  *(u32x4_t*)p = u32x4_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+}
+template <typename T>
+__global__ __launch_bounds__(256) void mlp_hidden_grad_kernel(ravel_mlp a, ravel_mlp_grad g, T* dg, T* du) {
+  const int n8 = a.hidden / 8;
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (id >= (int64_t)a.rows * n8) return;
+  const int64_t m = id / n8;
+  const int n = (int)(id - m * n8) * 8;
+  float x[8], u[8], dh[8];
+  get8((const T*)a.gate + m * a.gate_stride + n, x);
+  get8((const T*)a.up + m * a.gate_stride + n, u);
+  get8((const T*)g.dh + m * g.dh_stride + n, dh);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    float y, slope;
+    act_grad(x[i], a.act, y, slope);
+    x[i] = dh[i] * u[i] * slope;
+    u[i] = dh[i] * y;
+  }
+  put8(dg + m * a.hidden + n, x);
+  put8(du + m * a.hidden + n, u);
+}
+
+// ---------------------------------------------------------------------------
+// plans
+// ---------------------------------------------------------------------------
+struct MatPlan {
+  int tile;  // 0: 256 x 256, 1: 128 x 128, 2: 64 x 64
+  int splits, per;
+};
+constexpr int kTile[3] = {256, 128, 64};
+int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+
+// The largest tile that still gives every CU a block; then, with 64 x 64 ones and `split` allowed, ranges of the
+// contraction of at least 4 tiles.
+MatPlan plan_matrix(int64_t M, int64_t N, int64_t K, int pairs, int products, int elt, bool split) {
+  MatPlan p;
+  for (p.tile = elt == 4 ? 1 : 0; p.tile < 2; ++p.tile)
+    if ((int64_t)ceil_div(M, kTile[p.tile]) * ceil_div(N, kTile[p.tile]) * products >= 192) break;
+  const int64_t blocks = (int64_t)ceil_div(M, kTile[p.tile]) * ceil_div(N, kTile[p.tile]) * products;
+  const int tiles = ceil_div(K, 128 / elt) * pairs;
+  int s = split ? (int)(512 / blocks) : 1;
+  if (s > tiles / 4) s = tiles / 4;
+  if (s < 1) s = 1;
+  p.per = ceil_div(tiles, s);
+  if (p.per < 1) p.per = 1;
+  p.splits = tiles ? ceil_div(tiles, p.per) : 1;
+  return p;
+}
+
+template <typename T, typename O, bool AC, bool BC, int MODE>
+hipError_t launch_matrix(const MatArgs& a, int tile, hipStream_t s) {
+  const int64_t blocks = (int64_t)ceil_div(a.M, kTile[tile]) * ceil_div(a.N, kTile[tile]) * a.splits * (MODE == BOTH ? 2 : 1);
+  const dim3 grid((unsigned)blocks);
+  if (tile == 0) {
+    if constexpr (sizeof(T) == 2) mlp_matrix_kernel<T, O, 256, 256, 2, 4, AC, BC, MODE><<<grid, 512, 0, s>>>(a);
+  } else if (tile == 1) {
+    mlp_matrix_kernel<T, O, 128, 128, 2, 2, AC, BC, MODE><<<grid, 256, 0, s>>>(a);
+  } else {
+    mlp_matrix_kernel<T, O, 64, 64, 2, 2, AC, BC, MODE><<<grid, 256, 0, s>>>(a);
+  }
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t forward(const ravel_mlp& m, hipStream_t s) {
+  MatArgs a{};
+  a.A[0] = m.x;
+  a.B[0] = m.wg;
+  a.B[1] = m.wu;
+  a.lda = m.x_stride;
+  a.ldb = m.w_stride;
+  a.M = m.rows;
+  a.N = 2 * m.hidden;
+  a.K = m.width;
+  a.pairs = 1;
+  a.C[0] = m.h;
+  a.C[1] = m.gate;
+  a.C[2] = m.up;
+  a.ldc = m.h_stride;
+  a.ldg = m.gate_stride;
+  a.act = m.act;
+  const MatPlan p = plan_matrix(a.M, a.N, a.K, 1, 1, sizeof(T), false);
+  a.splits = p.splits;
+  a.per = p.per;
+  return launch_matrix<T, T, false, false, FORWARD>(a, p.tile, s);
+}
+
+struct GradBytes {
+  size_t hidden, part;  // of one of dg and du; of the ranges' sums
+};
+GradBytes grad_bytes(const ravel_mlp& m, const ravel_mlp_grad& g) {
+  const int e = m.dtype == RAVEL_F32 ? 4 : 2;
+  GradBytes b{};
+  if (!g.dx && !g.dwg) return b;
+  b.hidden = ((size_t)m.rows * m.hidden * e + 255) / 256 * 256;
+  if (g.dx) {
+    const MatPlan p = plan_matrix(m.rows, m.width, m.hidden, 2, 1, e, true);
+    if (p.splits > 1) b.part = (size_t)p.splits * m.rows * m.width * 4;
+  }
+  if (g.dwg) {
+    const MatPlan p = plan_matrix(m.hidden, m.width, m.rows, 1, 2, e, true);
+    const size_t n = p.splits > 1 ? (size_t)p.splits * 2 * m.hidden * m.width * 4 : 0;
+    if (n > b.part) b.part = n;
+  }
+  b.part = (b.part + 255) / 256 * 256;
+  return b;
+}
+
+template <typename O>
+hipError_t add_ranges(const MatArgs& a, int products, hipStream_t s) {
+  const dim3 grid((unsigned)ceil_div((int64_t)a.M * (a.N / 4), 256), products);
+  mlp_sum_kernel<O><<<grid, 256, 0, s>>>(a.part, a.splits, (int64_t)products * a.M * a.N, (O*)a.C[0], (O*)a.C[1], a.ldc, a.M, a.N);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t gradients(const ravel_mlp& m, const ravel_mlp_grad& g, hipStream_t s) {
+  const GradBytes b = grad_bytes(m, g);
+  char* const ws = (char*)g.workspace;
+  T *const dg = (T*)ws, *const du = (T*)(ws + b.hidden);
+  float* const part = (float*)(ws + 2 * b.hidden);
+  hipError_t e;
+  if (m.rows > 0) {
+    mlp_hidden_grad_kernel<T><<<ceil_div((int64_t)m.rows * (m.hidden / 8), 256), 256, 0, s>>>(m, g, dg, du);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  if (g.dx && m.rows > 0) {
+    MatArgs a{};
+    a.A[0] = dg, a.A[1] = du;
+    a.B[0] = m.wg, a.B[1] = m.wu;
+    a.lda = m.hidden;
+    a.ldb = m.w_stride;
+    a.M = m.rows, a.N = m.width, a.K = m.hidden, a.pairs = 2;
+    a.C[0] = g.dx;
+    a.ldc = g.dx_stride;
+    const MatPlan p = plan_matrix(a.M, a.N, a.K, 2, 1, sizeof(T), true);
+    a.splits = p.splits, a.per = p.per;
+    a.part = p.splits > 1 ? part : nullptr;
+    if ((e = launch_matrix<T, T, false, true, STORE>(a, p.tile, s)) != hipSuccess) return e;
+    if (a.part && (e = add_ranges<T>(a, 1, s)) != hipSuccess) return e;
+  }
+  if (g.dwg) {
+    MatArgs a{};
+    a.A[0] = dg, a.A[1] = du;
+    a.B[0] = m.x;
+    a.lda = m.hidden;
+    a.ldb = m.x_stride;
+    a.M = m.hidden, a.N = m.width, a.K = m.rows, a.pairs = 1;
+    a.C[0] = g.dwg, a.C[1] = g.dwu;
+    a.ldc = g.dw_stride;
+    const MatPlan p = plan_matrix(a.M, a.N, a.K, 1, 2, sizeof(T), true);
+    a.splits = p.splits, a.per = p.per;
+    a.part = p.splits > 1 ? part : nullptr;
+    const bool wide = g.weight_dtype == RAVEL_F32;
+    if ((e = wide ? launch_matrix<T, float, true, true, BOTH>(a, p.tile, s) : launch_matrix<T, T, true, true, BOTH>(a, p.tile, s)) !=
+        hipSuccess)
+      return e;
+    if (a.part && (e = wide ? add_ranges<float>(a, 2, s) : add_ranges<T>(a, 2, s)) != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+}  // namespace
+
+size_t mlp_workspace(const ravel_mlp&) { return 0; }
+hipError_t launch_gated_mlp(const ravel_mlp& m, hipStream_t s) {
+  if (m.rows == 0) return hipSuccess;
+  return m.dtype == RAVEL_F32 ? forward<float>(m, s) : forward<bf16_t>(m, s);
+}
+size_t mlp_grad_workspace(const ravel_mlp& m, const ravel_mlp_grad& g) {
+  const GradBytes b = grad_bytes(m, g);
+  return 2 * b.hidden + b.part;
+}
+hipError_t launch_gated_mlp_grad(const ravel_mlp& m, const ravel_mlp_grad& g, hipStream_t s) {
+  if (!g.dx && !g.dwg) return hipSuccess;
+  return m.dtype == RAVEL_F32 ? gradients<float>(m, g, s) : gradients<bf16_t>(m, g, s);
+}
+
+}  // namespace ravel

@@ -65,8 +65,56 @@ class RavelCacheQuery(ctypes.Structure):
         ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_int64)]
 
 
-# RavelCacheQuery's fields in one call (filling the structure field by field costs more than a launch)
+class RavelNorm(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("stream_dtype", "dtype", "rows", "width", "mods", "group")] + [
+        ("eps", ctypes.c_float), ("reserved", ctypes.c_int32)] + [
+        (n, ctypes.c_void_p) for n in ("x", "f", "post", "alpha", "gate", "scale", "shift", "x_out", "y")] + [
+        (n + "_stride", ctypes.c_int64) for n in ("x", "f", "x_out", "y", "gate", "scale", "shift")]
+
+
+class RavelNormGrad(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in (
+        "dy", "d_out", "dx", "df", "dpost", "dalpha", "dgate", "dscale", "dshift")] + [
+        (n + "_stride", ctypes.c_int64) for n in ("dy", "d_out", "dx", "df", "dgate", "dscale", "dshift")] + [
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_int64)]
+
+
+class RavelCross(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "dtype", "batch", "n_q_heads", "n_kv_heads", "head_dim", "rows", "keys")] + [("scale", ctypes.c_float)] + [
+        (n, ctypes.c_void_p) for n in ("q_len", "k_len", "q", "k", "v", "out", "lse")] + [
+        (n + "_stride", ctypes.c_int64 * 3) for n in ("q", "k", "v", "out")] + [
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_int64)]
+
+
+class RavelCrossGrad(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("dout", "dq", "dk", "dv")] + [
+        (n + "_stride", ctypes.c_int64 * 3) for n in ("dout", "dq", "dk", "dv")] + [
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_int64)]
+
+
+class RavelMlp(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "act", "rows", "width", "hidden", "reserved")] + [
+        (n, ctypes.c_void_p) for n in ("x", "wg", "wu", "h", "gate", "up")] + [
+        (n + "_stride", ctypes.c_int64) for n in ("x", "w", "h", "gate")] + [
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_int64)]
+
+
+class RavelMlpGrad(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("weight_dtype", "reserved")] + [
+        (n, ctypes.c_void_p) for n in ("dh", "dx", "dwg", "dwu")] + [
+        (n + "_stride", ctypes.c_int64) for n in ("dh", "dx", "dw")] + [
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_int64)]
+
+
+# The structures' fields in one call (filling them field by field costs more than a launch)
 _pack_query = struct.Struct("@6ifi5P9qPq").pack
+_pack_norm = struct.Struct("@6ifi9P7q").pack
+_pack_norm_grad = struct.Struct("@9P7qPq").pack
+_pack_cross = struct.Struct("@7if7P12qPq").pack
+_pack_cross_grad = struct.Struct("@4P12qPq").pack
+_pack_mlp = struct.Struct("@6i6P4qPq").pack
+_pack_mlp_grad = struct.Struct("@2i4P3qPq").pack
 
 
 SYMBOLS = [
@@ -79,6 +127,10 @@ SYMBOLS = [
     "ravel_cache_append", "ravel_cache_attention_workspace", "ravel_cache_attention", "ravel_cache_evict_workspace",
     "ravel_cache_evict", "ravel_buffer_create_quantized", "ravel_context_track", "ravel_context_evict",
     "ravel_context_cache",
+    "ravel_norm_residual", "ravel_norm_residual_grad_workspace", "ravel_norm_residual_grad",
+    "ravel_cross_attention_workspace", "ravel_cross_attention", "ravel_cross_attention_grad_workspace",
+    "ravel_cross_attention_grad", "ravel_gated_mlp_workspace", "ravel_gated_mlp", "ravel_gated_mlp_grad_workspace",
+    "ravel_gated_mlp_grad",
 ]
 
 _lib = None
@@ -126,6 +178,17 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "ravel_context_track": ([vp, i32], i32),
         "ravel_context_evict": ([vp, i32, i32, i32, vp], i32),
         "ravel_context_cache": ([vp, i32, ctypes.POINTER(RavelCache)], i32),
+        "ravel_norm_residual": ([vp, vp], i32),
+        "ravel_norm_residual_grad_workspace": ([vp, vp, ctypes.POINTER(i64)], i32),
+        "ravel_norm_residual_grad": ([vp, vp, vp], i32),
+        "ravel_cross_attention_workspace": ([vp, ctypes.POINTER(i64)], i32),
+        "ravel_cross_attention": ([vp, vp], i32),
+        "ravel_cross_attention_grad_workspace": ([vp, vp, ctypes.POINTER(i64)], i32),
+        "ravel_cross_attention_grad": ([vp, vp, vp], i32),
+        "ravel_gated_mlp_workspace": ([vp, ctypes.POINTER(i64)], i32),
+        "ravel_gated_mlp": ([vp, vp], i32),
+        "ravel_gated_mlp_grad_workspace": ([vp, vp, ctypes.POINTER(i64)], i32),
+        "ravel_gated_mlp_grad": ([vp, vp, vp], i32),
     }
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
@@ -516,3 +579,352 @@ class Cache:
                                          None if into is None else into._ref, self._index("into_seq", into_seq, B),
                                          kept.data_ptr(), ws.data_ptr(), n.value, s))
         return kept
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# A layer's operators (ravel_norm_residual, ravel_cross_attention, ravel_gated_mlp and their gradients)
+#
+# Tensors are the caller's, on one GPU; outputs that are not given are allocated.  Calls are enqueued on ``stream``
+# (default: torch's current one of that GPU).
+# ---------------------------------------------------------------------------------------------------------------------
+GELU_TANH, SILU = 0, 1
+_ACTS = {"gelu": GELU_TANH, "silu": SILU}
+_tools = None
+
+
+def _layer_tools():
+    """(torch, library, torch's types as RAVEL_*, device -> its current stream's handle)"""
+    global _tools
+    if _tools is None:
+        import torch
+
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda device: torch.cuda.current_stream(device).cuda_stream)
+        _tools = torch, load_library(), {torch.float32: F32, torch.bfloat16: BF16}, raw
+    return _tools
+
+
+class _Placed:
+    """A call's device and stream: ``with`` makes both current (for the launches and what the call allocates), and
+    ``handle`` is the stream's."""
+
+    def __init__(self, stream, first, *rest):
+        torch, _, _, raw = _layer_tools()
+        device = first.get_device()
+        if device < 0:
+            raise ValueError("the call needs its tensors on a GPU")
+        for t in rest:
+            if t is not None and t.get_device() != device:
+                raise ValueError(f"every tensor of the call must be on {first.device}")
+        self.guard = None
+        if stream is None:
+            self.handle = raw(device)
+            if device != torch.cuda.current_device():
+                self.guard = torch.cuda.device(device)
+            return
+        if isinstance(stream, int):
+            stream = torch.cuda.ExternalStream(stream, device=first.device)
+        elif stream.device != first.device:
+            raise ValueError(f"the stream must be one of {first.device}")
+        self.guard, self.handle = torch.cuda.stream(stream), stream.cuda_stream
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+        return self
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def _dtype_of(name, t) -> int:
+    d = _layer_tools()[2].get(t.dtype)
+    if d is None:
+        raise ValueError(f"{name} must be bfloat16 or float32, got {t.dtype}")
+    return d
+
+
+def _like(name, t, shape, dtype):
+    if t.shape != shape or t.dtype is not dtype:
+        raise ValueError(f"{name} must be a {dtype} tensor {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    if shape[-1] > 1 and t.stride(-1) != 1 and t.numel():
+        raise ValueError(f"{name}'s last dimension must be contiguous")
+
+
+def _rows2(name, t, shape, dtype):
+    """(address, row stride) of a matrix, or (0, 0) for None."""
+    if t is None:
+        return 0, 0
+    _like(name, t, shape, dtype)
+    return t.data_ptr(), t.stride(0)
+
+
+def _scratch(fn, *packed):
+    """Workspace of a call: (tensor that holds it or None, address, bytes).  It is the call's alone: torch keeps its memory
+    from later calls on the stream until this one has run."""
+    torch = _layer_tools()[0]
+    n = ctypes.c_int64(0)
+    _check(fn(*packed, ctypes.byref(n)))
+    if n.value == 0:
+        return None, 0, 0
+    memory = torch.empty(n.value, dtype=torch.uint8, device=torch.device("cuda", torch.cuda.current_device()))
+    return memory, memory.data_ptr(), n.value
+
+
+def _modulation(x, post, alpha, gate, scale, shift):
+    """Addresses of what modulates x [rows, width], strides of gate, scale and shift, and their common row count."""
+    torch = _layer_tools()[0]
+    width, mods, ptr, stride = x.shape[1], 1, [], []
+    for name, t in (("post", post), ("alpha", alpha)):
+        if t is not None and (t.dtype is not torch.float32 or t.numel() != (width if name == "post" else 1) or
+                              not t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous float32 tensor of {width if name == 'post' else 1}")
+        ptr.append(0 if t is None else t.data_ptr())
+    for name, t in (("gate", gate), ("scale", scale), ("shift", shift)):
+        if t is not None and t.dim() == 2:
+            if mods not in (1, t.shape[0]) and t.shape[0] != 1:
+                raise ValueError("gate, scale and shift must have the same number of rows, or one")
+            mods = max(mods, t.shape[0])
+    for name, t in (("gate", gate), ("scale", scale), ("shift", shift)):
+        if t is None:
+            ptr.append(0), stride.append(0)
+            continue
+        if t.dim() not in (1, 2) or t.shape[-1] != width or t.dtype is not torch.float32:
+            raise ValueError(f"{name} must be a float32 tensor [{width}] or [rows of modulation, {width}]")
+        if t.stride(-1) != 1 and width > 1:
+            raise ValueError(f"{name}'s last dimension must be contiguous")
+        if t.dim() == 2 and t.shape[0] > 1 and t.stride(0) == 0:
+            raise ValueError(f"{name}: pass the row that is repeated as a vector")
+        ptr.append(t.data_ptr()), stride.append(t.stride(0) if t.dim() == 2 and t.shape[0] > 1 else 0)
+    return ptr, stride, mods
+
+
+def norm_residual(x, f=None, post=None, alpha=None, gate=None, scale=None, shift=None, group: int = 1, eps: float = 1e-6,
+                  y=None, x_out=None, stream=None):
+    """(y, x_out): the residual stream x ``[rows, width]`` after a block's output f, t = x + alpha * gate * F with F = f or,
+    with ``post``, f / rms(f) * (1 + post), and the next block's input y = t / rms(t) * (1 + scale) + shift.
+
+    y has f's dtype (without f: that of a given y, or bfloat16).  ``post`` ``[width]`` and ``alpha`` (one number) are
+    float32 tensors; ``gate``, ``scale`` and ``shift`` float32 ``[width]`` or ``[mods, width]``, of which row r uses
+    (r // group) % mods.  Without f, x_out is x itself.  x_out may be x.
+    """
+    torch, lib, types, _ = _layer_tools()
+    if x.dim() != 2:
+        raise ValueError("x must be [rows, width]")
+    T = f.dtype if f is not None else y.dtype if y is not None else torch.bfloat16
+    S, shape = x.dtype, x.shape
+    sizes = (_dtype_of("x", x), types.get(T, -1), *shape)
+    ptr, stride, mods = _modulation(x, post, alpha, gate, scale, shift)
+    with _Placed(stream, x, f, post, alpha, gate, scale, shift, y, x_out) as on:
+        if y is None:
+            y = torch.empty(shape, dtype=T, device=x.device)
+        if f is not None and x_out is None:
+            x_out = torch.empty(shape, dtype=S, device=x.device)
+        elif f is None and x_out is not None:
+            raise ValueError("x_out goes with f")
+        xp, xs = _rows2("x", x, shape, S)
+        fp, fs = _rows2("f", f, shape, T)
+        yp, ys = _rows2("y", y, shape, T)
+        op, os_ = _rows2("x_out", x_out, shape, S)
+        _check(lib.ravel_norm_residual(_pack_norm(*sizes, mods, group, eps, 0, xp, fp, *ptr, op, yp, xs, fs, os_, ys, *stride),
+                                       on.handle))
+    return y, x if f is None else x_out
+
+
+def norm_residual_grad(x_out, dy=None, d_out=None, f=None, post=None, alpha=None, gate=None, scale=None, shift=True,
+                       group: int = 1, eps: float = 1e-6, grads=None, stream=None):
+    """Gradients of norm_residual from those of y (``dy``) and of x_out (``d_out``; None: zero), as a dict.
+
+    ``x_out`` is the forward's (without f: its x); the other inputs are the forward's.  ``grads`` names the outputs and may
+    hold their tensors: ``{"x": tensor or None, "f": ..., "post": ..., "alpha": ..., "gate": ..., "scale": ..., "shift":
+    ...}``, None being allocated; by default every input that is given, and ``shift`` (pass the forward's, or its shape's
+    like; False: none) in scale's shape.  Gradients of the stream and the block have their dtype, the others float32.
+    """
+    torch, lib, types, _ = _layer_tools()
+    if x_out.dim() != 2:
+        raise ValueError("x_out must be [rows, width]")
+    S, shape = x_out.dtype, x_out.shape
+    T = f.dtype if f is not None else dy.dtype if dy is not None else torch.bfloat16
+    given = {"x": x_out, "f": f, "post": post, "alpha": alpha, "gate": gate, "scale": scale}
+    if grads is None:
+        grads = {n: None for n, t in given.items() if t is not None}
+        if shift is not False and shift is not None and (scale is not None or shift is not True):
+            grads["shift"] = None
+    given["shift"] = shift if hasattr(shift, "shape") else scale
+    for n in grads:
+        if n not in given or given[n] is None and grads[n] is None:
+            raise ValueError(f"no gradient of {n}: it is not given")
+    mod_shift = grads.get("shift") if grads.get("shift") is not None else given["shift"] if "shift" in grads else None
+    ptr, stride, mods = _modulation(x_out, post, alpha, gate, scale, mod_shift)
+    sizes = (_dtype_of("x_out", x_out), types.get(T, -1), *shape)
+    with _Placed(stream, x_out, dy, d_out, f, post, alpha, gate, scale, *grads.values()) as on:
+        out = {}
+        for n, t in grads.items():
+            like = given[n]
+            if t is None:
+                t = torch.empty(like.shape, dtype=S if n == "x" else T if n == "f" else torch.float32, device=x_out.device)
+            elif n not in ("x", "f", "shift") and t.shape != like.shape:
+                raise ValueError(f"the gradient of {n} must be {tuple(like.shape)}")
+            out[n] = t
+        xp, xs = _rows2("x_out", x_out, shape, S)
+        fp, fs = _rows2("f", f, shape, T)
+        norm = _pack_norm(*sizes, mods, group, eps, 0, 0 if f is not None else xp, fp, *ptr, xp if f is not None else 0, 0, xs, fs,
+                          xs, 0, *stride)
+        yp, ys = _rows2("dy", dy, shape, T)
+        dp, ds = _rows2("d_out", d_out, shape, S)
+        gx, gxs = _rows2("the gradient of x", out.get("x"), shape, S)
+        gf, gfs = _rows2("the gradient of f", out.get("f"), shape, T)
+        gp, gs, _ = _modulation(x_out, out.get("post"), out.get("alpha"), out.get("gate"), out.get("scale"), out.get("shift"))
+        tail = (ys, ds, gxs, gfs, *gs)
+        memory, ws, n = _scratch(lib.ravel_norm_residual_grad_workspace, norm, _pack_norm_grad(yp, dp, gx, gf, *gp, *tail, 0, 0))
+        _check(lib.ravel_norm_residual_grad(norm, _pack_norm_grad(yp, dp, gx, gf, *gp, *tail, ws, n), on.handle))
+    return out
+
+
+def _heads4(name, t, shape, dtype):
+    _like(name, t, shape, dtype)
+    return t.data_ptr(), t.stride()[:3]
+
+
+def _lengths(name, t, batch):
+    if t is None:
+        return 0
+    if t.dtype is not _layer_tools()[0].int32 or t.shape != (batch,) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor [{batch}]")
+    return t.data_ptr()
+
+
+def _cross_sizes(q, k, scale):
+    if q.dim() != 4 or k.dim() != 4 or k.shape[0] != q.shape[0] or k.shape[3] != q.shape[3]:
+        raise ValueError("q must be [batch, rows, n_q_heads, head_dim], k and v [batch, keys, n_kv_heads, head_dim]")
+    B, rows, nq, hd = q.shape
+    return (_dtype_of("q", q), B, nq, k.shape[2], hd, rows, k.shape[1], hd ** -0.5 if scale is None else scale)
+
+
+def cross_attention(q, k, v, q_len=None, k_len=None, scale=None, out=None, lse=None, stream=None):
+    """out = softmax(scale q k^T) v: q ``[batch, rows, n_q_heads, head_dim]`` over k, v ``[batch, keys, n_kv_heads,
+    head_dim]`` of one dtype; the first ``k_len`` keys and ``q_len`` rows of each batch row take part (int32 tensors
+    ``[batch]``; None: all), out is 0 for the other rows and where there are no keys.  ``lse``: float32 ``[batch,
+    n_q_heads, rows]`` that receives what the gradients need."""
+    torch, lib, _, _ = _layer_tools()
+    sizes = _cross_sizes(q, k, scale)
+    with _Placed(stream, q, k, v, q_len, k_len, out, lse) as on:
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        qp, qs = _heads4("q", q, q.shape, q.dtype)
+        kp, ks = _heads4("k", k, k.shape, q.dtype)
+        vp, vs = _heads4("v", v, k.shape, q.dtype)
+        op, os_ = _heads4("out", out, q.shape, q.dtype)
+        if lse is not None and (lse.shape != (sizes[1], sizes[2], sizes[5]) or lse.dtype is not torch.float32 or
+                                not lse.is_contiguous()):
+            raise ValueError(f"lse must be a contiguous float32 tensor {(sizes[1], sizes[2], sizes[5])}")
+        fields = (*sizes, _lengths("q_len", q_len, sizes[1]), _lengths("k_len", k_len, sizes[1]), qp, kp, vp, op,
+                  0 if lse is None else lse.data_ptr(), *qs, *ks, *vs, *os_)
+        memory, ws, n = _scratch(lib.ravel_cross_attention_workspace, _pack_cross(*fields, 0, 0))
+        _check(lib.ravel_cross_attention(_pack_cross(*fields, ws, n), on.handle))
+    return out
+
+
+def cross_attention_grad(q, k, v, out, lse, dout, q_len=None, k_len=None, scale=None, dq=None, dk=None, dv=None,
+                         need_q: bool = True, need_kv: bool = True, stream=None):
+    """(dq, dk, dv) from ``dout``, with cross_attention's ``out`` and ``lse``; what is not needed is None."""
+    torch, lib, _, _ = _layer_tools()
+    sizes = _cross_sizes(q, k, scale)
+    with _Placed(stream, q, k, v, out, lse, dout, q_len, k_len, dq, dk, dv) as on:
+        T, device = q.dtype, q.device
+        if lse.shape != (sizes[1], sizes[2], sizes[5]) or lse.dtype is not torch.float32 or not lse.is_contiguous():
+            raise ValueError(f"lse must be a contiguous float32 tensor {(sizes[1], sizes[2], sizes[5])}")
+        if not need_q:
+            dq = None
+        elif dq is None:
+            dq = torch.empty(q.shape, dtype=T, device=device)
+        if not need_kv:
+            dk = dv = None
+        else:
+            dk = torch.empty(k.shape, dtype=T, device=device) if dk is None else dk
+            dv = torch.empty(k.shape, dtype=T, device=device) if dv is None else dv
+        none = (0, (0, 0, 0))
+        qp, qs = _heads4("q", q, q.shape, T)
+        kp, ks = _heads4("k", k, k.shape, T)
+        vp, vs = _heads4("v", v, k.shape, T)
+        op, os_ = _heads4("out", out, q.shape, T)
+        dp, ds = _heads4("dout", dout, q.shape, T)
+        gq, gqs = none if dq is None else _heads4("dq", dq, q.shape, T)
+        gk, gks = none if dk is None else _heads4("dk", dk, k.shape, T)
+        gv, gvs = none if dv is None else _heads4("dv", dv, k.shape, T)
+        cross = _pack_cross(*sizes, _lengths("q_len", q_len, sizes[1]), _lengths("k_len", k_len, sizes[1]), qp, kp, vp, op,
+                            lse.data_ptr(), *qs, *ks, *vs, *os_, 0, 0)
+        fields = (dp, gq, gk, gv, *ds, *gqs, *gks, *gvs)
+        memory, ws, n = _scratch(lib.ravel_cross_attention_grad_workspace, cross, _pack_cross_grad(*fields, 0, 0))
+        _check(lib.ravel_cross_attention_grad(cross, _pack_cross_grad(*fields, ws, n), on.handle))
+    return dq, dk, dv
+
+
+def _mlp_sizes(x, wg, wu, act):
+    if x.dim() != 2 or wg.dim() != 2 or wg.shape[1] != x.shape[1]:
+        raise ValueError("x must be [rows, width], wg and wu [hidden, width]")
+    if act not in _ACTS:
+        raise ValueError(f"act must be one of {sorted(_ACTS)}, got {act!r}")
+    if wu.stride() != wg.stride():
+        raise ValueError("wg and wu must have the same strides")
+    return _dtype_of("x", x), _ACTS[act], x.shape[0], x.shape[1], wg.shape[0], 0
+
+
+def _pair(name, a, b, shape, dtype):
+    """(address, address, row stride) of two matrices of the same strides, or zeros for None."""
+    if a is None and b is None:
+        return 0, 0, 0
+    if a is None or b is None or a.stride() != b.stride():
+        raise ValueError(f"{name} must both be given, with the same strides, or both be None")
+    ap, stride = _rows2(name, a, shape, dtype)
+    return ap, _rows2(name, b, shape, dtype)[0], stride
+
+
+def gated_mlp(x, wg, wu, act: str = "gelu", h=None, gate=None, up=None, stream=None):
+    """h = act(x wg^T) * (x wu^T): x ``[rows, width]``, wg and wu ``[hidden, width]``, act "gelu" (tanh form) or "silu".
+    ``gate`` and ``up`` ``[rows, hidden]`` receive x wg^T and x wu^T, for the gradients."""
+    torch, lib, _, _ = _layer_tools()
+    sizes = _mlp_sizes(x, wg, wu, act)
+    with _Placed(stream, x, wg, wu, h, gate, up) as on:
+        T, shape = x.dtype, (x.shape[0], wg.shape[0])
+        if h is None:
+            h = torch.empty(shape, dtype=T, device=x.device)
+        xp, xs = _rows2("x", x, x.shape, T)
+        wp, vp, ws = _pair("wg and wu", wg, wu, wg.shape, T)
+        hp, hs = _rows2("h", h, shape, T)
+        gp, up_, gs = _pair("gate and up", gate, up, shape, T)
+        fields = (*sizes, xp, wp, vp, hp, gp, up_, xs, ws, hs, gs)
+        memory, at, n = _scratch(lib.ravel_gated_mlp_workspace, _pack_mlp(*fields, 0, 0))
+        _check(lib.ravel_gated_mlp(_pack_mlp(*fields, at, n), on.handle))
+    return h
+
+
+def gated_mlp_grad(x, wg, wu, gate, up, dh, act: str = "gelu", dx=None, dwg=None, dwu=None, need_x: bool = True,
+                   need_w: bool = True, weight_dtype=None, stream=None):
+    """(dx, dwg, dwu) from ``dh``, with gated_mlp's ``gate`` and ``up``; what is not needed is None.  The weights'
+    gradients have ``weight_dtype``: the weights' own (the default), or float32."""
+    torch, lib, types, _ = _layer_tools()
+    sizes = _mlp_sizes(x, wg, wu, act)
+    with _Placed(stream, x, wg, wu, gate, up, dh, dx, dwg, dwu) as on:
+        T, W, shape = x.dtype, (dwg.dtype if dwg is not None else weight_dtype or x.dtype), (x.shape[0], wg.shape[0])
+        if not need_x:
+            dx = None
+        elif dx is None:
+            dx = torch.empty(x.shape, dtype=T, device=x.device)
+        if not need_w:
+            dwg = dwu = None
+        else:
+            dwg = torch.empty(wg.shape, dtype=W, device=x.device) if dwg is None else dwg
+            dwu = torch.empty(wg.shape, dtype=W, device=x.device) if dwu is None else dwu
+        xp, xs = _rows2("x", x, x.shape, T)
+        wp, vp, ws = _pair("wg and wu", wg, wu, wg.shape, T)
+        gp, up_, gs = _pair("gate and up", gate, up, shape, T)
+        hp, hs = _rows2("dh", dh, shape, T)
+        dxp, dxs = _rows2("dx", dx, x.shape, T)
+        dgp, dup, dws = _pair("dwg and dwu", dwg, dwu, wg.shape, W)
+        mlp = _pack_mlp(*sizes, xp, wp, vp, 0, gp, up_, xs, ws, 0, gs, 0, 0)
+        fields = (types.get(W, -1), 0, hp, dxp, dgp, dup, hs, dxs, dws)
+        memory, at, n = _scratch(lib.ravel_gated_mlp_grad_workspace, mlp, _pack_mlp_grad(*fields, 0, 0))
+        _check(lib.ravel_gated_mlp_grad(mlp, _pack_mlp_grad(*fields, at, n), on.handle))
+    return dx, dwg, dwu
