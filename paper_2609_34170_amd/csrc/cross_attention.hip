@@ -78,7 +78,7 @@ RAVEL_DEV void load_keys(const Segments<T, HD * sizeof(T)>& at, const T* head, c
   for (int i = 0; i < Z::SEGS; ++i) {
     const int seg = wave * Z::SEGS + i;
     const T* const from = head + (int64_t)(first + seg * at.ROWS) * stride;
-    load_segment(buffer_until((const char*)from, (const char*)end), tile, seg, row + at.byte_of(seg));
+    load_segment(buffer_from(from, (const char*)end - (const char*)from), tile, seg, row + at.byte_of(seg));
   }
 }
 // Rows [first, first + TR) of a (batch row, KV head)'s row space; rows from `end` on are zeros.  head: row 0 of the first

@@ -58,39 +58,43 @@ __global__ __launch_bounds__(64 * WM * WN) void mlp_matrix_kernel(MatArgs a) {
   const int m0 = (tr - which * tiles_m) * BM, n0 = tc * BN;
   const int k0 = z * a.per, k1 = min(tiles_k * a.pairs, k0 + a.per);
 
-  // An operand's rows are its own (AC false) or the contraction's; its end is its last element's, rows behind it are
-  // zeros.  Columns behind a row's end read the next row: across the contraction they are outputs that are not
-  // stored, along it (the last tile) they are cut off.
+  // An operand's rows are its own (AC false) or the contraction's; behind its last element are zeros.  Columns
+  // behind a row's end read the next row: across the contraction they are outputs that are not stored, along it (the
+  // last tile) they are cut off.
   const Segments<T, RA> sa0(lane);
   const Segments<T, RBB> sb0(lane);
   const int lda = (int)a.lda * E, ldb = (int)a.ldb * E;
-  const auto issue = [&](int t, char* Ad, char* Bd) {
+  // bytes from a tile's first element to the operand's end, at k = 0, and bytes to the next tile
+  const int64_t a_left = AC ? (int64_t)(a.K - 1) * lda + (a.M - m0) * E : (int64_t)(a.M - 1 - m0) * lda + a.K * E;
+  const int64_t b_left = BC                ? (int64_t)(a.K - 1) * ldb + (a.N - n0) * E
+                         : MODE == FORWARD ? (int64_t)((a.N - n0) / 2 - 1) * ldb + a.K * E
+                                           : (int64_t)(a.N - 1 - n0) * ldb + a.K * E;
+  const int64_t a_next = AC ? (int64_t)BK * lda : 128, b_next = BC ? (int64_t)BK * ldb : 128;
+  const int64_t a_first = AC ? m0 * E : (int64_t)m0 * lda, b_first = BC ? n0 * E : (int64_t)(MODE == FORWARD ? n0 / 2 : n0) * ldb;
+  const auto issue = [&](int t, char* Ad, char* Bd) {  // behind the last tile: zeros
     const auto sa = sa0.fresh();
     const auto sb = sb0.fresh();
-    const unsigned ra = __umul24(sa.row, lda), rb = __umul24(sb.row, ldb);
-    const int pair = t >= tiles_k ? 1 : 0, k = (t - pair * tiles_k) * BK, left = (a.K - k) * E;
-    const char* const A = (const char*)a.A[MODE == BOTH ? which : pair];
-    const char* const A_end = A + (AC ? (int64_t)(a.K - 1) * lda + a.M * E : (int64_t)(a.M - 1) * lda + a.K * E);
+    const int pair = t >= tiles_k ? 1 : 0, kt = t - pair * tiles_k, left = a.K * E - kt * 128;
+    const rsrc_t fa = buffer_from((const char*)a.A[MODE == BOTH ? which : pair] + a_first + kt * a_next, t < k1 ? a_left - kt * a_next : 0);
+    const int ra = __umul24(sa.row, lda), rb = __umul24(sb.row, ldb);
 #pragma unroll
     for (int i = 0; i < SA; ++i) {
-      const int seg = wave * SA + i, r = seg * sa.ROWS, c = sa.byte_of(seg);
-      const rsrc_t from = buffer_until(A + (AC ? (int64_t)(k + r) * lda + m0 * E : (int64_t)(m0 + r) * lda + k * E), A_end);
-      load_segment(from, Ad, seg, AC || c < left ? ra + c : kOutside);
+      const int seg = wave * SA + i, c = sa.byte_of(seg);
+      load_segment(fa, Ad, seg, AC || c < left ? ra + c + seg * sa.ROWS * lda : kOutside);
     }
-    const char* const B = (const char*)a.B[MODE == STORE ? pair : 0];
+    const rsrc_t fb = buffer_from((const char*)a.B[MODE == STORE ? pair : 0] + b_first + kt * b_next, t < k1 ? b_left - kt * b_next : 0);
+    if constexpr (MODE == FORWARD) {  // rows 32 j .. + 15 of the tile: gate, the next 16: up weights of the same units
+      const rsrc_t fu = buffer_from((const char*)a.B[1] + b_first + kt * b_next, t < k1 ? b_left - kt * b_next : 0);
 #pragma unroll
-    for (int i = 0; i < SB; ++i) {
-      const int seg = wave * SB + i, c = sb.byte_of(seg);
-      if constexpr (MODE == FORWARD) {  // rows 32 j .. + 15 of the tile: gate, the next 16: up weights of the same units
-        const char* const W = (const char*)a.B[(seg >> 1) & 1];
-        const int u = n0 / 2 + (seg >> 2) * 16 + (seg & 1) * 8;
-        const rsrc_t from = buffer_until(W + (int64_t)u * ldb + k * E, W + (int64_t)(a.N / 2 - 1) * ldb + a.K * E);
-        load_segment(from, Bd, seg, c < left ? rb + c : kOutside);
-      } else {
-        const int r = seg * sb.ROWS;
-        const char* const B_end = B + (BC ? (int64_t)(a.K - 1) * ldb + a.N * E : (int64_t)(a.N - 1) * ldb + a.K * E);
-        const rsrc_t from = buffer_until(B + (BC ? (int64_t)(k + r) * ldb + n0 * E : (int64_t)(n0 + r) * ldb + k * E), B_end);
-        load_segment(from, Bd, seg, BC || c < left ? rb + c : kOutside);
+      for (int i = 0; i < SB; ++i) {
+        const int seg = wave * SB + i, c = sb.byte_of(seg), u = (seg >> 2) * 16 + (seg & 1) * 8;
+        load_segment(seg & 2 ? fu : fb, Bd, seg, c < left ? rb + c + u * ldb : kOutside);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < SB; ++i) {
+        const int seg = wave * SB + i, c = sb.byte_of(seg);
+        load_segment(fb, Bd, seg, BC || c < left ? rb + c + seg * sb.ROWS * ldb : kOutside);
       }
     }
   };
@@ -104,34 +108,48 @@ __global__ __launch_bounds__(64 * WM * WN) void mlp_matrix_kernel(MatArgs a) {
   TileLane<T, RBB, true> lb(lane);
   la.advance(AC ? 0 : wm * TM, AC ? wm * TM : 0);
   lb.advance(BC ? 0 : wn * TN, BC ? wn * TN : 0);
-  const auto compute = [&](const char* Ad, const char* Bd) {
+  // The contraction's steps are pipelined by one: the fragments of a tile's second step are read under the matrix
+  // instructions of its first, those of the next tile's first step under the second's.  Between the two the waves
+  // meet: by then every fragment of the tile is in registers, so its buffer takes the tile after the next.
+  constexpr int PRODUCTS = TM * TN * (E == 4 ? 4 : 1), READS = TM * (AC ? (E == 4 ? 4 : 2) : 1) + TN * (BC ? (E == 4 ? 4 : 2) : 1);
+  frag af[2][TM], bf[2][TN];
+  const auto read = [&](const char* Ad, const char* Bd, int s) {
     lds_char_t* const as = (lds_char_t*)Ad;
     lds_char_t* const bs = (lds_char_t*)Bd;
+    const auto ta = la.fresh();
+    const auto tb = lb.fresh();
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const auto ta = la.fresh();
-      const auto tb = lb.fresh();
-      frag af[TM], bf[TN];
+    for (int j = 0; j < TN; ++j) bf[s][j] = BC ? tb.along_col(bs, s, j) : tb.along_row(bs, j, s);
 #pragma unroll
-      for (int j = 0; j < TN; ++j) bf[j] = BC ? tb.along_col(bs, s, j) : tb.along_row(bs, j, s);
-#pragma unroll
-      for (int i = 0; i < TM; ++i) af[i] = AC ? ta.along_col(as, s, i) : ta.along_row(as, i, s);
-#pragma unroll
-      for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j) acc[i][j] = M::mma(bf[j], af[i], acc[i][j]);
-      __builtin_amdgcn_sched_barrier(0);  // the next step's fragments have no registers before these are used
-    }
+    for (int i = 0; i < TM; ++i) af[s][i] = AC ? ta.along_col(as, s, i) : ta.along_row(as, i, s);
   };
-  if (k0 < k1) issue(k0, As0, Bs0);
-  for (int t = k0; t < k1; t += 2) {  // two buffers: the next tile is in flight while one is multiplied
+  const auto multiply = [&](int s) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) acc[i][j] = M::mma(bf[s][j], af[s][i], acc[i][j]);
+  };
+  const auto tile = [&](int t, char* Ac, char* Bc, char* An, char* Bn) {
+    read(Ac, Bc, 1);
+    multiply(0);
+    spread<LDS_READS, READS, PRODUCTS>();
+    __builtin_amdgcn_sched_barrier(0);
     tile_barrier<0>();
-    if (t + 1 < k1) issue(t + 1, As1, Bs1);
-    compute(As0, Bs0);
-    if (t + 1 < k1) {
-      tile_barrier<0>();
-      if (t + 2 < k1) issue(t + 2, As0, Bs0);
-      compute(As1, Bs1);
+    issue(t + 2, Ac, Bc);
+    read(An, Bn, 0);                          // (what the buffer holds, not used)
+    multiply(1);
+    spread<GLOBAL_LOADS, SA + SB, PRODUCTS / 2>();
+    spread<LDS_READS, READS, PRODUCTS - PRODUCTS / 2>();
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  if (k0 < k1) {
+    issue(k0, As0, Bs0);
+    tile_barrier<0>();
+    issue(k0 + 1, As1, Bs1);
+    read(As0, Bs0, 0);
+    for (int t = k0; t < k1; t += 2) {
+      tile(t, As0, Bs0, As1, Bs1);
+      if (t + 1 < k1) tile(t + 1, As1, Bs1, As0, Bs0);
     }
   }
 
@@ -249,21 +267,29 @@ struct MatPlan {
 constexpr int kTile[3] = {256, 128, 64};
 int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
-// The largest tile that still gives every CU a block; then, with 64 x 64 ones and `split` allowed, ranges of the
-// contraction of at least 4 tiles.
+// Tile and ranges of the contraction by the time of the fullest CU: the blocks it gets, one behind the other or side by
+// side, times a block's work over its tile's rate; ranges cost the traffic of their sums.
 MatPlan plan_matrix(int64_t M, int64_t N, int64_t K, int pairs, int products, int elt, bool split) {
-  MatPlan p;
-  for (p.tile = elt == 4 ? 1 : 0; p.tile < 2; ++p.tile)
-    if ((int64_t)ceil_div(M, kTile[p.tile]) * ceil_div(N, kTile[p.tile]) * products >= 192) break;
-  const int64_t blocks = (int64_t)ceil_div(M, kTile[p.tile]) * ceil_div(N, kTile[p.tile]) * products;
-  const int tiles = ceil_div(K, 128 / elt) * pairs;
-  int s = split ? (int)(512 / blocks) : 1;
-  if (s > tiles / 4) s = tiles / 4;
-  if (s < 1) s = 1;
-  p.per = ceil_div(tiles, s);
-  if (p.per < 1) p.per = 1;
-  p.splits = tiles ? ceil_div(tiles, p.per) : 1;
-  return p;
+  constexpr double rate[3] = {1.0, 0.75, 0.5};  // of a CU, by tile
+  MatPlan best{};
+  double least = 0;
+  for (int t = elt == 4 ? 1 : 0; t < 3; ++t) {
+    const int64_t blocks = (int64_t)ceil_div(M, kTile[t]) * ceil_div(N, kTile[t]) * products;
+    const int tiles = ceil_div(K, 128 / elt) * pairs;
+    for (int s = 1; s <= (split ? 16 : 1); ++s) {
+      if (s > 1 && tiles / s < 4) break;
+      const int per = tiles ? ceil_div(tiles, s) : 1;
+      // in steps of a 64 x 64 block's tile: 0.07 us at a CU's full rate of such steps, 6 for a block's first loads and end
+      const double step = (kTile[t] / 64) * (kTile[t] / 64) / rate[t];
+      double cost = (double)((blocks * s + 255) / 256) * (per * step + 6);
+      if (s > 1) cost += 30 + (double)M * N * products * (s + 1) * 4 * 2 / 4e12 / 0.07e-6;
+      if (least == 0 || cost < least) {
+        least = cost;
+        best = {t, tiles ? ceil_div(tiles, per) : 1, per};
+      }
+    }
+  }
+  return best;
 }
 
 template <typename T, typename O, bool AC, bool BC, int MODE>

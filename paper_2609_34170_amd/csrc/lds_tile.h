@@ -141,10 +141,10 @@ struct Segments {
 RAVEL_DEV void load_segment(rsrc_t from, char* tile, int seg, unsigned offset) {
   __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_dst_t*)(tile + seg * 1024), 16, (int)offset, 0, 0, 0);
 }
-// what is readable from p on, up to `end` (uniform); reads behind it give 0
-RAVEL_DEV rsrc_t buffer_until(const char* p, const char* end) {
-  const int64_t n = end - p;
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), (short)0, n > 0x7fffffff ? 0x7fffffff : n < 0 ? 0 : (int)n, 0x00020000);
+// `bytes` readable bytes from p on, none if negative (uniform); reads behind them give 0
+RAVEL_DEV rsrc_t buffer_from(const void* p, int64_t bytes) {
+  const int n = bytes > 0x7fffffff ? 0x7fffffff : bytes < 0 ? 0 : (int)bytes;
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), (short)0, n, 0x00020000);
 }
 RAVEL_DEV int wave_index() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }  // (the compiler knows it uniform)
 
@@ -159,6 +159,19 @@ RAVEL_DEV void tile_barrier() {
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
   __atomic_signal_fence(__ATOMIC_SEQ_CST);
+}
+
+// Instructions of the region up to here in this order: N of a kind (LDS_READS, GLOBAL_LOADS), each followed by its share
+// of PRODUCTS matrix instructions, so that neither waits for the other's queue.
+enum { MATRIX = 0x8, GLOBAL_LOADS = 0x20, LDS_READS = 0x100 };
+template <int KIND, int N, int PRODUCTS, int I = 0>
+RAVEL_DEV void spread() {
+  if constexpr (I < N) {
+    constexpr int share = PRODUCTS * (I + 1) / N - PRODUCTS * I / N;
+    __builtin_amdgcn_sched_group_barrier(KIND, 1, 0);
+    if constexpr (share > 0) __builtin_amdgcn_sched_group_barrier(MATRIX, share, 0);
+    spread<KIND, N, PRODUCTS, I + 1>();
+  }
 }
 
 }  // namespace ravel
