@@ -186,6 +186,63 @@ __global__ __launch_bounds__(64 * WM * WN) void mlp_matrix_kernel(MatArgs a) {
   }
 }
 
+// Few rows (up to 16 MT): the weights are all there is to read, once, so nothing is staged.  A block takes 16 hidden
+// units, its eight waves a range of the contraction each, with every weight of the range (up to 512 bytes a row) requested
+// before the first is used; the waves' sums meet in LDS.
+template <typename T, int MT>
+__global__ __launch_bounds__(512) void mlp_rows_kernel(MatArgs a) {
+  typedef Mat<T> M;
+  typedef typename M::frag frag;
+  constexpr int E = sizeof(T), BATCH = MT == 4 ? 4 : 8;  // steps of 64 bytes requested at once
+  __shared__ f32x4_t part[8][2][MT][64];
+  const int lane = threadIdx.x & 63, wave = wave_index(), l16 = lane & 15, grp = lane >> 4;
+  const int hidden = a.N / 2, u0 = blockIdx.x * 16;
+  const int steps = (a.K * E + 63) / 64, per = (steps + 7) / 8;
+  const int s0 = wave * per, s1 = min(steps, s0 + per);
+  const int unit = min(u0 + l16, hidden - 1);
+  const T* const wg = (const T*)a.B[0] + unit * a.ldb;
+  const T* const wu = (const T*)a.B[1] + unit * a.ldb;
+  f32x4_t acc[2][MT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) acc[0][i] = acc[1][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  for (int s = s0; s < s1; s += BATCH) {
+    frag g[BATCH], u[BATCH], x[BATCH][MT];
+#pragma unroll
+    for (int j = 0; j < BATCH; ++j) {
+      const int k = ((s + j) * 4 + grp) * (16 / E);
+      const bool in = s + j < s1 && k < a.K;
+      g[j] = in ? *(const frag*)(wg + k) : frag{};
+      u[j] = in ? *(const frag*)(wu + k) : frag{};
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+        x[j][i] = in && i * 16 + l16 < a.M ? *(const frag*)((const T*)a.A[0] + (i * 16 + l16) * a.lda + k) : frag{};
+    }
+#pragma unroll
+    for (int j = 0; j < BATCH; ++j)
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        acc[0][i] = M::mma(g[j], x[j][i], acc[0][i]);
+        acc[1][i] = M::mma(u[j], x[j][i], acc[1][i]);
+      }
+  }
+#pragma unroll
+  for (int i = 0; i < MT; ++i) part[wave][0][i][lane] = acc[0][i], part[wave][1][i][lane] = acc[1][i];
+  __syncthreads();
+  const int i = threadIdx.x >> 6;  // 16 rows of the sums; lane: row l16, units 4 grp .. + 3
+  const int m = i * 16 + l16, n = u0 + grp * 4;
+  if (i >= MT || m >= a.M || n >= hidden) return;
+  f32x4_t g = part[0][0][i][lane], u = part[0][1][i][lane], h;
+#pragma unroll
+  for (int w = 1; w < 8; ++w) g += part[w][0][i][lane], u += part[w][1][i][lane];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) h[r] = act_f(g[r], a.act) * u[r];
+  put4((T*)a.C[0] + m * a.ldc + n, h);
+  if (a.C[1]) {
+    put4((T*)a.C[1] + m * a.ldg + n, g);
+    put4((T*)a.C[2] + m * a.ldg + n, u);
+  }
+}
+
 // Ranges of the contraction added in order.
 template <typename O>
 __global__ __launch_bounds__(256) void mlp_sum_kernel(const float* part, int splits, int64_t range, O* c0, O* c1, int64_t ldc,
@@ -268,9 +325,12 @@ constexpr int kTile[3] = {256, 128, 64};
 int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 // Tile and ranges of the contraction by the time of the fullest CU: the blocks it gets, one behind the other or side by
-// side, times a block's work over its tile's rate; ranges cost the traffic of their sums.
+// side, times a block's work; ranges cost the traffic of their sums.
 MatPlan plan_matrix(int64_t M, int64_t N, int64_t K, int pairs, int products, int elt, bool split) {
-  constexpr double rate[3] = {1.0, 0.75, 0.5};  // of a CU, by tile
+  // Measured with 64-wide tiles of the contraction: 1.85 us a tile of 256 x 256; 0.67 of 128 x 128 with two blocks side by
+  // side, 0.88 with one alone, which is worth 1.3 of them; 64 x 64 ones 0.25 side by side, the first two in the
+  // time of two.
+  constexpr double us[3] = {1.85, 0.67, 0.25}, alone[3] = {1.0, 1.3, 2.0};
   MatPlan best{};
   double least = 0;
   for (int t = elt == 4 ? 1 : 0; t < 3; ++t) {
@@ -279,10 +339,9 @@ MatPlan plan_matrix(int64_t M, int64_t N, int64_t K, int pairs, int products, in
     for (int s = 1; s <= (split ? 16 : 1); ++s) {
       if (s > 1 && tiles / s < 4) break;
       const int per = tiles ? ceil_div(tiles, s) : 1;
-      // in steps of a 64 x 64 block's tile: 0.07 us at a CU's full rate of such steps, 6 for a block's first loads and end
-      const double step = (kTile[t] / 64) * (kTile[t] / 64) / rate[t];
-      double cost = (double)((blocks * s + 255) / 256) * (per * step + 6);
-      if (s > 1) cost += 30 + (double)M * N * products * (s + 1) * 4 * 2 / 4e12 / 0.07e-6;
+      const double n = (double)((blocks * s + 255) / 256);
+      double cost = (n > alone[t] ? n : alone[t]) * per * us[t] * (elt == 4 ? 2.6 : 1) + n * 2;  // 2: a block's first loads and its end
+      if (s > 1) cost += 4 + (double)M * N * products * s * 8 / 4e6;       // a launch, and the sums there and back
       if (least == 0 || cost < least) {
         least = cost;
         best = {t, tiles ? ceil_div(tiles, per) : 1, per};
@@ -324,6 +383,13 @@ hipError_t forward(const ravel_mlp& m, hipStream_t s) {
   a.ldc = m.h_stride;
   a.ldg = m.gate_stride;
   a.act = m.act;
+  if (a.M <= 64) {
+    const dim3 grid((unsigned)ceil_div(m.hidden, 16));
+    if (a.M <= 16) mlp_rows_kernel<T, 1><<<grid, 512, 0, s>>>(a);
+    else if (a.M <= 32) mlp_rows_kernel<T, 2><<<grid, 512, 0, s>>>(a);
+    else mlp_rows_kernel<T, 4><<<grid, 512, 0, s>>>(a);
+    return hipGetLastError();
+  }
   const MatPlan p = plan_matrix(a.M, a.N, a.K, 1, 1, sizeof(T), false);
   a.splits = p.splits;
   a.per = p.per;
