@@ -17,7 +17,7 @@
 namespace ravel {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f, kLazy = 8.f;
 
 struct CrossArgs {
   ravel_cross c;
@@ -69,16 +69,17 @@ struct Tiles {
   static_assert(BYTES % 4096 == 0, "segments of four waves");
 };
 
-// Keys [first, first + TK) of one head into a tile; keys behind `end` (the last live key's end) are zeros.
+// Keys [first, first + TK) of one head into a tile; keys behind the head's last `bytes` are zeros.
 template <typename T, int HD, int TK>
-RAVEL_DEV void load_keys(const Segments<T, HD * sizeof(T)>& at, const T* head, const T* end, int stride, int first, char* tile, int wave) {
+RAVEL_DEV void load_keys(const Segments<T, HD * sizeof(T)>& at, const T* head, int64_t bytes, int stride, int first, char* tile, int wave) {
   typedef Tiles<T, HD, TK> Z;
-  const unsigned row = __umul24(at.row, stride * (unsigned)sizeof(T));
+  const int step = stride * (int)sizeof(T), row = __umul24(at.row, step);
+  const int64_t skip = (int64_t)first * step;
+  const rsrc_t from = buffer_from((const char*)head + skip, bytes - skip);
 #pragma unroll
   for (int i = 0; i < Z::SEGS; ++i) {
     const int seg = wave * Z::SEGS + i;
-    const T* const from = head + (int64_t)(first + seg * at.ROWS) * stride;
-    load_segment(buffer_from(from, (const char*)end - (const char*)from), tile, seg, row + at.byte_of(seg));
+    load_segment(from, tile, seg, row + at.byte_of(seg) + seg * at.ROWS * step);
   }
 }
 // Rows [first, first + TR) of a (batch row, KV head)'s row space; rows from `end` on are zeros.  head: row 0 of the first
@@ -131,12 +132,13 @@ __global__ __launch_bounds__(256, (4 * Tiles<T, HD, TK>::BYTES <= 65536 ? 2 : 1)
   const T* const q = (const T*)c.q + w.b * c.q_stride[0] + (int64_t)w.h * a.G * c.q_stride[2];
   const T* const k = (const T*)c.k + w.b * c.k_stride[0] + w.h * c.k_stride[2];
   const T* const v = (const T*)c.v + w.b * c.v_stride[0] + w.h * c.v_stride[2];
-  const T *const k_end = k + (int64_t)(klen - 1) * (int)c.k_stride[1] + HD, *const v_end = v + (int64_t)(klen - 1) * (int)c.v_stride[1] + HD;
+  const int64_t k_bytes = ((int64_t)(klen - 1) * (int)c.k_stride[1] + HD) * sizeof(T);
+  const int64_t v_bytes = ((int64_t)(klen - 1) * (int)c.v_stride[1] + HD) * sizeof(T);
   const Segments<T, RB> seg0(lane);
   const auto issue = [&](int t, char* kt, char* vt) {
     const auto seg = seg0.fresh();
-    load_keys<T, HD, TK>(seg, k, k_end, (int)c.k_stride[1], t * TK, kt, wave);
-    load_keys<T, HD, TK>(seg, v, v_end, (int)c.v_stride[1], t * TK, vt, wave);
+    load_keys<T, HD, TK>(seg, k, k_bytes, (int)c.k_stride[1], t * TK, kt, wave);
+    load_keys<T, HD, TK>(seg, v, v_bytes, (int)c.v_stride[1], t * TK, vt, wave);
   };
   if (t0 < t1) issue(t0, k0, v0);
 
@@ -196,26 +198,26 @@ __global__ __launch_bounds__(256, (4 * Tiles<T, HD, TK>::BYTES <= 65536 ? 2 : 1)
     for (int i = 0; i < MI; ++i) {
       float top = -INFINITY;
 #pragma unroll
-      for (int f = 0; f < NF; ++f) {
-        s[i][f] *= cs;
+      for (int f = 0; f < NF; ++f)
 #pragma unroll
         for (int r = 0; r < 4; ++r) top = fmaxf(top, s[i][f][r]);
-      }
       top = fmaxf(top, __shfl_xor(top, 16, 64));
-      top = fmaxf(top, __shfl_xor(top, 32, 64));
-      top = fmaxf(top, m[i]);
-      const float ref = top == -INFINITY ? 0.f : top, fall = __builtin_amdgcn_exp2f(m[i] - ref);
-      if (__any(top != m[i])) {
+      top = fmaxf(top, __shfl_xor(top, 32, 64)) * cs;
+      // The reference moves only where the maximum is past it by kLazy (log2 units): probabilities stay below 2^kLazy,
+      // and what was summed is scaled rarely.
+      if (__any(top > m[i] + kLazy)) {
+        const float to = fmaxf(m[i], top), fall = __builtin_amdgcn_exp2f(m[i] - (to == -INFINITY ? 0.f : to));
         l[i] *= fall;
 #pragma unroll
         for (int d = 0; d < DF; ++d) o[i][d] *= fall;
+        m[i] = to;
       }
-      m[i] = top;
+      const float ref = m[i] == -INFINITY ? 0.f : m[i];
 #pragma unroll
       for (int f = 0; f < NF; ++f)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          s[i][f][r] = __builtin_amdgcn_exp2f(s[i][f][r] - ref);
+          s[i][f][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][f][r], cs, -ref));
           l[i] += s[i][f][r];
         }
 #pragma unroll
@@ -345,12 +347,13 @@ __global__ __launch_bounds__(256, (4 * Tiles<T, HD, TK>::BYTES <= 65536 ? 2 : 1)
 
   const T* const k = (const T*)c.k + w.b * c.k_stride[0] + w.h * c.k_stride[2];
   const T* const v = (const T*)c.v + w.b * c.v_stride[0] + w.h * c.v_stride[2];
-  const T *const k_end = k + (int64_t)(klen - 1) * (int)c.k_stride[1] + HD, *const v_end = v + (int64_t)(klen - 1) * (int)c.v_stride[1] + HD;
+  const int64_t k_bytes = ((int64_t)(klen - 1) * (int)c.k_stride[1] + HD) * sizeof(T);
+  const int64_t v_bytes = ((int64_t)(klen - 1) * (int)c.v_stride[1] + HD) * sizeof(T);
   const Segments<T, RB> seg0(lane);
   const auto issue = [&](int t, char* kt, char* vt) {
     const auto seg = seg0.fresh();
-    load_keys<T, HD, TK>(seg, k, k_end, (int)c.k_stride[1], t * TK, kt, wave);
-    load_keys<T, HD, TK>(seg, v, v_end, (int)c.v_stride[1], t * TK, vt, wave);
+    load_keys<T, HD, TK>(seg, k, k_bytes, (int)c.k_stride[1], t * TK, kt, wave);
+    load_keys<T, HD, TK>(seg, v, v_bytes, (int)c.v_stride[1], t * TK, vt, wave);
   };
   if (t0 < t1) issue(t0, k0, v0);
 
@@ -429,7 +432,7 @@ __global__ __launch_bounds__(256, (4 * Tiles<T, HD, TK>::BYTES <= 65536 ? 2 : 1)
         for (int f = 0; f < FP; ++f)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const float pr = __builtin_amdgcn_exp2f(s[i][f][r] * cs - lse[i]);
+            const float pr = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][f][r], cs, -lse[i]));
             s[i][f][r] = pr * (dp[i][f][r] - D[i]);
           }
         ds[i] = M::operand(s[i]);
@@ -563,7 +566,7 @@ __global__ __launch_bounds__(256, (4 * Tiles<T, HD, TR>::BYTES <= 65536 && Tiles
         for (int f = 0; f < FP; ++f)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const float pr = __builtin_amdgcn_exp2f(s[i][f][r] * cs - le[f][r]);
+            const float pr = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][f][r], cs, -le[f][r]));
             s[i][f][r] = pr;
             dp[i][f][r] = pr * (dp[i][f][r] - Dr[f][r]);
           }
