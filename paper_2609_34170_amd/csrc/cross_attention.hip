@@ -48,6 +48,20 @@ RAVEL_DEV float dot16(bf16x8_t a, bf16x8_t b) {
   return s;
 }
 
+// A value of the four lanes that hold a column's parts (lanes l16 + 16 g), combined.
+RAVEL_DEV float column_max(float x) {
+  auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+RAVEL_DEV float column_sum(float x) {
+  auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
 // Block `id` of a launch: its tile, KV head, batch row and range, neighbours sharing a batch row and head (and their XCD's
 // L2).
 struct Work {
@@ -65,8 +79,7 @@ RAVEL_DEV Work work_of(const CrossArgs& a) {
 // K and V tiles (or q and dout): sizes and what a wave loads.
 template <typename T, int HD, int ROWS>
 struct Tiles {
-  static constexpr int RB = HD * sizeof(T), BYTES = ROWS * RB, SEGS = BYTES / 1024 / 4;  // segments per wave
-  static_assert(BYTES % 4096 == 0, "segments of four waves");
+  static constexpr int RB = HD * sizeof(T), BYTES = ROWS * RB, SEGS = (BYTES + 4095) / 4096;  // segments per wave
 };
 
 // Keys [first, first + TK) of one head into a tile; keys behind the head's last `bytes` are zeros.
@@ -79,6 +92,7 @@ RAVEL_DEV void load_keys(const Segments<T, HD * sizeof(T)>& at, const T* head, i
 #pragma unroll
   for (int i = 0; i < Z::SEGS; ++i) {
     const int seg = wave * Z::SEGS + i;
+    if (Z::BYTES % 4096 && seg * 1024 >= Z::BYTES) break;
     load_segment(from, tile, seg, row + at.byte_of(seg) + seg * at.ROWS * step);
   }
 }
@@ -96,6 +110,7 @@ RAVEL_DEV void load_rows(const Segments<T, HD * sizeof(T)>& at, const T* head, i
 #pragma unroll
   for (int i = 0; i < Z::SEGS; ++i) {
     const int seg = wave * Z::SEGS + i, r = seg * at.ROWS + at.row;
+    if (Z::BYTES % 4096 && seg * 1024 >= Z::BYTES) break;
     const unsigned x = rest + r, q = __umul24(x, sp.inv) >> 23, g = x - __umul24(q, sp.G);
     const unsigned off = __umul24(q, (unsigned)row_stride * (unsigned)sizeof(T)) + __umul24(g, head_stride * (unsigned)sizeof(T));
     load_segment(from, tile, seg, first + r < end ? off + at.byte_of(seg) : kOutside);
@@ -170,6 +185,8 @@ __global__ __launch_bounds__(256, (4 * Tiles<T, HD, TK>::BYTES <= 65536 ? 2 : 1)
   const auto step = [&](int t, const char* kc, const char* vc, char* kn, char* vn) {
     tile_barrier<0>();
     if (t + 1 < t1) issue(t + 1, kn, vn);
+    if (row0 >= live) return;  // (a wave without rows, or without keys in this tile, has loaded its part)
+    if (KW > 1 && t * TK + wk * TKW >= klen) return;
     lds_char_t* const kt = (lds_char_t*)kc + wk * TKW * RB;
     lds_char_t* const vt = (lds_char_t*)vc + wk * TKW * RB;
     if (t == ktiles - 1) {
@@ -201,8 +218,7 @@ __global__ __launch_bounds__(256, (4 * Tiles<T, HD, TK>::BYTES <= 65536 ? 2 : 1)
       for (int f = 0; f < NF; ++f)
 #pragma unroll
         for (int r = 0; r < 4; ++r) top = fmaxf(top, s[i][f][r]);
-      top = fmaxf(top, __shfl_xor(top, 16, 64));
-      top = fmaxf(top, __shfl_xor(top, 32, 64)) * cs;
+      top = column_max(top) * cs;
       // The reference moves only where the maximum is past it by kLazy (log2 units): probabilities stay below 2^kLazy,
       // and what was summed is scaled rarely.
       if (__any(top > m[i] + kLazy)) {
@@ -238,10 +254,7 @@ __global__ __launch_bounds__(256, (4 * Tiles<T, HD, TK>::BYTES <= 65536 ? 2 : 1)
     if (t + 1 < t1) step(t + 1, k1, v1, k0, v0);
   }
 #pragma unroll
-  for (int i = 0; i < MI; ++i) {
-    l[i] += __shfl_xor(l[i], 16, 64);
-    l[i] += __shfl_xor(l[i], 32, 64);
-  }
+  for (int i = 0; i < MI; ++i) l[i] = column_sum(l[i]);
   if constexpr (KW > 1) {  // the waves that share rows: wave wk = 0 takes their sum
     __syncthreads();
     const auto results = [&](int w) { return (float*)(w == 0 ? k0 : w == 1 ? v0 : w == 2 ? k1 : v1); };
@@ -325,23 +338,25 @@ __global__ __launch_bounds__(256) void cross_join_kernel(CrossArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// dq (and D): a wave owns 16 MI rows, the block walks the keys
+// dq (and D): KW waves share 16 MI rows and split a tile's keys between them, the block walks the keys
 // ---------------------------------------------------------------------------
-template <typename T, int HD, int MI, int TK>
+template <typename T, int HD, int MI, int KW, int TK>
 __global__ __launch_bounds__(256, (4 * Tiles<T, HD, TK>::BYTES <= 65536 ? 2 : 1)) void cross_dq_kernel(CrossArgs a) {
   typedef Tiles<T, HD, TK> Z;
   typedef Mat<T> M;
   typedef typename M::frag frag;
-  constexpr int RB = Z::RB, STEPS = RB / 64, DF = HD / 16, NP = TK / M::CK, FP = M::CK / 16;
+  constexpr int RB = Z::RB, STEPS = RB / 64, DF = HD / 16, TKW = TK / KW, NP = TKW / M::CK, FP = M::CK / 16;
+  static_assert(TKW % M::CK == 0 && (KW == 1 || 16 * MI * HD * 4 <= Z::BYTES), "whole contraction steps, a wave's sums in a tile");
   __shared__ __attribute__((aligned(1024))) char k0[Z::BYTES], v0[Z::BYTES], k1[Z::BYTES], v1[Z::BYTES];
 
   const int lane = threadIdx.x & 63, wave = wave_index(), l16 = lane & 15, grp = lane >> 4;
+  const int wk = wave % KW, wr = wave / KW;
   const ravel_cross& c = a.c;
   const ravel_cross_grad& g = a.g;
   const Work w = work_of(a);
   const int live = live_len(c.q_len, w.b, c.rows) * a.G, all = c.rows * a.G;
   const int klen = live_len(c.k_len, w.b, c.keys);
-  const int row0 = w.tile * (64 * MI) + wave * 16 * MI;
+  const int row0 = w.tile * (16 * MI * (4 / KW)) + wr * 16 * MI;
   const int ktiles = g.dq ? (klen + TK - 1) / TK : 0, per = (ktiles + a.splits - 1) / a.splits;
   const int t0 = min(ktiles, w.split * per), t1 = min(ktiles, t0 + per);
 
@@ -374,10 +389,9 @@ __global__ __launch_bounds__(256, (4 * Tiles<T, HD, TK>::BYTES <= 65536 ? 2 : 1)
       of[i][s] = in ? *(const frag*)(pd + e) : frag{};
       D[i] += dot16(of[i][s], in ? *(const frag*)(po + e) : frag{});
     }
-    D[i] += __shfl_xor(D[i], 16, 64);
-    D[i] += __shfl_xor(D[i], 32, 64);
+    D[i] = column_sum(D[i]);
     lse[i] = in ? c.lse[((size_t)w.b * c.n_q_heads + gh) * c.rows + qr] * kLog2e : INFINITY;
-    if (a.stat && grp == 0 && w.split == 0) {
+    if (a.stat && grp == 0 && wk == 0 && w.split == 0) {
       float* const p = a.stat + ((size_t)w.b * c.n_kv_heads + w.h) * a.padded + r;
       p[0] = lse[i];
       p[(size_t)c.batch * c.n_kv_heads * a.padded] = D[i];
@@ -392,18 +406,20 @@ __global__ __launch_bounds__(256, (4 * Tiles<T, HD, TK>::BYTES <= 65536 ? 2 : 1)
     for (int d = 0; d < DF; ++d) dq[i][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   const TileLane<T, RB> at0(lane);
 
-  f32x4_t start[TK / 16];  // as in the forward: keys that do not exist
+  f32x4_t start[TKW / 16];  // as in the forward: keys that do not exist
 #pragma unroll
-  for (int f = 0; f < TK / 16; ++f) start[f] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  for (int f = 0; f < TKW / 16; ++f) start[f] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   const auto step = [&](int t, const char* kc, const char* vc, char* kn, char* vn) {
     tile_barrier<0>();
     if (t + 1 < t1) issue(t + 1, kn, vn);
-    lds_char_t* const kt = (lds_char_t*)kc;
-    lds_char_t* const vt = (lds_char_t*)vc;
+    if (row0 >= live) return;  // (a wave without rows, or without keys in this tile, has loaded its part)
+    if (KW > 1 && t * TK + wk * TKW >= klen) return;
+    lds_char_t* const kt = (lds_char_t*)kc + wk * TKW * RB;
+    lds_char_t* const vt = (lds_char_t*)vc + wk * TKW * RB;
     if (t == ktiles - 1) {
-      const int left = klen - t * TK - grp * 4;
+      const int left = klen - t * TK - wk * TKW - grp * 4;
 #pragma unroll
-      for (int f = 0; f < TK / 16; ++f)
+      for (int f = 0; f < TKW / 16; ++f)
 #pragma unroll
         for (int r = 0; r < 4; ++r) start[f][r] = f * 16 + r < left ? 0.f : -INFINITY;
     }
@@ -448,6 +464,23 @@ __global__ __launch_bounds__(256, (4 * Tiles<T, HD, TK>::BYTES <= 65536 ? 2 : 1)
   for (int t = t0; t < t1; t += 2) {
     step(t, k0, v0, k1, v1);
     if (t + 1 < t1) step(t + 1, k1, v1, k0, v0);
+  }
+  if constexpr (KW > 1) {  // the waves that share rows: wave wk = 0 takes their sum
+    const auto sums = [&](int w) { return (float*)(w == 0 ? k0 : w == 1 ? v0 : w == 2 ? k1 : v1); };
+    __syncthreads();
+    if (wk > 0)
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int d = 0; d < DF; ++d) *(f32x4_t*)(sums(wave) + (i * DF + d) * 256 + lane * 4) = dq[i][d];
+    __syncthreads();
+    if (wk > 0) return;
+#pragma unroll
+    for (int j = 1; j < KW; ++j)
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int d = 0; d < DF; ++d) dq[i][d] += *(const f32x4_t*)(sums(wave + j) + (i * DF + d) * 256 + lane * 4);
   }
 #pragma unroll
   for (int i = 0; i < MI; ++i) {
@@ -537,6 +570,7 @@ __global__ __launch_bounds__(256, (4 * Tiles<T, HD, TR>::BYTES <= 65536 && Tiles
     tile_barrier<0>();
     if (t + 1 < t1) issue(t + 1, qn, on, sn);
     RAVEL_LDS const float* const st = (RAVEL_LDS const float*)sc + wr * TRW + grp * 4;
+    if (key0 >= klen || (RW > 1 && t * TR + wr * TRW >= live)) return;  // nothing for this wave
     lds_char_t* const qt = (lds_char_t*)qc + wr * TRW * RB;
     lds_char_t* const ot = (lds_char_t*)oc + wr * TRW * RB;
 #pragma unroll
@@ -635,6 +669,169 @@ __global__ __launch_bounds__(256, (4 * Tiles<T, HD, TR>::BYTES <= 65536 && Tiles
   }
 }
 
+// ---------------------------------------------------------------------------
+// all gradients where there are at most 16 KF keys: one pass over the rows
+// ---------------------------------------------------------------------------
+// Every row tile sees all keys, so its scores serve dq and, through LDS (the contraction over rows needs them as columns),
+// its share of dk and dv as well: q and dout are read once, not by two passes (with 16 keys of 256 dims 64 x 400 rows
+// take 19 us instead of 37).  A wave takes 16 rows, or where a tile has fewer than 64 a part of their dims; for dk and
+// dv the dims are dealt out to the waves.
+template <typename T, int HD, int KF, int TR>
+__global__ __launch_bounds__(256) void cross_few_keys_grad_kernel(CrossArgs a) {
+  typedef Tiles<T, HD, TR> Z;
+  typedef Tiles<T, HD, 32> ZK;
+  typedef Mat<T> M;
+  typedef typename M::frag frag;
+  constexpr int E = sizeof(T), RB = Z::RB, STEPS = RB / 64, DF = HD / 16, NK = 32 / M::CK, FP = M::CK / 16;
+  constexpr int RF = TR / 16, DW = 4 / RF, DQ = DF / DW < 1 ? 1 : DF / DW, DKV = (DF + 3) / 4;
+  constexpr int PB = 32 * E;  // bytes of a row of probabilities
+  __shared__ __attribute__((aligned(1024))) char kt[ZK::BYTES], vt[ZK::BYTES], qt[Z::BYTES], ot[Z::BYTES], pt[TR * PB], st[TR * PB];
+
+  const int lane = threadIdx.x & 63, wave = wave_index(), l16 = lane & 15, grp = lane >> 4;
+  const int rf = wave % RF, dw = wave / RF;
+  const ravel_cross& c = a.c;
+  const ravel_cross_grad& g = a.g;
+  const Work w = work_of(a);
+  const int klen = live_len(c.k_len, w.b, c.keys), all = c.rows * a.G;
+  const int live = klen > 0 ? live_len(c.q_len, w.b, c.rows) * a.G : 0;
+  const int rtiles = (all + TR - 1) / TR, per = (rtiles + a.splits - 1) / a.splits;
+  const int t0 = min(rtiles, w.split * per), t1 = min(rtiles, t0 + per);
+
+  const T* const k = (const T*)c.k + w.b * c.k_stride[0] + w.h * c.k_stride[2];
+  const T* const v = (const T*)c.v + w.b * c.v_stride[0] + w.h * c.v_stride[2];
+  const T* const q = (const T*)c.q + w.b * c.q_stride[0] + (int64_t)w.h * a.G * c.q_stride[2];
+  const T* const dout = (const T*)g.dout + w.b * g.dout_stride[0] + (int64_t)w.h * a.G * g.dout_stride[2];
+  const RowSpace space{a.G, ((1 << 23) + a.G - 1) / a.G};
+  const Segments<T, RB> seg(lane);
+  load_keys<T, HD, 32>(seg, k, ((int64_t)(klen - 1) * (int)c.k_stride[1] + HD) * E, (int)c.k_stride[1], 0, kt, wave);
+  load_keys<T, HD, 32>(seg, v, ((int64_t)(klen - 1) * (int)c.v_stride[1] + HD) * E, (int)c.v_stride[1], 0, vt, wave);
+  const TileLane<T, RB> at0(lane);
+  const TileLane<T, PB> ap0(lane);
+  const float cs = c.scale > 0.f ? c.scale * kLog2e : 1.f;
+  f32x4_t start[KF];  // keys that do not exist
+#pragma unroll
+  for (int f = 0; f < KF; ++f)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) start[f][r] = f * 16 + grp * 4 + r < klen ? 0.f : -INFINITY;
+  f32x4_t dk[DKV][KF], dv[DKV][KF];
+#pragma unroll
+  for (int d = 0; d < DKV; ++d)
+#pragma unroll
+    for (int f = 0; f < KF; ++f) dk[d][f] = dv[d][f] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+
+  for (int t = t0; t < t1; ++t) {
+    load_rows<T, HD, TR>(seg, q, c.q_stride[1], (int)c.q_stride[2], space, t * TR, live, qt, wave);
+    load_rows<T, HD, TR>(seg, dout, g.dout_stride[1], (int)g.dout_stride[2], space, t * TR, live, ot, wave);
+    const int r = t * TR + rf * 16 + l16, qr = r / a.G, gh = w.h * a.G + r - qr * a.G;
+    const bool in = r < live;
+    const T* const po = (const T*)c.out + w.b * c.out_stride[0] + qr * c.out_stride[1] + gh * c.out_stride[2];
+    frag of[STEPS], oo[STEPS];
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) oo[s] = in ? *(const frag*)(po + (s * 4 + grp) * (16 / E)) : frag{};
+    const float lse = in ? c.lse[((size_t)w.b * c.n_q_heads + gh) * c.rows + qr] * kLog2e : INFINITY;
+    tile_barrier<0>();
+    const auto at = at0.fresh();
+    float D = 0.f;
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+      of[s] = at.along_row((lds_char_t*)ot, rf, s);
+      D += dot16(of[s], oo[s]);
+    }
+    D = column_sum(D);
+    f32x4_t s[2], dp[2];
+#pragma unroll
+    for (int f = 0; f < 2; ++f) s[f] = dp[f] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int f = 0; f < KF; ++f) s[f] = start[f];
+#pragma unroll
+    for (int x = 0; x < STEPS; ++x) {
+      frag qf = at.along_row((lds_char_t*)qt, rf, x);
+      if (!(c.scale > 0.f)) qf = frag{};
+#pragma unroll
+      for (int f = 0; f < KF; ++f) {
+        s[f] = M::mma(at.along_row((lds_char_t*)kt, f, x), qf, s[f]);
+        dp[f] = M::mma(at.along_row((lds_char_t*)vt, f, x), of[x], dp[f]);
+      }
+    }
+#pragma unroll
+    for (int f = 0; f < KF; ++f)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[f][i], cs, -lse));
+        s[f][i] = p;
+        dp[f][i] = p * (dp[f][i] - D);
+      }
+    if (dw == 0) {  // columns 16 f + 4 grp .. + 3 of the row's probabilities and their gradients
+      const int row = rf * 16 + l16;
+#pragma unroll
+      for (int f = 0; f < 2; ++f) {
+        const int byte = (f * 16 + grp * 4) * E, to = row * PB + ((byte & ~15) ^ (swizzle<T, PB>(row) << 4)) + (byte & 15);
+        store_row4<T>((T*)(pt + to), s[f]);
+        store_row4<T>((T*)(st + to), dp[f]);
+      }
+    }
+    if (g.dq) {  // (every lane's fragments take part, also those of rows that do not exist)
+      T* const to = (T*)g.dq + w.b * g.dq_stride[0] + qr * g.dq_stride[1] + gh * g.dq_stride[2];
+#pragma unroll
+      for (int d = 0; d < DQ; ++d) {
+        const int df = dw * DQ + d;
+        if (df >= DF) continue;
+        f32x4_t dq = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < NK; ++j)
+          if (j * FP < KF) dq = M::mma(at.along_col((lds_char_t*)kt, j, df), M::operand(&dp[j * FP]), dq);
+        if (r < all) store_row4<T>(to + df * 16 + grp * 4, in ? dq * c.scale : f32x4_t{0.f, 0.f, 0.f, 0.f});
+      }
+    }
+    __syncthreads();
+    if (g.dk)
+#pragma unroll
+      for (int j = 0; j < TR / M::CK; ++j) {
+        const auto ap = ap0.fresh();
+        frag pf[KF], sf[KF];
+#pragma unroll
+        for (int f = 0; f < KF; ++f) {
+          pf[f] = ap.along_col((lds_char_t*)pt, j, f);
+          sf[f] = ap.along_col((lds_char_t*)st, j, f);
+        }
+#pragma unroll
+        for (int d = 0; d < DKV; ++d) {
+          const int df = wave + d * 4;
+          if (df >= DF) continue;
+          const frag qc = at.along_col((lds_char_t*)qt, j, df), oc = at.along_col((lds_char_t*)ot, j, df);
+#pragma unroll
+          for (int f = 0; f < KF; ++f) {
+            dv[d][f] = M::mma(oc, pf[f], dv[d][f]);
+            dk[d][f] = M::mma(qc, sf[f], dk[d][f]);
+          }
+        }
+      }
+    __syncthreads();
+  }
+  if (!g.dk) return;
+#pragma unroll
+  for (int f = 0; f < KF; ++f) {
+    const int key = f * 16 + l16;
+    if (key >= c.keys) continue;
+    const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
+    const size_t to = (((size_t)w.split * c.batch + w.b) * c.n_kv_heads + w.h) * c.keys + key;
+    T* const pk = (T*)g.dk + w.b * g.dk_stride[0] + key * g.dk_stride[1] + w.h * g.dk_stride[2];
+    T* const pv = (T*)g.dv + w.b * g.dv_stride[0] + key * g.dv_stride[1] + w.h * g.dv_stride[2];
+#pragma unroll
+    for (int d = 0; d < DKV; ++d) {
+      const int df = wave + d * 4, e = df * 16 + grp * 4;
+      if (df >= DF) continue;
+      if (a.part) {
+        *(f32x4_t*)(a.part + to * HD + e) = dk[d][f];
+        *(f32x4_t*)(a.part2 + to * HD + e) = dv[d][f];
+      } else {
+        store_row4<T>(pk + e, key < klen ? dk[d][f] * c.scale : zero);
+        store_row4<T>(pv + e, key < klen ? dv[d][f] : zero);
+      }
+    }
+  }
+}
+
 // Partial sums of ranges added in order: to (b, i, h, d) of a tensor whose index i takes the G heads of a KV head (dq) or
 // is a key (dk, dv: G = 1).
 struct SumArgs {
@@ -666,18 +863,24 @@ __global__ __launch_bounds__(256) void cross_sum_kernel(SumArgs x0, SumArgs x1) 
 // ---------------------------------------------------------------------------
 // plans
 // ---------------------------------------------------------------------------
-// Rows of a few-row block (its waves split the keys) and of a many-row block; tile heights.
+// Tile heights, the rows (or keys) of a wave in 16s, and how many waves of a block share theirs.
 template <typename T, int HD>
 struct Shape {
   static constexpr int RB = HD * sizeof(T);
-  static constexpr int MI = RB >= 1024 ? 1 : 2, TK = RB >= 256 ? 16384 / RB : 64;       // many rows: 128 a block
-  static constexpr int KW = RB >= 512 ? 2 : 4, TF = RB >= 256 ? 32768 / RB : 128;  // few: 16 * 4 / KW a block
-  static constexpr int BI = RB >= 512 ? 1 : 2;                          // gradients: 16-row (or -key) fragments of a wave
+  // many rows or keys a block: 128 in the forward (64 where 256 dims leave no registers for more), 64 BI in the gradients
+  static constexpr int MI = RB >= 512 ? 1 : 2, BI = RB >= 512 ? 1 : 2, TK = RB >= 256 ? 16384 / RB : 64;
+  // few: waves share rows and split tiles of up to 16 KB, of which each takes one contraction step at least
+  static constexpr int TF = RB >= 128 ? 16384 / RB : 128, KW = TF / Mat<T>::CK < 4 ? TF / Mat<T>::CK : 4;
+  // few keys in the gradients: the same over rows, tiles of up to 32 KB
+  static constexpr int TR = RB >= 256 ? 32768 / RB : 128, RW = TR / Mat<T>::CK < 4 ? TR / Mat<T>::CK : 4;
+  // up to 32 keys: rows of a tile
+  static constexpr int TS = RB >= 1024 ? 16 : RB >= 512 ? 32 : 64;
 };
 constexpr int kFill = 512;  // blocks that fill the chip, two a CU
 
-int ranges(int64_t blocks, int tiles, int least) {  // of `tiles` tiles, at least `least` each
-  int64_t s = kFill / (blocks < 1 ? 1 : blocks);
+// Ranges of `tiles` tiles, at least `least` tiles each, for `blocks` blocks to become `fill`.
+int ranges(int64_t blocks, int tiles, int least, int fill) {
+  int64_t s = fill / (blocks < 1 ? 1 : blocks);
   if (s > tiles / least) s = tiles / least;
   return s < 1 ? 1 : (int)(s > 64 ? 64 : s);
 }
@@ -693,12 +896,13 @@ template <typename T, int HD>
 Plan plan_forward(const ravel_cross& c) {
   typedef Shape<T, HD> S;
   const int all = c.rows * (c.n_q_heads / c.n_kv_heads);
+  const int64_t heads = (int64_t)c.batch * c.n_kv_heads;
   Plan p;
-  p.few = all <= 32;
+  // Waves that share rows read a tile's keys once instead of four times, and finish small calls sooner.
+  p.few = all <= 32 || heads * ((all + 64 * S::MI - 1) / (64 * S::MI)) < kFill / 2;
   const int per = p.few ? 16 * (4 / S::KW) : 64 * S::MI, tk = p.few ? S::TF : S::TK;
   p.tiles = (all + per - 1) / per;
-  const int64_t heads = (int64_t)c.batch * c.n_kv_heads;
-  p.splits = ranges(heads * p.tiles, (c.keys + tk - 1) / tk, p.few ? 2 : 4);
+  p.splits = ranges(heads * p.tiles, (c.keys + tk - 1) / tk, 4, p.few ? 3 * kFill : kFill);
   p.bytes = p.splits > 1 ? round256((size_t)p.splits * heads * all * (HD + 2) * 4) : 0;
   return p;
 }
@@ -730,7 +934,7 @@ hipError_t forward(const ravel_cross& c, hipStream_t s) {
 
 struct GradPlan {
   int qtiles, qsplits, ktiles, ksplits, padded;
-  bool few;  // keys
+  bool few_rows, few_keys, one_pass;
   size_t stat, part;
 };
 template <typename T, int HD>
@@ -739,16 +943,23 @@ GradPlan plan_grad(const ravel_cross& c, const ravel_cross_grad& g) {
   const int all = c.rows * (c.n_q_heads / c.n_kv_heads);
   const int64_t heads = (int64_t)c.batch * c.n_kv_heads;
   GradPlan p{};
-  const int per = 64 * S::BI;
+  if (c.keys > 0 && c.keys <= 32) {
+    p.one_pass = true;
+    p.ksplits = ranges(heads, (all + S::TS - 1) / S::TS, 1, kFill);
+    p.part = g.dk && p.ksplits > 1 ? round256((size_t)p.ksplits * heads * c.keys * HD * 4 * 2) : 0;
+    return p;
+  }
   p.padded = (all + 127) / 128 * 128;  // whole tiles of either pass: every row that one reads has its lse and D
+  p.few_rows = all <= 32 || heads * (p.padded / (64 * S::BI)) < kFill / 2;
+  const int per = p.few_rows ? 16 * (4 / S::KW) : 64 * S::BI, tk = p.few_rows ? S::TF : S::TK;
   p.qtiles = p.padded / per;
-  p.qsplits = g.dq ? ranges(heads * p.qtiles, (c.keys + S::TK - 1) / S::TK, 4) : 1;
+  p.qsplits = g.dq ? ranges(heads * ((all + per - 1) / per), (c.keys + tk - 1) / tk, 4, kFill) : 1;
   if (p.qsplits > 1) p.part = (size_t)p.qsplits * heads * all * HD * 4;
   if (g.dk) {
-    p.few = c.keys <= 16 * (4 / S::KW);
-    const int kper = p.few ? 16 * (4 / S::KW) : per, tr = p.few ? S::TF : S::TK;
+    p.few_keys = c.keys <= 64;
+    const int kper = p.few_keys ? 16 * (4 / S::RW) : 64 * S::BI, tr = p.few_keys ? S::TR : S::TK;
     p.ktiles = (c.keys + kper - 1) / kper;
-    p.ksplits = ranges(heads * p.ktiles, (all + tr - 1) / tr, p.few ? 1 : 4);
+    p.ksplits = ranges(heads * p.ktiles, (all + tr - 1) / tr, p.few_keys ? 1 : 4, kFill);
     p.stat = round256((size_t)heads * p.padded * 2 * 4);
     if (p.ksplits > 1) {
       const size_t n = (size_t)p.ksplits * heads * c.keys * HD * 4 * 2;
@@ -757,6 +968,23 @@ GradPlan plan_grad(const ravel_cross& c, const ravel_cross_grad& g) {
   }
   p.part = round256(p.part);
   return p;
+}
+
+// dk and dv from the ranges' sums
+template <typename T>
+hipError_t sum_keys(const CrossArgs& a, hipStream_t s) {
+  const ravel_cross& c = a.c;
+  const ravel_cross_grad& g = a.g;
+  SumArgs x{a.part, g.dk, {g.dk_stride[0], g.dk_stride[1], g.dk_stride[2]}, a.splits, c.batch, c.n_kv_heads, c.keys, 1, c.head_dim,
+            c.k_len, c.keys, c.scale};
+  SumArgs y = x;
+  y.part = a.part2;
+  y.to = g.dv;
+  for (int i = 0; i < 3; ++i) y.stride[i] = g.dv_stride[i];
+  y.scale = 1.f;
+  const int64_t n = (int64_t)c.batch * c.n_kv_heads * c.keys * (c.head_dim / 4);
+  cross_sum_kernel<T><<<dim3((unsigned)((n + 255) / 256), 2), 256, 0, s>>>(x, y);
+  return hipGetLastError();
 }
 
 template <typename T, int HD>
@@ -772,11 +1000,28 @@ hipError_t gradients(const ravel_cross& c, const ravel_cross_grad& g, hipStream_
   float* const part = (float*)((char*)g.workspace + p.stat);
   const int64_t heads = (int64_t)c.batch * c.n_kv_heads, all = (int64_t)c.rows * a.G;
   hipError_t e;
+  if (p.one_pass) {
+    a.tiles = 1;
+    a.splits = p.ksplits;
+    a.part = p.ksplits > 1 ? part : nullptr;
+    a.part2 = part + (size_t)p.ksplits * heads * c.keys * HD;
+    const dim3 grid((unsigned)(heads * a.splits));
+    if (c.keys <= 16)
+      cross_few_keys_grad_kernel<T, HD, 1, S::TS><<<grid, 256, 0, s>>>(a);
+    else
+      cross_few_keys_grad_kernel<T, HD, 2, S::TS><<<grid, 256, 0, s>>>(a);
+    if ((e = hipGetLastError()) != hipSuccess || !g.dk || p.ksplits == 1) return e;
+    return sum_keys<T>(a, s);
+  }
   if (all > 0) {
     a.tiles = p.qtiles;
     a.splits = p.qsplits;
     a.part = p.qsplits > 1 ? part : nullptr;
-    cross_dq_kernel<T, HD, S::BI, S::TK><<<dim3((unsigned)(heads * a.tiles * a.splits)), 256, 0, s>>>(a);
+    const dim3 grid((unsigned)(heads * a.tiles * a.splits));
+    if (p.few_rows)
+      cross_dq_kernel<T, HD, 1, S::KW, S::TF><<<grid, 256, 0, s>>>(a);
+    else
+      cross_dq_kernel<T, HD, S::BI, 1, S::TK><<<grid, 256, 0, s>>>(a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     if (a.part) {
       const SumArgs x{part, g.dq, {g.dq_stride[0], g.dq_stride[1], g.dq_stride[2]}, p.qsplits, c.batch, c.n_kv_heads,
@@ -791,20 +1036,12 @@ hipError_t gradients(const ravel_cross& c, const ravel_cross_grad& g, hipStream_
   a.part = p.ksplits > 1 ? part : nullptr;
   a.part2 = part + (size_t)p.ksplits * heads * c.keys * HD;
   const dim3 grid((unsigned)(heads * a.tiles * a.splits));
-  if (p.few)
-    cross_dkv_kernel<T, HD, 1, S::KW, S::TF><<<grid, 256, 0, s>>>(a);
+  if (p.few_keys)
+    cross_dkv_kernel<T, HD, 1, S::RW, S::TR><<<grid, 256, 0, s>>>(a);
   else
     cross_dkv_kernel<T, HD, S::BI, 1, S::TK><<<grid, 256, 0, s>>>(a);
   if ((e = hipGetLastError()) != hipSuccess || !a.part) return e;
-  SumArgs x{part, g.dk, {g.dk_stride[0], g.dk_stride[1], g.dk_stride[2]}, p.ksplits, c.batch, c.n_kv_heads, c.keys, 1, HD,
-            c.k_len, c.keys, c.scale};
-  SumArgs y = x;
-  y.part = a.part2;
-  y.to = g.dv;
-  for (int i = 0; i < 3; ++i) y.stride[i] = g.dv_stride[i];
-  y.scale = 1.f;
-  cross_sum_kernel<T><<<dim3((unsigned)((heads * c.keys * (HD / 4) + 255) / 256), 2), 256, 0, s>>>(x, y);
-  return hipGetLastError();
+  return sum_keys<T>(a, s);
 }
 
 template <typename F>
