@@ -26,12 +26,28 @@ RAVEL_DEV f32x4_t rounded(f32x4_t v, const bf16_t*) {
 RAVEL_DEV f32x4_t all4(float v) { return f32x4_t{v, v, v, v}; }
 RAVEL_DEV float sum4(f32x4_t v) { return (v[0] + v[1]) + (v[2] + v[3]); }
 
+// Sum over the wave's lanes without LDS: rotations inside its rows of 16, then the rows.
+template <int ROTATE>
+RAVEL_DEV float plus_rotated(float v) {
+  return v + __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x120 + ROTATE, 0xf, 0xf, true));
+}
+RAVEL_DEV float lanes_sum(float v) {
+  v = plus_rotated<8>(v);
+  v = plus_rotated<4>(v);
+  v = plus_rotated<2>(v);
+  v = plus_rotated<1>(v);
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
 // Sums over the TPR threads of a row.  `slot` alternates between consecutive calls (0, 1, 0, ...), so that one
 // barrier a call is enough.
 template <int TPR, int N>
 RAVEL_DEV void row_sum(float (&v)[N], float (*part)[TPR / 64][4], int slot) {
 #pragma unroll
-  for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
+  for (int i = 0; i < N; ++i) v[i] = lanes_sum(v[i]);
   if constexpr (TPR > 64) {
     const int wave = threadIdx.x >> 6;
     if ((threadIdx.x & 63) == 0)
@@ -108,10 +124,11 @@ __global__ __launch_bounds__(TPR * rows_per_block<TPR>()) void norm_residual_ker
 }
 
 // How the rows are dealt out.  Row i of modulation row m (i < count) is row (i / group) * group * mods + m * group +
-// i % group where that is below rows.  A worker takes `per` modulation rows whole (segs 1), or rows [s seg, (s + 1) seg)
-// of one.
+// i % group where that is below rows.  Worker k takes modulation rows k, k + workers, ... whole (segs 1), or rows s, s +
+// segs, ... of row m (k = m segs + s): at any time all workers are at neighbouring rows.  (Runs of rows a worker, spread
+// over the whole tensors, took 76 us instead of 69 for 6400 x 2048.)
 struct GradPlan {
-  int mods, group, count, per, segs, seg, workers;
+  int mods, group, count, segs, workers;
   // where the sums go: to their place (one worker), or to the workspace, to be added
   bool mod_part, all_part;
   bool all[3];  // gate, scale, shift: summed over all rows
@@ -120,8 +137,6 @@ struct GradPlan {
   float* partial[5];  // the workspace's sums of dgate, dscale, dshift, dpost, dalpha; null: none
   size_t bytes;
 };
-
-int threads_per_row(int width) { return width <= 1024 ? 64 : width <= 4096 ? 256 : 512; }
 
 GradPlan grad_plan(const ravel_norm& n, const ravel_norm_grad& g) {
   GradPlan p{};
@@ -139,25 +154,15 @@ GradPlan grad_plan(const ravel_norm& n, const ravel_norm_grad& g) {
   if (p.group < 1) p.group = 1;
   const long long cycle = (long long)p.group * p.mods, rest = n.rows % cycle;
   p.count = (int)(n.rows / cycle * p.group + (rest < p.group ? rest : p.group));
-  // At least 4 rows a worker, so that its sums are few beside its rows; 8 waves a CU keep enough loads in flight.
-  const int most = n.width <= 1024 ? 2048 : n.width <= 4096 ? 768 : 512;
+  // At least 4 rows a worker, so that its sums are few beside its rows, and no more workers than run at once (two waves a
+  // SIMD): 914 of 256 threads, where 512 fit, took 96 us for 6400 x 2048, 512 took 90.
+  const int most = n.width <= 256 ? 4096 : n.width <= 512 ? 2048 : n.width <= 1024 ? 1024 : n.width <= 2048 ? 512 : 256;
   const int rows = n.rows > p.mods ? n.rows : p.mods;
   int want = (rows + 3) / 4;
   want = want < 1 ? 1 : want > most ? most : want;
-  if (p.mods >= want) {
-    p.per = (p.mods + want - 1) / want;
-    p.segs = 1;
-    p.seg = p.count;
-    p.workers = (p.mods + p.per - 1) / p.per;
-  } else {
-    p.per = 1;
-    const int segs = want / p.mods;
-    p.seg = (p.count + segs - 1) / segs;
-    if (p.seg < 1) p.seg = 1;
-    p.segs = (p.count + p.seg - 1) / p.seg;
-    if (p.segs < 1) p.segs = 1;
-    p.workers = p.mods * p.segs;
-  }
+  p.segs = want / p.mods < p.count ? want / p.mods : p.count;
+  if (p.segs < 1) p.segs = 1;
+  p.workers = p.mods >= want ? want : p.mods * p.segs;
   p.mod_part = any_mod && p.segs > 1;
   p.all_part = any_all && p.workers > 1;
   float* const dst[5] = {g.dgate, g.dscale, g.dshift, g.dpost, g.dalpha};
@@ -182,120 +187,152 @@ GradPlan grad_plan(const ravel_norm& n, const ravel_norm_grad& g) {
   return p;
 }
 
+// A row of a tensor as a buffer: what lies behind its width, or the whole of an absent row, reads as 0 and is not stored.
+struct RowBuffer {
+  __amdgpu_buffer_rsrc_t r;
+  RAVEL_DEV RowBuffer(const void* p, long long stride, long long row, int width, int elt, bool there) {
+    r = __builtin_amdgcn_make_buffer_rsrc((char*)const_cast<void*>(p) + row * stride * elt, (short)0, p && there ? width * elt : 0,
+                                          0x00020000);
+  }
+  template <typename T> RAVEL_DEV f32x4_t load(int col) const {
+    if constexpr (sizeof(T) == 4) return __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(r, col * 4, 0, 0));
+    const u32x2_t w = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_raw_buffer_load_b64(r, col * 2, 0, 0));
+    return f32x4_t{__uint_as_float(w[0] << 16), __uint_as_float(w[0] & 0xFFFF0000u), __uint_as_float(w[1] << 16),
+                   __uint_as_float(w[1] & 0xFFFF0000u)};
+  }
+  template <typename T> RAVEL_DEV void store(int col, f32x4_t v) const {
+    if constexpr (sizeof(T) == 4) {
+      __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, v), r, col * 4, 0, 0);
+    } else {
+      __builtin_amdgcn_raw_buffer_store_b64(u32x2_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])}, r, col * 2, 0, 0);
+    }
+  }
+};
+
 // dn = dy (1 + scale); dt = d_out + r (dn - n mean(dn n)) with n = t r; dF = alpha gate dt; and through the block
 // output's own norm, m = f rf, dm = dF (1 + post): df = rf (dm - m mean(dm m)).  The sums of t^2, dn t and f^2 are
 // formed together; the last one needs dt and comes second.
+//
+// All loads of a row are issued a row ahead (beyond 4096 elements, where registers do not hold two rows, at its start).  Loads and stores are waited for in the order of their issue, and the
+// compiler waits for as many as are certain to have been issued: a row therefore has no branch, only buffers of no
+// length for what is not there (with branches around its stores every row waited for the one before to be stored: 69 us
+// instead of 53 for 6400 x 2048: 4.4 TB/s).
 template <typename S, typename T, int TPR, int NC>
 __global__ __launch_bounds__(TPR * rows_per_block<TPR>()) void norm_residual_grad_kernel(ravel_norm a, ravel_norm_grad g,
                                                                                       GradPlan p) {
   __shared__ float part[2][TPR / 64][4];
   const int lane = threadIdx.x % TPR;
-  const int worker = blockIdx.x * rows_per_block<TPR>() + threadIdx.x / TPR;
+  const int worker = __builtin_amdgcn_readfirstlane(blockIdx.x * rows_per_block<TPR>() + threadIdx.x / TPR);
   if (worker >= p.workers) return;  // a whole wave; blocks of one worker have none
-  const int m_beg = p.segs > 1 ? worker / p.segs : worker * p.per;
-  const int m_end = min(p.mods, p.segs > 1 ? m_beg + 1 : m_beg + p.per);
-  const int i_beg = p.segs > 1 ? worker % p.segs * p.seg : 0, i_end = min(p.count, i_beg + p.seg);
+  const int m_step = p.segs > 1 ? p.mods : p.workers, i_beg = worker % p.segs;
   const long long cycle = (long long)p.group * p.mods;
-  const S* const t_in = (const S*)(a.f ? a.x_out : a.x);
+  const void* const t_in = a.f ? a.x_out : a.x;
   const long long t_stride = a.f ? a.x_out_stride : a.x_stride;
   const float alpha = a.f && a.alpha ? *a.alpha : 1.f, inv = 1.f / a.width;
-  const bool want_f = a.f && (g.df || g.dpost || g.dgate || g.dalpha);
+  const bool want_f = a.f && (g.df || g.dpost || g.dgate || g.dalpha), second = a.post && g.df;
+  const float post_of = a.post ? 1.f : 0.f, gate_of = a.gate ? 0.f : 1.f;
 
-  f32x4_t s_gate[NC], s_scale[NC], s_shift[NC], s_post[NC];
+  f32x4_t s_gate[NC], s_scale[NC], s_shift[NC], s_post[NC], post1[NC];
   float s_alpha = 0.f;
 #pragma unroll
-  for (int c = 0; c < NC; ++c) s_gate[c] = s_scale[c] = s_shift[c] = s_post[c] = all4(0.f);
-  // one of the three sums to its place, and from 0 on again
-  const auto flush = [&](float* to, long long stride, size_t at, f32x4_t(&s)[NC]) {
+  for (int c = 0; c < NC; ++c) {
+    s_gate[c] = s_scale[c] = s_shift[c] = s_post[c] = all4(0.f);
+    post1[c] = RowBuffer(a.post, 0, 0, a.width, 4, true).load<float>((c * TPR + lane) * 4) + 1.f;
+  }
+  struct Row {
+    f32x4_t t[NC], dy[NC], dt[NC], f[NC], gate[NC], scale[NC];
+  } next;
+  const auto row_of = [&](int m, int i) { return i / p.group * cycle + (long long)m * p.group + i % p.group; };
+  const auto fetch = [&](int m, int i) {
+    const long long row = m < p.mods && i < p.count ? row_of(m, i) : a.rows;
+    const long long mod = (row / a.group) % a.mods;
+    const bool in = row < a.rows;
+    const RowBuffer t(t_in, t_stride, row, a.width, sizeof(S), in), dy(g.dy, g.dy_stride, row, a.width, sizeof(T), in),
+        dt(g.d_out, g.d_out_stride, row, a.width, sizeof(S), in), f(a.f, a.f_stride, row, a.width, sizeof(T), in && want_f),
+        gate(a.gate, a.gate_stride, mod, a.width, 4, in && want_f), scale(a.scale, a.scale_stride, mod, a.width, 4, in);
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
       const int col = (c * TPR + lane) * 4;
-      if (to && col < a.width) store4(to + at * stride + col, s[c]);
-      s[c] = all4(0.f);
+      next.t[c] = t.template load<S>(col);
+      next.dy[c] = dy.template load<T>(col);
+      next.dt[c] = dt.template load<S>(col);
+      next.f[c] = f.template load<T>(col);
+      next.gate[c] = gate.template load<float>(col);
+      next.scale[c] = scale.template load<float>(col);
+    }
+  };
+  // a modulation row's sum to its place, and from 0 on again; nothing where it is summed over all rows
+  const auto flush = [&](float* to, long long stride, int at, bool now, f32x4_t(&s)[NC]) {
+    const RowBuffer out(to, stride, at, a.width, 4, now);
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      out.template store<float>((c * TPR + lane) * 4, s[c]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[c][e] = now ? 0.f : s[c][e];
     }
   };
 
-  for (int m = m_beg; m < m_end; ++m) {
-    for (int i = i_beg; i < i_end; ++i) {
-      const long long row = i / p.group * cycle + (long long)m * p.group + i % p.group;
-      if (row >= a.rows) break;
-      const size_t mod = (row / a.group) % a.mods;
-      f32x4_t t[NC], dn[NC], dt[NC], f[NC], gate[NC];
-      float v[3] = {0.f, 0.f, 0.f};
+  constexpr bool AHEAD = NC < 4;
+  int m = worker / p.segs, i = i_beg;
+  if constexpr (AHEAD) fetch(m, i);
+  while (m < p.mods) {
+    if constexpr (!AHEAD) fetch(m, i);
+    const long long row = i < p.count ? row_of(m, i) : a.rows;
+    const bool in = row < a.rows;
+    const int i_next = i + p.segs;
+    const bool last = i_next >= p.count;
+    f32x4_t t[NC], dn[NC], dt[NC], f[NC], gate[NC], dy[NC], dm[NC];
+    float v[3] = {0.f, 0.f, 0.f};
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        const int col = (c * TPR + lane) * 4;
-        t[c] = dn[c] = dt[c] = f[c] = all4(0.f);
-        gate[c] = all4(1.f);
-        if (col < a.width) {
-          t[c] = load4(t_in + row * t_stride + col);
-          if (g.dy) dn[c] = load4((const T*)g.dy + row * g.dy_stride + col);
-          if (g.d_out) dt[c] = load4((const S*)g.d_out + row * g.d_out_stride + col);
-          if (want_f) f[c] = load4((const T*)a.f + row * a.f_stride + col);
-          if (want_f && a.gate) gate[c] = load4(a.gate + mod * a.gate_stride + col);
-        }
-      }
-      f32x4_t dy[NC];
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        const int col = (c * TPR + lane) * 4;
-        dy[c] = dn[c];
-        if (a.scale && col < a.width) dn[c] = dn[c] * (load4(a.scale + mod * a.scale_stride + col) + 1.f);
-        v[0] += sum4(t[c] * t[c]);
-        v[1] += sum4(dn[c] * t[c]);
-        v[2] += sum4(f[c] * f[c]);
-      }
-      row_sum<TPR>(v, part, 0);
-      const float r = 1.f / sqrtf(v[0] * inv + a.eps), k = r * r * (v[1] * inv);
-      const float rf = a.post ? 1.f / sqrtf(v[2] * inv + a.eps) : 1.f;
-      float u[1] = {0.f};
-      f32x4_t dm[NC];
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        const int col = (c * TPR + lane) * 4;
-        const bool in = col < a.width;
-        dt[c] += r * (dn[c] - k * t[c]);
-        if (in && g.dx) store4((S*)g.dx + row * g.dx_stride + col, dt[c]);
-        s_scale[c] += dy[c] * (t[c] * r);
-        s_shift[c] += dy[c];
-        if (want_f) {
-          f[c] *= rf;  // m
-          const f32x4_t post1 = a.post && in ? load4(a.post + col) + 1.f : all4(1.f);
-          const f32x4_t d = dt[c] * f[c] * post1;  // dt F
-          s_gate[c] += alpha * d;
-          s_alpha += sum4(d * gate[c]);
-          dm[c] = alpha * gate[c] * dt[c];  // dF
-          s_post[c] += dm[c] * f[c];
-          dm[c] *= post1;
-          u[0] += sum4(dm[c] * f[c]);
-        }
-      }
-      if (a.post && g.df) row_sum<TPR>(u, part, 1);
-      if (g.df)
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-          const int col = (c * TPR + lane) * 4;
-          if (col >= a.width) continue;
-          const f32x4_t d = a.post ? rf * (dm[c] - (u[0] * inv) * f[c]) : dm[c];
-          store4((T*)g.df + row * g.df_stride + col, d);
-        }
-      if constexpr (TPR > 64)
-        if (!(a.post && g.df)) __syncthreads();  // the next row's first sum uses slot 0 again
+    for (int c = 0; c < NC; ++c) {
+      t[c] = next.t[c], dy[c] = next.dy[c], dt[c] = next.dt[c], f[c] = next.f[c], gate[c] = next.gate[c] + gate_of;
+      dn[c] = dy[c] * (next.scale[c] + 1.f);
     }
-    const size_t at = p.mod_part ? worker : m;
-    if (!p.all[0]) flush(p.gate, p.gate_stride, at, s_gate);
-    if (!p.all[1]) flush(p.scale, p.scale_stride, at, s_scale);
-    if (!p.all[2]) flush(p.shift, p.shift_stride, at, s_shift);
+    if constexpr (AHEAD) fetch(last ? m + m_step : m, last ? i_beg : i_next);
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      v[0] += sum4(t[c] * t[c]);
+      v[1] += sum4(dn[c] * t[c]);
+      v[2] += sum4(f[c] * f[c]);
+    }
+    row_sum<TPR>(v, part, 0);
+    const float r = 1.f / sqrtf(v[0] * inv + a.eps), k = r * r * (v[1] * inv);
+    const float rf = post_of != 0.f ? 1.f / sqrtf(v[2] * inv + a.eps) : 1.f;
+    const RowBuffer dx(g.dx, g.dx_stride, row, a.width, sizeof(S), in), df(g.df, g.df_stride, row, a.width, sizeof(T), in);
+    float u[1] = {0.f};
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      dt[c] += r * (dn[c] - k * t[c]);
+      dx.template store<S>((c * TPR + lane) * 4, dt[c]);
+      s_scale[c] += dy[c] * (t[c] * r);
+      s_shift[c] += dy[c];
+      f[c] *= rf;                                // m
+      const f32x4_t d = dt[c] * f[c] * post1[c];  // dt F
+      s_gate[c] += alpha * d;
+      s_alpha += sum4(d * gate[c]);
+      dm[c] = alpha * gate[c] * dt[c];  // dF
+      s_post[c] += dm[c] * f[c];
+      dm[c] *= post1[c];
+      u[0] += sum4(dm[c] * f[c]);
+    }
+    row_sum<TPR>(u, part, 1);
+    const float back = second ? u[0] * inv : 0.f;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) df.template store<T>((c * TPR + lane) * 4, rf * (dm[c] - back * f[c]));
+    const int at = p.mod_part ? worker : m;
+    flush(p.gate, p.gate_stride, at, last && !p.all[0], s_gate);
+    flush(p.scale, p.scale_stride, at, last && !p.all[1], s_scale);
+    flush(p.shift, p.shift_stride, at, last && !p.all[2], s_shift);
+    m = last ? m + m_step : m;
+    i = last ? i_beg : i_next;
   }
-  if (p.all[0]) flush(p.gate, p.gate_stride, worker, s_gate);
-  if (p.all[1]) flush(p.scale, p.scale_stride, worker, s_scale);
-  if (p.all[2]) flush(p.shift, p.shift_stride, worker, s_shift);
-  flush(p.post, a.width, worker, s_post);
-  if (p.alpha) {
-    float v[1] = {s_alpha};
-    row_sum<TPR>(v, part, 0);  // the last sum, if any, was slot 1's or has a barrier behind it
-    if (lane == 0) p.alpha[worker] = v[0];
-  }
+  flush(p.gate, p.gate_stride, worker, p.all[0], s_gate);
+  flush(p.scale, p.scale_stride, worker, p.all[1], s_scale);
+  flush(p.shift, p.shift_stride, worker, p.all[2], s_shift);
+  flush(p.post, a.width, worker, true, s_post);
+  float v[1] = {s_alpha};
+  row_sum<TPR>(v, part, 0);
+  if (p.alpha && lane == 0) p.alpha[worker] = v[0];
 }
 
 // Sums of the workers: row m of a task is the sum of partial rows m n .. m n + n - 1, each slice's in order, then the
@@ -313,8 +350,7 @@ __global__ __launch_bounds__(256) void norm_sum_kernel(SumTasks tasks) {
   const SumTask t = tasks.t[blockIdx.z];
   const int m = blockIdx.y;
   if (m >= t.rows) return;
-  __shared__ f32x4_t part[16][16];
-  const int quad = threadIdx.x & 15, slice = threadIdx.x >> 4;
+  __shared__ f32x4_t part[64][4];
   if (t.width == 1) {
     if (blockIdx.x) return;
     float s = 0.f;
@@ -323,39 +359,54 @@ __global__ __launch_bounds__(256) void norm_sum_kernel(SumTasks tasks) {
     f[threadIdx.x] = s;
     __syncthreads();
     if (threadIdx.x < 64) {
-      s = wave_sum(f[threadIdx.x] + f[threadIdx.x + 64] + f[threadIdx.x + 128] + f[threadIdx.x + 192]);
+      s = lanes_sum(f[threadIdx.x] + f[threadIdx.x + 64] + f[threadIdx.x + 128] + f[threadIdx.x + 192]);
       if (threadIdx.x == 0) t.dst[0] = s;
     }
     return;
   }
-  const int col = blockIdx.x * 64 + quad * 4;
+  const int quad = threadIdx.x & 3, slice = threadIdx.x >> 2, col = blockIdx.x * 16 + quad * 4;
   f32x4_t s = all4(0.f);
-  if (col < t.width)
-    for (int i = slice; i < t.n; i += 16) s += load4(t.src + ((size_t)m * t.n + i) * t.width + col);
+  if (col < t.width) {
+    const float* const p = t.src + (size_t)m * t.n * t.width + col;
+#pragma unroll 4
+    for (int i = slice; i < t.n; i += 64) s += load4(p + (size_t)i * t.width);
+  }
   part[slice][quad] = s;
   __syncthreads();
+  if (threadIdx.x >= 32) return;
+  s = part[slice][quad];  // eight slices of eight
+#pragma unroll
+  for (int i = 1; i < 8; ++i) s += part[slice + 8 * i][quad];
+  part[slice][quad] = s;
+  __builtin_amdgcn_wave_barrier();
   if (slice == 0 && col < t.width) {
 #pragma unroll
-    for (int i = 1; i < 16; ++i) s += part[i][quad];
+    for (int i = 1; i < 8; ++i) s += part[i][quad];
     store4(t.dst + m * t.stride + col, s);
   }
 }
 
+template <typename S, typename T, int TPR, int NC>
+void launch_forward(const ravel_norm& n, hipStream_t s) {
+  constexpr int R = rows_per_block<TPR>();
+  norm_residual_kernel<S, T, TPR, NC><<<(n.rows + R - 1) / R, TPR * R, 0, s>>>(n);
+}
 template <typename S, typename T, int TPR, int NC>
 void launch_rows(const ravel_norm& n, const ravel_norm_grad* g, const GradPlan& p, hipStream_t s) {
   constexpr int R = rows_per_block<TPR>();
   if (g)
     norm_residual_grad_kernel<S, T, TPR, NC><<<(p.workers + R - 1) / R, TPR * R, 0, s>>>(n, *g, p);
   else
-    norm_residual_kernel<S, T, TPR, NC><<<(n.rows + R - 1) / R, TPR * R, 0, s>>>(n);
+    launch_forward<S, T, TPR, NC>(n, s);
 }
 template <typename S, typename T>
 void launch_width(const ravel_norm& n, const ravel_norm_grad* g, const GradPlan& p, hipStream_t s) {
   if (n.width <= 256) launch_rows<S, T, 64, 1>(n, g, p, s);
   else if (n.width <= 512) launch_rows<S, T, 64, 2>(n, g, p, s);
-  else if (n.width <= 1024) launch_rows<S, T, 64, 4>(n, g, p, s);
+  else if (n.width <= 1024 && !g && n.rows >= 1024) launch_forward<S, T, 64, 4>(n, s);
+  else if (n.width <= 1024) launch_rows<S, T, 128, 2>(n, g, p, s);
   else if (n.width <= 2048) launch_rows<S, T, 256, 2>(n, g, p, s);
-  else if (n.width <= 4096) launch_rows<S, T, 256, 4>(n, g, p, s);
+  else if (n.width <= 4096) launch_rows<S, T, 512, 2>(n, g, p, s);
   else launch_rows<S, T, 512, 4>(n, g, p, s);
 }
 void launch_types(const ravel_norm& n, const ravel_norm_grad* g, const GradPlan& p, hipStream_t s) {
@@ -390,7 +441,7 @@ hipError_t launch_norm_residual_grad(const ravel_norm& n, const ravel_norm_grad&
     t = {p.partial[i], dst[i], all ? 0 : stride[i], all ? 1 : p.mods, all ? p.workers : p.segs, i == 4 ? 1 : n.width};
     if (t.rows > rows) rows = t.rows;
   }
-  norm_sum_kernel<<<dim3((n.width + 63) / 64, rows, count), 256, 0, s>>>(tasks);
+  norm_sum_kernel<<<dim3((n.width + 15) / 16, rows, count), 256, 0, s>>>(tasks);
   return hipGetLastError();
 }
 
