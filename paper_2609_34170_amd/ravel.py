@@ -604,99 +604,88 @@ def _layer_tools():
     return _tools
 
 
-class _Placed:
-    """A call's device and stream: ``with`` makes both current (for the launches and what the call allocates), and
-    ``handle`` is the stream's."""
+_HERE = contextlib.nullcontext()
 
-    def __init__(self, stream, first, *rest):
-        torch, _, _, raw = _layer_tools()
-        device = first.get_device()
-        if device < 0:
-            raise ValueError("the call needs its tensors on a GPU")
-        for t in rest:
-            if t is not None and t.get_device() != device:
-                raise ValueError(f"every tensor of the call must be on {first.device}")
-        self.guard = None
-        if stream is None:
-            self.handle = raw(device)
-            if device != torch.cuda.current_device():
-                self.guard = torch.cuda.device(device)
-            return
-        if isinstance(stream, int):
-            stream = torch.cuda.ExternalStream(stream, device=first.device)
-        elif stream.device != first.device:
-            raise ValueError(f"the stream must be one of {first.device}")
-        self.guard, self.handle = torch.cuda.stream(stream), stream.cuda_stream
 
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return self
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+def _place(stream, first, *rest):
+    """(guard, handle): a context that makes the tensors' device and the call's stream current, for the launches and what
+    the call allocates, and the stream's handle."""
+    torch, _, _, raw = _tools or _layer_tools()
+    device = first.get_device()
+    if device < 0:
+        raise ValueError("the call needs its tensors on a GPU")
+    for t in rest:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"every tensor of the call must be on {first.device}")
+    if stream is None:
+        return (_HERE if device == torch.cuda.current_device() else torch.cuda.device(device)), raw(device)
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream, device=first.device)
+    elif stream.device != first.device:
+        raise ValueError(f"the stream must be one of {first.device}")
+    return torch.cuda.stream(stream), stream.cuda_stream
 
 
 def _dtype_of(name, t) -> int:
-    d = _layer_tools()[2].get(t.dtype)
+    d = _tools[2].get(t.dtype)
     if d is None:
         raise ValueError(f"{name} must be bfloat16 or float32, got {t.dtype}")
     return d
 
 
 def _like(name, t, shape, dtype):
+    """t's strides, its shape, type and contiguous last dimension checked."""
     if t.shape != shape or t.dtype is not dtype:
         raise ValueError(f"{name} must be a {dtype} tensor {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
-    if shape[-1] > 1 and t.stride(-1) != 1 and t.numel():
+    stride = t.stride()
+    if stride[-1] != 1 and shape[-1] > 1 and t.numel():
         raise ValueError(f"{name}'s last dimension must be contiguous")
+    return stride
 
 
 def _rows2(name, t, shape, dtype):
     """(address, row stride) of a matrix, or (0, 0) for None."""
     if t is None:
         return 0, 0
-    _like(name, t, shape, dtype)
-    return t.data_ptr(), t.stride(0)
+    return t.data_ptr(), _like(name, t, shape, dtype)[0]
 
 
-def _scratch(fn, *packed):
+def _scratch(fn, device, *packed):
     """Workspace of a call: (tensor that holds it or None, address, bytes).  It is the call's alone: torch keeps its memory
     from later calls on the stream until this one has run."""
-    torch = _layer_tools()[0]
     n = ctypes.c_int64(0)
     _check(fn(*packed, ctypes.byref(n)))
     if n.value == 0:
         return None, 0, 0
-    memory = torch.empty(n.value, dtype=torch.uint8, device=torch.device("cuda", torch.cuda.current_device()))
+    torch = _tools[0]
+    memory = torch.empty(n.value, dtype=torch.uint8, device=device)
     return memory, memory.data_ptr(), n.value
 
 
-def _modulation(x, post, alpha, gate, scale, shift):
-    """Addresses of what modulates x [rows, width], strides of gate, scale and shift, and their common row count."""
-    torch = _layer_tools()[0]
-    width, mods, ptr, stride = x.shape[1], 1, [], []
-    for name, t in (("post", post), ("alpha", alpha)):
-        if t is not None and (t.dtype is not torch.float32 or t.numel() != (width if name == "post" else 1) or
-                              not t.is_contiguous()):
-            raise ValueError(f"{name} must be a contiguous float32 tensor of {width if name == 'post' else 1}")
-        ptr.append(0 if t is None else t.data_ptr())
-    for name, t in (("gate", gate), ("scale", scale), ("shift", shift)):
-        if t is not None and t.dim() == 2:
-            if mods not in (1, t.shape[0]) and t.shape[0] != 1:
-                raise ValueError("gate, scale and shift must have the same number of rows, or one")
-            mods = max(mods, t.shape[0])
-    for name, t in (("gate", gate), ("scale", scale), ("shift", shift)):
+def _modulation(width, post, alpha, gate, scale, shift):
+    """Addresses of what modulates rows of ``width``, strides of gate, scale and shift, and their common row count."""
+    f32 = _tools[0].float32
+    mods, ptr, stride = 1, [0, 0, 0, 0, 0], [0, 0, 0]
+    for i, name, t, n in ((0, "post", post, width), (1, "alpha", alpha, 1)):
+        if t is not None:
+            if t.dtype is not f32 or t.numel() != n or not t.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous float32 tensor of {n}")
+            ptr[i] = t.data_ptr()
+    for i, name, t in ((0, "gate", gate), (1, "scale", scale), (2, "shift", shift)):
         if t is None:
-            ptr.append(0), stride.append(0)
             continue
-        if t.dim() not in (1, 2) or t.shape[-1] != width or t.dtype is not torch.float32:
+        shape, st = t.shape, t.stride()
+        if len(shape) not in (1, 2) or shape[-1] != width or t.dtype is not f32:
             raise ValueError(f"{name} must be a float32 tensor [{width}] or [rows of modulation, {width}]")
-        if t.stride(-1) != 1 and width > 1:
+        if st[-1] != 1 and t.numel():
             raise ValueError(f"{name}'s last dimension must be contiguous")
-        if t.dim() == 2 and t.shape[0] > 1 and t.stride(0) == 0:
-            raise ValueError(f"{name}: pass the row that is repeated as a vector")
-        ptr.append(t.data_ptr()), stride.append(t.stride(0) if t.dim() == 2 and t.shape[0] > 1 else 0)
+        if len(shape) == 2 and shape[0] != 1:
+            if shape[0] == 0 or mods not in (1, shape[0]):
+                raise ValueError("gate, scale and shift must have the same number of rows, or one")
+            if st[0] == 0:
+                raise ValueError(f"{name}: pass the row that is repeated as a vector")
+            mods, stride[i] = shape[0], st[0]
+        ptr[i + 2] = t.data_ptr()
     return ptr, stride, mods
 
 
@@ -709,14 +698,15 @@ def norm_residual(x, f=None, post=None, alpha=None, gate=None, scale=None, shift
     float32 tensors; ``gate``, ``scale`` and ``shift`` float32 ``[width]`` or ``[mods, width]``, of which row r uses
     (r // group) % mods.  Without f, x_out is x itself.  x_out may be x.
     """
-    torch, lib, types, _ = _layer_tools()
+    torch, lib, types, _ = _tools or _layer_tools()
     if x.dim() != 2:
         raise ValueError("x must be [rows, width]")
     T = f.dtype if f is not None else y.dtype if y is not None else torch.bfloat16
     S, shape = x.dtype, x.shape
     sizes = (_dtype_of("x", x), types.get(T, -1), *shape)
-    ptr, stride, mods = _modulation(x, post, alpha, gate, scale, shift)
-    with _Placed(stream, x, f, post, alpha, gate, scale, shift, y, x_out) as on:
+    ptr, stride, mods = _modulation(shape[1], post, alpha, gate, scale, shift)
+    guard, handle = _place(stream, x, f, post, alpha, gate, scale, shift, y, x_out)
+    with guard:
         if y is None:
             y = torch.empty(shape, dtype=T, device=x.device)
         if f is not None and x_out is None:
@@ -728,7 +718,7 @@ def norm_residual(x, f=None, post=None, alpha=None, gate=None, scale=None, shift
         yp, ys = _rows2("y", y, shape, T)
         op, os_ = _rows2("x_out", x_out, shape, S)
         _check(lib.ravel_norm_residual(_pack_norm(*sizes, mods, group, eps, 0, xp, fp, *ptr, op, yp, xs, fs, os_, ys, *stride),
-                                       on.handle))
+                                       handle))
     return y, x if f is None else x_out
 
 
@@ -741,7 +731,7 @@ def norm_residual_grad(x_out, dy=None, d_out=None, f=None, post=None, alpha=None
     ...}``, None being allocated; by default every input that is given, and ``shift`` (pass the forward's, or its shape's
     like; False: none) in scale's shape.  Gradients of the stream and the block have their dtype, the others float32.
     """
-    torch, lib, types, _ = _layer_tools()
+    torch, lib, types, _ = _tools or _layer_tools()
     if x_out.dim() != 2:
         raise ValueError("x_out must be [rows, width]")
     S, shape = x_out.dtype, x_out.shape
@@ -756,9 +746,10 @@ def norm_residual_grad(x_out, dy=None, d_out=None, f=None, post=None, alpha=None
         if n not in given or given[n] is None and grads[n] is None:
             raise ValueError(f"no gradient of {n}: it is not given")
     mod_shift = grads.get("shift") if grads.get("shift") is not None else given["shift"] if "shift" in grads else None
-    ptr, stride, mods = _modulation(x_out, post, alpha, gate, scale, mod_shift)
+    ptr, stride, mods = _modulation(shape[1], post, alpha, gate, scale, mod_shift)
     sizes = (_dtype_of("x_out", x_out), types.get(T, -1), *shape)
-    with _Placed(stream, x_out, dy, d_out, f, post, alpha, gate, scale, *grads.values()) as on:
+    guard, handle = _place(stream, x_out, dy, d_out, f, post, alpha, gate, scale, *grads.values())
+    with guard:
         out = {}
         for n, t in grads.items():
             like = given[n]
@@ -775,22 +766,21 @@ def norm_residual_grad(x_out, dy=None, d_out=None, f=None, post=None, alpha=None
         dp, ds = _rows2("d_out", d_out, shape, S)
         gx, gxs = _rows2("the gradient of x", out.get("x"), shape, S)
         gf, gfs = _rows2("the gradient of f", out.get("f"), shape, T)
-        gp, gs, _ = _modulation(x_out, out.get("post"), out.get("alpha"), out.get("gate"), out.get("scale"), out.get("shift"))
+        gp, gs, _ = _modulation(shape[1], out.get("post"), out.get("alpha"), out.get("gate"), out.get("scale"), out.get("shift"))
         tail = (ys, ds, gxs, gfs, *gs)
-        memory, ws, n = _scratch(lib.ravel_norm_residual_grad_workspace, norm, _pack_norm_grad(yp, dp, gx, gf, *gp, *tail, 0, 0))
-        _check(lib.ravel_norm_residual_grad(norm, _pack_norm_grad(yp, dp, gx, gf, *gp, *tail, ws, n), on.handle))
+        memory, ws, n = _scratch(lib.ravel_norm_residual_grad_workspace, x_out.device, norm, _pack_norm_grad(yp, dp, gx, gf, *gp, *tail, 0, 0))
+        _check(lib.ravel_norm_residual_grad(norm, _pack_norm_grad(yp, dp, gx, gf, *gp, *tail, ws, n), handle))
     return out
 
 
 def _heads4(name, t, shape, dtype):
-    _like(name, t, shape, dtype)
-    return t.data_ptr(), t.stride()[:3]
+    return t.data_ptr(), _like(name, t, shape, dtype)[:3]
 
 
 def _lengths(name, t, batch):
     if t is None:
         return 0
-    if t.dtype is not _layer_tools()[0].int32 or t.shape != (batch,) or not t.is_contiguous():
+    if t.dtype is not _tools[0].int32 or t.shape != (batch,) or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous int32 tensor [{batch}]")
     return t.data_ptr()
 
@@ -807,9 +797,10 @@ def cross_attention(q, k, v, q_len=None, k_len=None, scale=None, out=None, lse=N
     head_dim]`` of one dtype; the first ``k_len`` keys and ``q_len`` rows of each batch row take part (int32 tensors
     ``[batch]``; None: all), out is 0 for the other rows and where there are no keys.  ``lse``: float32 ``[batch,
     n_q_heads, rows]`` that receives what the gradients need."""
-    torch, lib, _, _ = _layer_tools()
+    torch, lib, _, _ = _tools or _layer_tools()
     sizes = _cross_sizes(q, k, scale)
-    with _Placed(stream, q, k, v, q_len, k_len, out, lse) as on:
+    guard, handle = _place(stream, q, k, v, q_len, k_len, out, lse)
+    with guard:
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         qp, qs = _heads4("q", q, q.shape, q.dtype)
@@ -821,17 +812,18 @@ def cross_attention(q, k, v, q_len=None, k_len=None, scale=None, out=None, lse=N
             raise ValueError(f"lse must be a contiguous float32 tensor {(sizes[1], sizes[2], sizes[5])}")
         fields = (*sizes, _lengths("q_len", q_len, sizes[1]), _lengths("k_len", k_len, sizes[1]), qp, kp, vp, op,
                   0 if lse is None else lse.data_ptr(), *qs, *ks, *vs, *os_)
-        memory, ws, n = _scratch(lib.ravel_cross_attention_workspace, _pack_cross(*fields, 0, 0))
-        _check(lib.ravel_cross_attention(_pack_cross(*fields, ws, n), on.handle))
+        memory, ws, n = _scratch(lib.ravel_cross_attention_workspace, q.device, _pack_cross(*fields, 0, 0))
+        _check(lib.ravel_cross_attention(_pack_cross(*fields, ws, n), handle))
     return out
 
 
 def cross_attention_grad(q, k, v, out, lse, dout, q_len=None, k_len=None, scale=None, dq=None, dk=None, dv=None,
                          need_q: bool = True, need_kv: bool = True, stream=None):
     """(dq, dk, dv) from ``dout``, with cross_attention's ``out`` and ``lse``; what is not needed is None."""
-    torch, lib, _, _ = _layer_tools()
+    torch, lib, _, _ = _tools or _layer_tools()
     sizes = _cross_sizes(q, k, scale)
-    with _Placed(stream, q, k, v, out, lse, dout, q_len, k_len, dq, dk, dv) as on:
+    guard, handle = _place(stream, q, k, v, out, lse, dout, q_len, k_len, dq, dk, dv)
+    with guard:
         T, device = q.dtype, q.device
         if lse.shape != (sizes[1], sizes[2], sizes[5]) or lse.dtype is not torch.float32 or not lse.is_contiguous():
             raise ValueError(f"lse must be a contiguous float32 tensor {(sizes[1], sizes[2], sizes[5])}")
@@ -856,8 +848,8 @@ def cross_attention_grad(q, k, v, out, lse, dout, q_len=None, k_len=None, scale=
         cross = _pack_cross(*sizes, _lengths("q_len", q_len, sizes[1]), _lengths("k_len", k_len, sizes[1]), qp, kp, vp, op,
                             lse.data_ptr(), *qs, *ks, *vs, *os_, 0, 0)
         fields = (dp, gq, gk, gv, *ds, *gqs, *gks, *gvs)
-        memory, ws, n = _scratch(lib.ravel_cross_attention_grad_workspace, cross, _pack_cross_grad(*fields, 0, 0))
-        _check(lib.ravel_cross_attention_grad(cross, _pack_cross_grad(*fields, ws, n), on.handle))
+        memory, ws, n = _scratch(lib.ravel_cross_attention_grad_workspace, q.device, cross, _pack_cross_grad(*fields, 0, 0))
+        _check(lib.ravel_cross_attention_grad(cross, _pack_cross_grad(*fields, ws, n), handle))
     return dq, dk, dv
 
 
@@ -884,9 +876,10 @@ def _pair(name, a, b, shape, dtype):
 def gated_mlp(x, wg, wu, act: str = "gelu", h=None, gate=None, up=None, stream=None):
     """h = act(x wg^T) * (x wu^T): x ``[rows, width]``, wg and wu ``[hidden, width]``, act "gelu" (tanh form) or "silu".
     ``gate`` and ``up`` ``[rows, hidden]`` receive x wg^T and x wu^T, for the gradients."""
-    torch, lib, _, _ = _layer_tools()
+    torch, lib, _, _ = _tools or _layer_tools()
     sizes = _mlp_sizes(x, wg, wu, act)
-    with _Placed(stream, x, wg, wu, h, gate, up) as on:
+    guard, handle = _place(stream, x, wg, wu, h, gate, up)
+    with guard:
         T, shape = x.dtype, (x.shape[0], wg.shape[0])
         if h is None:
             h = torch.empty(shape, dtype=T, device=x.device)
@@ -895,8 +888,8 @@ def gated_mlp(x, wg, wu, act: str = "gelu", h=None, gate=None, up=None, stream=N
         hp, hs = _rows2("h", h, shape, T)
         gp, up_, gs = _pair("gate and up", gate, up, shape, T)
         fields = (*sizes, xp, wp, vp, hp, gp, up_, xs, ws, hs, gs)
-        memory, at, n = _scratch(lib.ravel_gated_mlp_workspace, _pack_mlp(*fields, 0, 0))
-        _check(lib.ravel_gated_mlp(_pack_mlp(*fields, at, n), on.handle))
+        memory, at, n = _scratch(lib.ravel_gated_mlp_workspace, x.device, _pack_mlp(*fields, 0, 0))
+        _check(lib.ravel_gated_mlp(_pack_mlp(*fields, at, n), handle))
     return h
 
 
@@ -904,9 +897,10 @@ def gated_mlp_grad(x, wg, wu, gate, up, dh, act: str = "gelu", dx=None, dwg=None
                    need_w: bool = True, weight_dtype=None, stream=None):
     """(dx, dwg, dwu) from ``dh``, with gated_mlp's ``gate`` and ``up``; what is not needed is None.  The weights'
     gradients have ``weight_dtype``: the weights' own (the default), or float32."""
-    torch, lib, types, _ = _layer_tools()
+    torch, lib, types, _ = _tools or _layer_tools()
     sizes = _mlp_sizes(x, wg, wu, act)
-    with _Placed(stream, x, wg, wu, gate, up, dh, dx, dwg, dwu) as on:
+    guard, handle = _place(stream, x, wg, wu, gate, up, dh, dx, dwg, dwu)
+    with guard:
         T, W, shape = x.dtype, (dwg.dtype if dwg is not None else weight_dtype or x.dtype), (x.shape[0], wg.shape[0])
         if not need_x:
             dx = None
@@ -925,6 +919,6 @@ def gated_mlp_grad(x, wg, wu, gate, up, dh, act: str = "gelu", dx=None, dwg=None
         dgp, dup, dws = _pair("dwg and dwu", dwg, dwu, wg.shape, W)
         mlp = _pack_mlp(*sizes, xp, wp, vp, 0, gp, up_, xs, ws, 0, gs, 0, 0)
         fields = (types.get(W, -1), 0, hp, dxp, dgp, dup, hs, dxs, dws)
-        memory, at, n = _scratch(lib.ravel_gated_mlp_grad_workspace, mlp, _pack_mlp_grad(*fields, 0, 0))
-        _check(lib.ravel_gated_mlp_grad(mlp, _pack_mlp_grad(*fields, at, n), on.handle))
+        memory, at, n = _scratch(lib.ravel_gated_mlp_grad_workspace, x.device, mlp, _pack_mlp_grad(*fields, 0, 0))
+        _check(lib.ravel_gated_mlp_grad(mlp, _pack_mlp_grad(*fields, at, n), handle))
     return dx, dwg, dwu
