@@ -724,20 +724,9 @@ __global__ __launch_bounds__(256) void cross_few_keys_grad_kernel(CrossArgs a) {
     load_rows<T, HD, TR>(seg, dout, g.dout_stride[1], (int)g.dout_stride[2], space, t * TR, live, ot, wave);
     const int r = t * TR + rf * 16 + l16, qr = r / a.G, gh = w.h * a.G + r - qr * a.G;
     const bool in = r < live;
-    const T* const po = (const T*)c.out + w.b * c.out_stride[0] + qr * c.out_stride[1] + gh * c.out_stride[2];
-    frag of[STEPS], oo[STEPS];
-#pragma unroll
-    for (int s = 0; s < STEPS; ++s) oo[s] = in ? *(const frag*)(po + (s * 4 + grp) * (16 / E)) : frag{};
     const float lse = in ? c.lse[((size_t)w.b * c.n_q_heads + gh) * c.rows + qr] * kLog2e : INFINITY;
     tile_barrier<0>();
     const auto at = at0.fresh();
-    float D = 0.f;
-#pragma unroll
-    for (int s = 0; s < STEPS; ++s) {
-      of[s] = at.along_row((lds_char_t*)ot, rf, s);
-      D += dot16(of[s], oo[s]);
-    }
-    D = column_sum(D);
     f32x4_t s[2], dp[2];
 #pragma unroll
     for (int f = 0; f < 2; ++f) s[f] = dp[f] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -746,21 +735,27 @@ __global__ __launch_bounds__(256) void cross_few_keys_grad_kernel(CrossArgs a) {
 #pragma unroll
     for (int x = 0; x < STEPS; ++x) {
       frag qf = at.along_row((lds_char_t*)qt, rf, x);
+      const frag of = at.along_row((lds_char_t*)ot, rf, x);
       if (!(c.scale > 0.f)) qf = frag{};
 #pragma unroll
       for (int f = 0; f < KF; ++f) {
         s[f] = M::mma(at.along_row((lds_char_t*)kt, f, x), qf, s[f]);
-        dp[f] = M::mma(at.along_row((lds_char_t*)vt, f, x), of[x], dp[f]);
+        dp[f] = M::mma(at.along_row((lds_char_t*)vt, f, x), of, dp[f]);
       }
     }
+    float D = 0.f;  // sum p dout v^T, which is dout out before out was rounded
 #pragma unroll
     for (int f = 0; f < KF; ++f)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[f][i], cs, -lse));
-        s[f][i] = p;
-        dp[f][i] = p * (dp[f][i] - D);
+        s[f][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[f][i], cs, -lse));
+        D += s[f][i] * dp[f][i];
       }
+    D = column_sum(D);
+#pragma unroll
+    for (int f = 0; f < KF; ++f)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) dp[f][i] = s[f][i] * (dp[f][i] - D);
     if (dw == 0) {  // columns 16 f + 4 grp .. + 3 of the row's probabilities and their gradients
       const int row = rf * 16 + l16;
 #pragma unroll
