@@ -10,7 +10,6 @@
 // The gradients are two passes over the same tiles, each writing what it owns, so that nothing is added by atomics:
 // rows against all keys (dq; also each row's D = sum dout out), then keys against all rows (dk, dv).  That forms
 // s and dout v^T twice, 7 products for 5.
-#include "gemm_epilogue.h"
 #include "layer.h"
 #include "lds_tile.h"
 
@@ -62,17 +61,19 @@ RAVEL_DEV float column_sum(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// Block `id` of a launch: its tile, KV head, batch row and range, neighbours sharing a batch row and head (and their XCD's
-// L2).
+// A block's tile, range, KV head and batch row.  Neighbouring blocks, which run on different XCDs, take the tiles of one
+// head: lengths differ from batch row to batch row, and where every XCD had heads of its own (their keys in one L2) the one
+// with the longest rows ended last, 203 us instead of 149 for 16 batch rows of up to 2048 keys.  Tiles are
+// turned by the head, so that those behind a length do not all fall to one XCD either.
 struct Work {
   int tile, h, b, split;
 };
 RAVEL_DEV Work work_of(const CrossArgs& a) {
-  int id = xcd_tile(blockIdx.x, gridDim.x);
+  const unsigned id = blockIdx.x, head = id / (a.tiles * a.splits), in = id - head * (a.tiles * a.splits);
   Work w;
-  w.tile = id % a.tiles, id /= a.tiles;
-  w.split = id % a.splits, id /= a.splits;
-  w.h = id % a.c.n_kv_heads, w.b = id / a.c.n_kv_heads;
+  w.split = in / a.tiles;
+  w.tile = (in - w.split * a.tiles + head) % a.tiles;
+  w.h = head % a.c.n_kv_heads, w.b = head / a.c.n_kv_heads;
   return w;
 }
 
