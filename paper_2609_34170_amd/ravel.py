@@ -650,16 +650,26 @@ def _rows2(name, t, shape, dtype):
     return t.data_ptr(), _like(name, t, shape, dtype)[0]
 
 
-def _scratch(fn, device, *packed):
-    """Workspace of a call: (tensor that holds it or None, address, bytes).  It is the call's alone: torch keeps its memory
-    from later calls on the stream until this one has run."""
-    n = ctypes.c_int64(0)
-    _check(fn(*packed, ctypes.byref(n)))
-    if n.value == 0:
+_scratch_bytes = {}  # by call and sizes
+
+
+def _scratch(fn, device, key, *packed):
+    """Workspace of a call: (tensor that holds it or None, address, bytes), the bytes by ``key``, which with ``fn`` stands for
+    everything that they depend on.  It is the call's alone: torch keeps its memory from later calls on the stream until
+    this one has run."""
+    at = fn.__name__, key
+    size = _scratch_bytes.get(at)
+    if size is None:
+        n = ctypes.c_int64(0)
+        _check(fn(*(pack(*fields, 0, 0) if fields else pack for pack, fields in packed), ctypes.byref(n)))
+        if len(_scratch_bytes) >= 4096:
+            _scratch_bytes.clear()
+        size = _scratch_bytes[at] = n.value
+    if size == 0:
         return None, 0, 0
     torch = _tools[0]
-    memory = torch.empty(n.value, dtype=torch.uint8, device=device)
-    return memory, memory.data_ptr(), n.value
+    memory = torch.empty(size, dtype=torch.uint8, device=device)
+    return memory, memory.data_ptr(), size
 
 
 def _modulation(width, post, alpha, gate, scale, shift):
@@ -768,8 +778,10 @@ def norm_residual_grad(x_out, dy=None, d_out=None, f=None, post=None, alpha=None
         gf, gfs = _rows2("the gradient of f", out.get("f"), shape, T)
         gp, gs, _ = _modulation(shape[1], out.get("post"), out.get("alpha"), out.get("gate"), out.get("scale"), out.get("shift"))
         tail = (ys, ds, gxs, gfs, *gs)
-        memory, ws, n = _scratch(lib.ravel_norm_residual_grad_workspace, x_out.device, norm, _pack_norm_grad(yp, dp, gx, gf, *gp, *tail, 0, 0))
-        _check(lib.ravel_norm_residual_grad(norm, _pack_norm_grad(yp, dp, gx, gf, *gp, *tail, ws, n), handle))
+        fields = (yp, dp, gx, gf, *gp, *tail)
+        key = (sizes, mods, group, tuple(map(bool, gp)), tuple(map(bool, gs)))
+        memory, ws, n = _scratch(lib.ravel_norm_residual_grad_workspace, x_out.device, key, (norm, ()), (_pack_norm_grad, fields))
+        _check(lib.ravel_norm_residual_grad(norm, _pack_norm_grad(*fields, ws, n), handle))
     return out
 
 
@@ -812,7 +824,7 @@ def cross_attention(q, k, v, q_len=None, k_len=None, scale=None, out=None, lse=N
             raise ValueError(f"lse must be a contiguous float32 tensor {(sizes[1], sizes[2], sizes[5])}")
         fields = (*sizes, _lengths("q_len", q_len, sizes[1]), _lengths("k_len", k_len, sizes[1]), qp, kp, vp, op,
                   0 if lse is None else lse.data_ptr(), *qs, *ks, *vs, *os_)
-        memory, ws, n = _scratch(lib.ravel_cross_attention_workspace, q.device, _pack_cross(*fields, 0, 0))
+        memory, ws, n = _scratch(lib.ravel_cross_attention_workspace, q.device, sizes, (_pack_cross, fields))
         _check(lib.ravel_cross_attention(_pack_cross(*fields, ws, n), handle))
     return out
 
@@ -848,7 +860,8 @@ def cross_attention_grad(q, k, v, out, lse, dout, q_len=None, k_len=None, scale=
         cross = _pack_cross(*sizes, _lengths("q_len", q_len, sizes[1]), _lengths("k_len", k_len, sizes[1]), qp, kp, vp, op,
                             lse.data_ptr(), *qs, *ks, *vs, *os_, 0, 0)
         fields = (dp, gq, gk, gv, *ds, *gqs, *gks, *gvs)
-        memory, ws, n = _scratch(lib.ravel_cross_attention_grad_workspace, q.device, cross, _pack_cross_grad(*fields, 0, 0))
+        memory, ws, n = _scratch(lib.ravel_cross_attention_grad_workspace, q.device, (sizes, need_q, need_kv), (cross, ()),
+                                 (_pack_cross_grad, fields))
         _check(lib.ravel_cross_attention_grad(cross, _pack_cross_grad(*fields, ws, n), handle))
     return dq, dk, dv
 
@@ -888,7 +901,7 @@ def gated_mlp(x, wg, wu, act: str = "gelu", h=None, gate=None, up=None, stream=N
         hp, hs = _rows2("h", h, shape, T)
         gp, up_, gs = _pair("gate and up", gate, up, shape, T)
         fields = (*sizes, xp, wp, vp, hp, gp, up_, xs, ws, hs, gs)
-        memory, at, n = _scratch(lib.ravel_gated_mlp_workspace, x.device, _pack_mlp(*fields, 0, 0))
+        memory, at, n = _scratch(lib.ravel_gated_mlp_workspace, x.device, sizes, (_pack_mlp, fields))
         _check(lib.ravel_gated_mlp(_pack_mlp(*fields, at, n), handle))
     return h
 
@@ -919,6 +932,7 @@ def gated_mlp_grad(x, wg, wu, gate, up, dh, act: str = "gelu", dx=None, dwg=None
         dgp, dup, dws = _pair("dwg and dwu", dwg, dwu, wg.shape, W)
         mlp = _pack_mlp(*sizes, xp, wp, vp, 0, gp, up_, xs, ws, 0, gs, 0, 0)
         fields = (types.get(W, -1), 0, hp, dxp, dgp, dup, hs, dxs, dws)
-        memory, at, n = _scratch(lib.ravel_gated_mlp_grad_workspace, x.device, mlp, _pack_mlp_grad(*fields, 0, 0))
+        memory, at, n = _scratch(lib.ravel_gated_mlp_grad_workspace, x.device, (sizes, need_x, need_w), (mlp, ()),
+                                 (_pack_mlp_grad, fields))
         _check(lib.ravel_gated_mlp_grad(mlp, _pack_mlp_grad(*fields, at, n), handle))
     return dx, dwg, dwu
