@@ -25,7 +25,7 @@ struct CrossArgs {
   int padded;            // rows of stat (and of a partial) per (batch row, KV head)
   float* part;           // partial results [split][batch][KV head][row or key][head_dim], or null
   float* part_ml;        // forward: [split][batch][KV head][row][2], maximum (log2 units) and sum
-  float* stat;           // gradients: [2][batch][KV head][padded]: lse (log2 units), D
+  float* stat;           // gradients: [2][batch][KV head][padded]: what a row's scores and dout v^T start from, -lse / scale and -D
   float* part2;          // dv's partials
 };
 
@@ -374,7 +374,8 @@ __global__ __launch_bounds__(256, (4 * Tiles<T, HD, TK>::BYTES <= 65536 ? 2 : 1)
   if (t0 < t1) issue(t0, k0, v0);
 
   frag qf[MI][STEPS], of[MI][STEPS];  // of: dout
-  float lse[MI], D[MI];
+  const float cs = c.scale > 0.f ? c.scale * kLog2e : 1.f;
+  float lse[MI], D[MI];  // negative: what the sums start from, so that p = exp2(cs s) and ds = p dp
 #pragma unroll
   for (int i = 0; i < MI; ++i) {
     const int r = row0 + i * 16 + l16, qr = r / a.G, gh = w.h * a.G + r - qr * a.G;
@@ -390,8 +391,8 @@ __global__ __launch_bounds__(256, (4 * Tiles<T, HD, TK>::BYTES <= 65536 ? 2 : 1)
       of[i][s] = in ? *(const frag*)(pd + e) : frag{};
       D[i] += dot16(of[i][s], in ? *(const frag*)(po + e) : frag{});
     }
-    D[i] = column_sum(D[i]);
-    lse[i] = in ? c.lse[((size_t)w.b * c.n_q_heads + gh) * c.rows + qr] * kLog2e : INFINITY;
+    D[i] = -column_sum(D[i]);
+    lse[i] = in ? -(c.lse[((size_t)w.b * c.n_q_heads + gh) * c.rows + qr] * kLog2e / cs) : -INFINITY;
     if (a.stat && grp == 0 && wk == 0 && w.split == 0) {
       float* const p = a.stat + ((size_t)w.b * c.n_kv_heads + w.h) * a.padded + r;
       p[0] = lse[i];
@@ -399,7 +400,6 @@ __global__ __launch_bounds__(256, (4 * Tiles<T, HD, TK>::BYTES <= 65536 ? 2 : 1)
     }
   }
   if (!g.dq) return;
-  const float cs = c.scale > 0.f ? c.scale * kLog2e : 1.f;
   f32x4_t dq[MI][DF];
 #pragma unroll
   for (int i = 0; i < MI; ++i)
@@ -431,7 +431,7 @@ __global__ __launch_bounds__(256, (4 * Tiles<T, HD, TK>::BYTES <= 65536 ? 2 : 1)
 #pragma unroll
       for (int f = 0; f < FP; ++f) {
 #pragma unroll
-        for (int i = 0; i < MI; ++i) s[i][f] = start[p * FP + f], dp[i][f] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < MI; ++i) s[i][f] = start[p * FP + f] + lse[i], dp[i][f] = f32x4_t{D[i], D[i], D[i], D[i]};
 #pragma unroll
         for (int st = 0; st < STEPS; ++st) {
           const frag kf = at.along_row(kt, p * FP + f, st), vf = at.along_row(vt, p * FP + f, st);
@@ -449,8 +449,7 @@ __global__ __launch_bounds__(256, (4 * Tiles<T, HD, TK>::BYTES <= 65536 ? 2 : 1)
         for (int f = 0; f < FP; ++f)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const float pr = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][f][r], cs, -lse[i]));
-            s[i][f][r] = pr * (dp[i][f][r] - D[i]);
+            s[i][f][r] = __builtin_amdgcn_exp2f(s[i][f][r] * cs) * dp[i][f][r];
           }
         ds[i] = M::operand(s[i]);
       }
@@ -577,20 +576,19 @@ __global__ __launch_bounds__(256, (4 * Tiles<T, HD, TR>::BYTES <= 65536 && Tiles
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
       const auto at = at0.fresh();
-      f32x4_t s[KI][FP], dp[KI][FP], le[FP], Dr[FP];
+      f32x4_t s[KI][FP], dp[KI][FP];
 #pragma unroll
       for (int f = 0; f < FP; ++f) {
-        le[f] = *(RAVEL_LDS const f32x4_t*)(st + (p * FP + f) * 16);
-        Dr[f] = *(RAVEL_LDS const f32x4_t*)(st + TS + (p * FP + f) * 16);
+        const f32x4_t s0 = *(RAVEL_LDS const f32x4_t*)(st + (p * FP + f) * 16), dp0 = *(RAVEL_LDS const f32x4_t*)(st + TS + (p * FP + f) * 16);
 #pragma unroll
-        for (int i = 0; i < KI; ++i) s[i][f] = dp[i][f] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < KI; ++i) s[i][f] = s0, dp[i][f] = dp0;
 #pragma unroll
-        for (int st = 0; st < STEPS; ++st) {
-          const frag qf = at.along_row(qt, p * FP + f, st), of = at.along_row(ot, p * FP + f, st);
+        for (int x = 0; x < STEPS; ++x) {
+          const frag qf = at.along_row(qt, p * FP + f, x), of = at.along_row(ot, p * FP + f, x);
 #pragma unroll
           for (int i = 0; i < KI; ++i) {
-            s[i][f] = M::mma(qf, kf[i][st], s[i][f]);
-            dp[i][f] = M::mma(of, vf[i][st], dp[i][f]);
+            s[i][f] = M::mma(qf, kf[i][x], s[i][f]);
+            dp[i][f] = M::mma(of, vf[i][x], dp[i][f]);
           }
         }
       }
@@ -601,9 +599,8 @@ __global__ __launch_bounds__(256, (4 * Tiles<T, HD, TR>::BYTES <= 65536 && Tiles
         for (int f = 0; f < FP; ++f)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const float pr = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][f][r], cs, -le[f][r]));
-            s[i][f][r] = pr;
-            dp[i][f][r] = pr * (dp[i][f][r] - Dr[f][r]);
+            s[i][f][r] = __builtin_amdgcn_exp2f(s[i][f][r] * cs);
+            dp[i][f][r] *= s[i][f][r];
           }
         pf[i] = M::operand(s[i]);
         ds[i] = M::operand(dp[i]);
