@@ -141,8 +141,8 @@ __global__ __launch_bounds__(256, (4 * Tiles<T, HD, TK>::BYTES <= 65536 ? 2 : 1)
   const Work w = work_of(a);
   const int live = live_len(c.q_len, w.b, c.rows) * a.G, all = c.rows * a.G;
   const int klen = live_len(c.k_len, w.b, c.keys);
-  const int row0 = w.tile * (16 * MI * (4 / KW)) + wr * 16 * MI;  // this wave's rows
-  const int ktiles = (klen + TK - 1) / TK, per = (ktiles + a.splits - 1) / a.splits;
+  const int first = w.tile * (16 * MI * (4 / KW)), row0 = first + wr * 16 * MI;  // the block's rows, this wave's
+  const int ktiles = first < live ? (klen + TK - 1) / TK : 0, per = (ktiles + a.splits - 1) / a.splits;
   const int t0 = min(ktiles, w.split * per), t1 = min(ktiles, t0 + per);
 
   const T* const q = (const T*)c.q + w.b * c.q_stride[0] + (int64_t)w.h * a.G * c.q_stride[2];
@@ -357,8 +357,8 @@ __global__ __launch_bounds__(256, (4 * Tiles<T, HD, TK>::BYTES <= 65536 ? 2 : 1)
   const Work w = work_of(a);
   const int live = live_len(c.q_len, w.b, c.rows) * a.G, all = c.rows * a.G;
   const int klen = live_len(c.k_len, w.b, c.keys);
-  const int row0 = w.tile * (16 * MI * (4 / KW)) + wr * 16 * MI;
-  const int ktiles = g.dq ? (klen + TK - 1) / TK : 0, per = (ktiles + a.splits - 1) / a.splits;
+  const int first = w.tile * (16 * MI * (4 / KW)), row0 = first + wr * 16 * MI;
+  const int ktiles = g.dq && first < live ? (klen + TK - 1) / TK : 0, per = (ktiles + a.splits - 1) / a.splits;
   const int t0 = min(ktiles, w.split * per), t1 = min(ktiles, t0 + per);
 
   const T* const k = (const T*)c.k + w.b * c.k_stride[0] + w.h * c.k_stride[2];
@@ -946,7 +946,7 @@ GradPlan plan_grad(const ravel_cross& c, const ravel_cross_grad& g) {
   p.few_rows = all <= 32 || heads * (p.padded / (64 * S::BI)) < kFill / 2;
   const int per = p.few_rows ? 16 * (4 / S::KW) : 64 * S::BI, tk = p.few_rows ? S::TF : S::TK;
   p.qtiles = p.padded / per;
-  p.qsplits = g.dq ? ranges(heads * ((all + per - 1) / per), (c.keys + tk - 1) / tk, 4, kFill) : 1;
+  p.qsplits = g.dq ? ranges(heads * ((all + per - 1) / per), (c.keys + tk - 1) / tk, 4, p.few_rows ? 3 * kFill : kFill) : 1;
   if (p.qsplits > 1) p.part = (size_t)p.qsplits * heads * all * HD * 4;
   if (g.dk) {
     p.few_keys = c.keys <= 64;
