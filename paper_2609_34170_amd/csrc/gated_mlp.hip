@@ -320,6 +320,7 @@ __global__ __launch_bounds__(256) void mlp_hidden_grad_kernel(ravel_mlp a, ravel
 struct MatPlan {
   int tile;  // 0: 256 x 256, 1: 128 x 128, 2: 64 x 64
   int splits, per;
+  double us;  // expected
 };
 constexpr int kTile[3] = {256, 128, 64};
 int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
@@ -331,21 +332,19 @@ MatPlan plan_matrix(int64_t M, int64_t N, int64_t K, int pairs, int products, in
   // side, 0.88 with one alone, which is worth 1.3 of them; 64 x 64 ones 0.25 side by side, the first two in the
   // time of two.
   constexpr double us[3] = {1.85, 0.67, 0.25}, alone[3] = {1.0, 1.3, 2.0};
+  constexpr double ends[3] = {3, 1, 0.5};  // a block's first loads and its end (the forward's stores three outputs)
   MatPlan best{};
-  double least = 0;
   for (int t = elt == 4 ? 1 : 0; t < 3; ++t) {
     const int64_t blocks = (int64_t)ceil_div(M, kTile[t]) * ceil_div(N, kTile[t]) * products;
     const int tiles = ceil_div(K, 128 / elt) * pairs;
+    const double end = split ? ends[t] : 3 * ends[t];
     for (int s = 1; s <= (split ? 16 : 1); ++s) {
       if (s > 1 && tiles / s < 4) break;
       const int per = tiles ? ceil_div(tiles, s) : 1;
       const double n = (double)((blocks * s + 255) / 256);
-      double cost = (n > alone[t] ? n : alone[t]) * per * us[t] * (elt == 4 ? 2.6 : 1) + n * 2;  // 2: a block's first loads and its end
+      double cost = (n > alone[t] ? n : alone[t]) * per * us[t] * (elt == 4 ? 2.6 : 1) + n * end;
       if (s > 1) cost += 4 + (double)M * N * products * s * 8 / 4e6;       // a launch, and the sums there and back
-      if (least == 0 || cost < least) {
-        least = cost;
-        best = {t, tiles ? ceil_div(tiles, per) : 1, per};
-      }
+      if (best.us == 0 || cost < best.us) best = {t, tiles ? ceil_div(tiles, per) : 1, per, cost};
     }
   }
   return best;
@@ -390,10 +389,32 @@ hipError_t forward(const ravel_mlp& m, hipStream_t s) {
     else mlp_rows_kernel<T, 4><<<grid, 512, 0, s>>>(a);
     return hipGetLastError();
   }
-  const MatPlan p = plan_matrix(a.M, a.N, a.K, 1, 1, sizeof(T), false);
+  // Blocks of 256 x 256 run one a CU, in rounds: the rows behind the last full round go into a launch of smaller tiles where
+  // that is sooner (6400 rows, 2048 -> 8192: 6 rounds and 256 rows in 128 x 128 tiles, 447 us, instead of a seventh round,
+  // 465; 3200 rows, 1024 -> 4096 stay whole). 4 us: the second launch and the first one's end.
+  MatPlan p = plan_matrix(a.M, a.N, a.K, 1, 1, sizeof(T), false), rest{};
+  int first = a.M;
+  if (p.tile == 0)
+    for (int64_t round = 1; round <= ceil_div(a.M, 256) * (int64_t)ceil_div(a.N, 256) / 256; ++round) {
+      const int64_t rows = round * 256 / ceil_div(a.N, 256) * 256;
+      if (rows < 1 || rows >= a.M) continue;
+      const MatPlan q = plan_matrix(a.M - rows, a.N, a.K, 1, 1, sizeof(T), false);
+      const MatPlan f = plan_matrix(rows, a.N, a.K, 1, 1, sizeof(T), false);
+      if (f.tile != 0 || f.us + q.us + 4 >= p.us + rest.us + (rest.us > 0 ? 4 : 0)) continue;
+      p = f, rest = q, first = (int)rows;
+    }
+  const int all = a.M;
+  a.M = first;
   a.splits = p.splits;
   a.per = p.per;
-  return launch_matrix<T, T, false, false, FORWARD>(a, p.tile, s);
+  const hipError_t e = launch_matrix<T, T, false, false, FORWARD>(a, p.tile, s);
+  if (e != hipSuccess || first == all) return e;
+  a.M = all - first;
+  a.per = rest.per;
+  a.A[0] = (const T*)a.A[0] + first * a.lda;
+  a.C[0] = (T*)a.C[0] + first * a.ldc;
+  if (a.C[1]) a.C[1] = (T*)a.C[1] + first * a.ldg, a.C[2] = (T*)a.C[2] + first * a.ldg;
+  return launch_matrix<T, T, false, false, FORWARD>(a, rest.tile, s);
 }
 
 struct GradBytes {
