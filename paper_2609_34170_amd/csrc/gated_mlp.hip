@@ -32,6 +32,18 @@ RAVEL_DEV float act_f(float x, int kind) { return kind == RAVEL_SILU ? silu_f(x)
 
 RAVEL_DEV void put4(float* p, f32x4_t v) { *(f32x4_t*)p = v; }
 RAVEL_DEV void put4(bf16_t* p, f32x4_t v) { *(u32x2_t*)p = u32x2_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])}; }
+// Blocks of 16 columns that follow each other, v and w: a lane holds 4 columns of its row in each.  Lane groups trade, the even
+// ones keep v, so that each lane stores 8 columns of one block and a row of the two is written as 64 bytes.
+RAVEL_DEV void put_pair(float* row, int n, int N, int grp, f32x4_t v, f32x4_t w) {
+  if (n + grp * 4 < N) put4(row + n + grp * 4, v);
+  if (n + 16 + grp * 4 < N) put4(row + n + 16 + grp * 4, w);
+}
+RAVEL_DEV void put_pair(bf16_t* row, int n, int N, int grp, f32x4_t v, f32x4_t w) {
+  const auto a = __builtin_amdgcn_permlane16_swap(pack_bf16x2(v[0], v[1]), pack_bf16x2(w[0], w[1]), false, false);
+  const auto b = __builtin_amdgcn_permlane16_swap(pack_bf16x2(v[2], v[3]), pack_bf16x2(w[2], w[3]), false, false);
+  n += (grp & 1) * 16 + (grp >> 1) * 8;
+  if (n < N) *(u32x4_t*)(row + n) = u32x4_t{a[0], b[0], a[1], b[1]};
+}
 
 // BM x BN outputs a block of WM x WN waves.  AC, BC: A, B lie as rows across the contraction.  O: type of the outputs.
 template <typename T, typename O, int BM, int BN, int WM, int WN, bool AC, bool BC, int MODE>
@@ -43,7 +55,8 @@ __global__ __launch_bounds__(64 * WM * WN) void mlp_matrix_kernel(MatArgs a) {
   constexpr int RA = AC ? BM * E : 128, RBB = BC ? BN * E : 128;  // bytes of a tile's row
   constexpr int SA = BM * 128 / 1024 / NW, SB = BN * 128 / 1024 / NW;
   static_assert(SA >= 1 && SB >= 1 && BM % (16 * WM) == 0 && BN % (16 * WN) == 0, "tiles");
-  static_assert(MODE != FORWARD || TN % 2 == 0, "a gate block and its up block in one wave");
+  static_assert(TN % 2 == 0, "two blocks of outputs that follow each other, or a gate block and its up block, in one wave");
+  constexpr int STEP = TN % 4 == 0 ? 4 : 2;
   // Four arrays: reads along columns of one buffer wait for the loads in flight into another unless the compiler sees
   // that they are apart.
   __shared__ __attribute__((aligned(1024))) char As0[BM * 128], As1[BM * 128], Bs0[BN * 128], Bs1[BN * 128];
@@ -157,30 +170,38 @@ __global__ __launch_bounds__(64 * WM * WN) void mlp_matrix_kernel(MatArgs a) {
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
     const int m = m0 + (wm * TM + i) * 16 + l16;
-    if (m >= a.M) continue;
+    if (m >= a.M) continue;  // (lanes that trade share their row)
     if constexpr (MODE == FORWARD) {
 #pragma unroll
-      for (int j = 0; j < TN; j += 2) {
-        const int u = n0 / 2 + (wn * TN + j) * 8 + grp * 4;
-        if (u >= a.N / 2) continue;
-        f32x4_t h;
+      for (int j = 0; j < TN; j += STEP) {
+        const int u = n0 / 2 + (wn * TN + j) * 8;
+        f32x4_t h[2];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) h[r] = act_f(acc[i][j][r], a.act) * acc[i][j + 1][r];
-        put4((O*)a.C[0] + m * a.ldc + u, h);
-        if (a.C[1]) {
-          put4((O*)a.C[1] + m * a.ldg + u, acc[i][j]);
-          put4((O*)a.C[2] + m * a.ldg + u, acc[i][j + 1]);
+        for (int k = 0; k < STEP / 2; ++k)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) h[k][r] = act_f(acc[i][j + 2 * k][r], a.act) * acc[i][j + 2 * k + 1][r];
+        if constexpr (STEP == 4) {
+          put_pair((O*)a.C[0] + m * a.ldc, u, a.N / 2, grp, h[0], h[1]);
+          if (a.C[1]) {
+            put_pair((O*)a.C[1] + m * a.ldg, u, a.N / 2, grp, acc[i][j], acc[i][j + 2]);
+            put_pair((O*)a.C[2] + m * a.ldg, u, a.N / 2, grp, acc[i][j + 1], acc[i][j + 3]);
+          }
+        } else if (u + grp * 4 < a.N / 2) {
+          put4((O*)a.C[0] + m * a.ldc + u + grp * 4, h[0]);
+          if (a.C[1]) {
+            put4((O*)a.C[1] + m * a.ldg + u + grp * 4, acc[i][j]);
+            put4((O*)a.C[2] + m * a.ldg + u + grp * 4, acc[i][j + 1]);
+          }
         }
       }
     } else {
 #pragma unroll
-      for (int j = 0; j < TN; ++j) {
-        const int n = n0 + (wn * TN + j) * 16 + grp * 4;
-        if (n >= a.N) continue;
+      for (int j = 0; j < TN; j += 2) {
+        const int n = n0 + (wn * TN + j) * 16;
         if (a.part)
-          put4(a.part + (((size_t)z * (MODE == BOTH ? 2 : 1) + which) * a.M + m) * a.N + n, acc[i][j]);
+          put_pair(a.part + (((size_t)z * (MODE == BOTH ? 2 : 1) + which) * a.M + m) * a.N, n, a.N, grp, acc[i][j], acc[i][j + 1]);
         else
-          put4((O*)a.C[which] + m * a.ldc + n, acc[i][j]);
+          put_pair((O*)a.C[which] + m * a.ldc, n, a.N, grp, acc[i][j], acc[i][j + 1]);
       }
     }
   }
