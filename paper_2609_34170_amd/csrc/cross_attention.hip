@@ -36,6 +36,12 @@ template <> RAVEL_DEV void store_row4<float>(float* p, f32x4_t v) { *(f32x4_t*)p
 template <> RAVEL_DEV void store_row4<bf16_t>(bf16_t* p, f32x4_t v) {
   *(u32x2_t*)p = u32x2_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
 }
+// 32 columns of row l16, two blocks (all lanes of a row take part)
+RAVEL_DEV void store_blocks(float* row, int lane, f32x4_t v, f32x4_t w) {
+  store_row4(row + (lane >> 4) * 4, v);
+  store_row4(row + 16 + (lane >> 4) * 4, w);
+}
+RAVEL_DEV void store_blocks(bf16_t* row, int lane, f32x4_t v, f32x4_t w) { *(u32x4_t*)(row + joined_column(lane)) = join_blocks(v, w); }
 RAVEL_DEV float dot16(f32x4_t a, f32x4_t b) { return (a[0] * b[0] + a[1] * b[1]) + (a[2] * b[2] + a[3] * b[3]); }
 RAVEL_DEV float dot16(bf16x8_t a, bf16x8_t b) {
   const u32x4_t x = __builtin_bit_cast(u32x4_t, a), y = __builtin_bit_cast(u32x4_t, b);
@@ -302,9 +308,10 @@ __global__ __launch_bounds__(256, (4 * Tiles<T, HD, TK>::BYTES <= 65536 ? 2 : 1)
     const int qr = r / a.G, g = r - qr * a.G;
     const bool any = r < live && klen > 0;
     const float f = any ? 1.f / l[i] : 0.f;
+    const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
     T* const out = (T*)c.out + w.b * c.out_stride[0] + qr * c.out_stride[1] + (int64_t)(w.h * a.G + g) * c.out_stride[2];
 #pragma unroll
-    for (int d = 0; d < DF; ++d) store_row4<T>(out + d * 16 + grp * 4, any ? o[i][d] * f : f32x4_t{0.f, 0.f, 0.f, 0.f});
+    for (int d = 0; d < DF; d += 2) store_blocks(out + d * 16, lane, any ? o[i][d] * f : zero, any ? o[i][d + 1] * f : zero);
     if (c.lse && grp == 0)
       c.lse[((size_t)w.b * c.n_q_heads + w.h * a.G + g) * c.rows + qr] = any ? m[i] * kLn2 + logf(l[i]) : -INFINITY;
   }
@@ -493,9 +500,11 @@ __global__ __launch_bounds__(256, (4 * Tiles<T, HD, TK>::BYTES <= 65536 ? 2 : 1)
       continue;
     }
     const int qr = r / a.G, gh = w.h * a.G + r - qr * a.G;
+    const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
     T* const to = (T*)g.dq + w.b * g.dq_stride[0] + qr * g.dq_stride[1] + gh * g.dq_stride[2];
 #pragma unroll
-    for (int d = 0; d < DF; ++d) store_row4<T>(to + d * 16 + grp * 4, r < live ? dq[i][d] * c.scale : f32x4_t{0.f, 0.f, 0.f, 0.f});
+    for (int d = 0; d < DF; d += 2)
+      store_blocks(to + d * 16, lane, r < live ? dq[i][d] * c.scale : zero, r < live ? dq[i][d + 1] * c.scale : zero);
   }
 }
 
@@ -660,9 +669,9 @@ __global__ __launch_bounds__(256, (4 * Tiles<T, HD, TR>::BYTES <= 65536 && Tiles
     T* const pv = (T*)g.dv + w.b * g.dv_stride[0] + key * g.dv_stride[1] + w.h * g.dv_stride[2];
     const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int d = 0; d < DF; ++d) {
-      store_row4<T>(pk + d * 16 + grp * 4, key < klen ? dk[i][d] * c.scale : zero);
-      store_row4<T>(pv + d * 16 + grp * 4, key < klen ? dv[i][d] : zero);
+    for (int d = 0; d < DF; d += 2) {
+      store_blocks(pk + d * 16, lane, key < klen ? dk[i][d] * c.scale : zero, key < klen ? dk[i][d + 1] * c.scale : zero);
+      store_blocks(pv + d * 16, lane, key < klen ? dv[i][d] : zero, key < klen ? dv[i][d + 1] : zero);
     }
   }
 }
@@ -682,6 +691,7 @@ __global__ __launch_bounds__(256) void cross_few_keys_grad_kernel(CrossArgs a) {
   typedef typename M::frag frag;
   constexpr int E = sizeof(T), RB = Z::RB, STEPS = RB / 64, DF = HD / 16, NK = 32 / M::CK, FP = M::CK / 16;
   constexpr int RF = TR / 16, DW = 4 / RF, DQ = DF / DW < 1 ? 1 : DF / DW, DKV = (DF + 3) / 4;
+  static_assert(DQ == 1 || DQ % 2 == 0, "blocks of dq stored in pairs");
   constexpr int PB = 32 * E;  // bytes of a row of probabilities
   __shared__ __attribute__((aligned(1024))) char kt[ZK::BYTES], vt[ZK::BYTES], qt[Z::BYTES], ot[Z::BYTES], pt[TR * PB], st[TR * PB];
 
@@ -765,15 +775,24 @@ __global__ __launch_bounds__(256) void cross_few_keys_grad_kernel(CrossArgs a) {
     }
     if (g.dq) {  // (every lane's fragments take part, also those of rows that do not exist)
       T* const to = (T*)g.dq + w.b * g.dq_stride[0] + qr * g.dq_stride[1] + gh * g.dq_stride[2];
-#pragma unroll
-      for (int d = 0; d < DQ; ++d) {
-        const int df = dw * DQ + d;
-        if (df >= DF) continue;
+      const auto product = [&](int df) {
         f32x4_t dq = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < NK; ++j)
           if (j * FP < KF) dq = M::mma(at.along_col((lds_char_t*)kt, j, df), M::operand(&dp[j * FP]), dq);
-        if (r < all) store_row4<T>(to + df * 16 + grp * 4, in ? dq * c.scale : f32x4_t{0.f, 0.f, 0.f, 0.f});
+        return in ? dq * c.scale : f32x4_t{0.f, 0.f, 0.f, 0.f};
+      };
+#pragma unroll
+      for (int d = 0; d < DQ; d += 2) {
+        const int df = dw * DQ + d;
+        if (df >= DF) continue;
+        if constexpr (DQ % 2 == 0) {
+          const f32x4_t x = product(df), y = product(df + 1);
+          if (r < all) store_blocks(to + df * 16, lane, x, y);
+        } else {
+          const f32x4_t x = product(df);
+          if (r < all) store_row4<T>(to + df * 16 + grp * 4, x);
+        }
       }
     }
     __syncthreads();

@@ -35,12 +35,6 @@ RAVEL_DEV void put4(bf16_t* p, f32x4_t v) { *(u32x2_t*)p = u32x2_t{pack_bf16x2(v
 // Outputs are written in 64 (the forward's) or 128 bytes of a row: a 16 x 16 block leaves the matrix instructions with 4
 // columns of row l16 in a lane, 8 bytes.  Stored so, 32 bytes of a row, the forward of 3200 rows, 1024 -> 4096, took 82 us
 // instead of 72 and the gradients' products 68 and 65 instead of 64 and 60.
-// Two blocks that follow each other: lane groups trade, the even ones keep v, and a lane holds 8 columns.
-RAVEL_DEV u32x4_t join_blocks(f32x4_t v, f32x4_t w) {
-  const auto a = __builtin_amdgcn_permlane16_swap(pack_bf16x2(v[0], v[1]), pack_bf16x2(w[0], w[1]), false, false);
-  const auto b = __builtin_amdgcn_permlane16_swap(pack_bf16x2(v[2], v[3]), pack_bf16x2(w[2], w[3]), false, false);
-  return u32x4_t{a[0], b[0], a[1], b[1]};
-}
 // Lanes l and l ^ 8 trade: afterwards p is of row l16 & 7 and q of row l16 | 8, the lower lanes' columns p's, the upper ones' q's.
 RAVEL_DEV void trade_rows(u32x4_t& p, u32x4_t& q) {
 #pragma unroll
@@ -64,7 +58,7 @@ RAVEL_DEV void put_blocks(float* out, int64_t ld, int m0, int M, int n, int N, i
 RAVEL_DEV void put_blocks(bf16_t* out, int64_t ld, int m0, int M, int n, int N, int lane, f32x4_t v, f32x4_t w) {
   const u32x4_t p = join_blocks(v, w);
   const int m = m0 + (lane & 15);
-  n += ((lane >> 4) & 1) * 16 + (lane >> 5) * 8;
+  n += joined_column(lane);
   if (n < N && m < M) *(u32x4_t*)(out + m * ld + n) = p;
 }
 RAVEL_DEV void put_blocks(float* out, int64_t ld, int m0, int M, int n, int N, int lane, f32x4_t v0, f32x4_t v1, f32x4_t v2, f32x4_t v3) {
@@ -74,7 +68,7 @@ RAVEL_DEV void put_blocks(float* out, int64_t ld, int m0, int M, int n, int N, i
 RAVEL_DEV void put_blocks(bf16_t* out, int64_t ld, int m0, int M, int n, int N, int lane, f32x4_t v0, f32x4_t v1, f32x4_t v2, f32x4_t v3) {
   u32x4_t p = join_blocks(v0, v1), q = join_blocks(v2, v3);
   trade_rows(p, q);
-  put_two_rows(out, ld, m0 + (lane & 7), M, n + (lane & 8) * 4 + ((lane >> 4) & 1) * 16 + (lane >> 5) * 8, N, p, q);
+  put_two_rows(out, ld, m0 + (lane & 7), M, n + (lane & 8) * 4 + joined_column(lane), N, p, q);
 }
 
 // BM x BN outputs a block of WM x WN waves.  AC, BC: A, B lie as rows across the contraction.  O: type of the outputs.

@@ -141,6 +141,14 @@ struct Segments {
 RAVEL_DEV void load_segment(rsrc_t from, char* tile, int seg, unsigned offset) {
   __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_dst_t*)(tile + seg * 1024), 16, (int)offset, 0, 0, 0);
 }
+// Results of two 16 x 16 blocks that follow each other, 4 columns of a row in a lane of each: lane groups trade, the even ones
+// keep v, and a lane holds the 8 columns joined_column on of its row.
+RAVEL_DEV u32x4_t join_blocks(f32x4_t v, f32x4_t w) {
+  const auto a = __builtin_amdgcn_permlane16_swap(pack_bf16x2(v[0], v[1]), pack_bf16x2(w[0], w[1]), false, false);
+  const auto b = __builtin_amdgcn_permlane16_swap(pack_bf16x2(v[2], v[3]), pack_bf16x2(w[2], w[3]), false, false);
+  return u32x4_t{a[0], b[0], a[1], b[1]};
+}
+RAVEL_DEV int joined_column(int lane) { return (lane & 16) + (lane >> 5) * 8; }
 // `bytes` readable bytes from p on, none if negative (uniform); reads behind them give 0
 RAVEL_DEV rsrc_t buffer_from(const void* p, int64_t bytes) {
   const int n = bytes > 0x7fffffff ? 0x7fffffff : bytes < 0 ? 0 : (int)bytes;
