@@ -560,7 +560,7 @@ typedef struct {
   int32_t stream_dtype; /* of x, x_out and their gradients                    */
   int32_t dtype;        /* of f, y and their gradients; RAVEL_BF16 with a
                            RAVEL_BF16 stream                                  */
-  int32_t rows;         /* >= 0                                               */
+  int32_t rows;         /* 0 .. 2^23 - 1                                      */
   int32_t width;        /* multiple of 8, <= 8192                             */
   int32_t mods;         /* rows of gate, scale and shift, >= 1                */
   int32_t group;        /* neighbouring rows that share one, >= 1             */
@@ -620,7 +620,9 @@ typedef struct {
   int32_t n_q_heads;  /* at most 256                            */
   int32_t n_kv_heads; /* divides n_q_heads                      */
   int32_t head_dim;   /* 32, 64, 128 or 256                     */
-  int32_t rows;       /* 0 .. 2^20                              */
+  int32_t rows;       /* 0 .. 2^20; batch * n_kv_heads * tiles of 64 rows
+                         (times query heads of a KV head) or, for dk and
+                         dv, of 64 keys: below 2^24             */
   int32_t keys;       /* 0 .. 2^24                              */
   float scale;        /* of the scores, e.g. 1 / sqrt(head_dim) */
   const int32_t* q_len; /* [batch] or NULL: rows; outside 0..rows: the nearer bound */
@@ -667,9 +669,9 @@ enum { RAVEL_GELU_TANH = 0, RAVEL_SILU = 1 };
 typedef struct {
   int32_t dtype;    /* RAVEL_F32 or RAVEL_BF16, of all tensors      */
   int32_t act;      /* RAVEL_GELU_TANH or RAVEL_SILU                */
-  int32_t rows;     /* >= 0                                         */
-  int32_t width;    /* of x: multiple of 8                          */
-  int32_t hidden;   /* of h: multiple of 8                          */
+  int32_t rows;     /* 0 .. 2^28                                    */
+  int32_t width;    /* of x: multiple of 8, <= 2^18                 */
+  int32_t hidden;   /* of h: multiple of 8, <= 2^18                 */
   int32_t reserved; /* 0 */
   const void* x;    /* [rows, width]                                */
   const void* wg;   /* [hidden, width]                              */

@@ -904,6 +904,12 @@ struct Plan {
 };
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
+// A single key's stride is of no account to the caller, but says where a tile's next rows, zeros, would lie.
+ravel_cross with_key_strides(ravel_cross c) {
+  if (c.keys == 1) c.k_stride[1] = c.v_stride[1] = c.head_dim;
+  return c;
+}
+
 template <typename T, int HD>
 Plan plan_forward(const ravel_cross& c) {
   typedef Shape<T, HD> S;
@@ -924,7 +930,7 @@ hipError_t forward(const ravel_cross& c, hipStream_t s) {
   typedef Shape<T, HD> S;
   const Plan p = plan_forward<T, HD>(c);
   CrossArgs a{};
-  a.c = c;
+  a.c = with_key_strides(c);
   a.G = c.n_q_heads / c.n_kv_heads;
   a.tiles = p.tiles;
   a.splits = p.splits;
@@ -1004,7 +1010,7 @@ hipError_t gradients(const ravel_cross& c, const ravel_cross_grad& g, hipStream_
   typedef Shape<T, HD> S;
   const GradPlan p = plan_grad<T, HD>(c, g);
   CrossArgs a{};
-  a.c = c;
+  a.c = with_key_strides(c);
   a.g = g;
   a.G = c.n_q_heads / c.n_kv_heads;
   a.padded = p.padded;

@@ -451,7 +451,7 @@ hipError_t forward(const ravel_mlp& m, hipStream_t s) {
   MatPlan p = plan_matrix(a.M, a.N, a.K, 1, 1, sizeof(T), false), rest{};
   int first = a.M;
   if (p.tile == 0)
-    for (int64_t round = 1; round <= ceil_div(a.M, 256) * (int64_t)ceil_div(a.N, 256) / 256; ++round) {
+    for (int64_t full = ceil_div(a.M, 256) * (int64_t)ceil_div(a.N, 256) / 256, round = full > 4 ? full - 3 : 1; round <= full; ++round) {
       const int64_t rows = round * 256 / ceil_div(a.N, 256) * 256;
       if (rows < 1 || rows >= a.M) continue;
       const MatPlan q = plan_matrix(a.M - rows, a.N, a.K, 1, 1, sizeof(T), false);
@@ -532,7 +532,7 @@ hipError_t gradients(const ravel_mlp& m, const ravel_mlp_grad& g, hipStream_t s)
     a.A[0] = dg, a.A[1] = du;
     a.B[0] = m.x;
     a.lda = m.hidden;
-    a.ldb = m.x_stride;
+    a.ldb = m.rows > 1 ? m.x_stride : m.width;  // (one row has no stride, but where the next, zeros, would lie)
     a.M = m.hidden, a.N = m.width, a.K = m.rows, a.pairs = 1;
     a.C[0] = g.dwg, a.C[1] = g.dwu;
     a.ldc = g.dw_stride;

@@ -68,7 +68,7 @@ void norm_sizes(Check& k, const ravel_norm* n) {
   k.dtype(n->dtype);
   k.valid(n->stream_dtype != RAVEL_BF16 || n->dtype == RAVEL_BF16, "a bf16 stream needs bf16 blocks");
   k.valid(n->reserved == 0, "reserved must be 0");
-  k.shape(n->rows >= 0 && n->rows <= 1 << 30, "rows must be in 0..2^30");
+  k.shape(n->rows >= 0 && n->rows < 1 << 23, "rows must be in 0..2^23 - 1");  // (times 512 threads below 2^32)
   k.shape(n->width >= 8 && n->width <= 8192 && n->width % 8 == 0, "width must be a multiple of 8 in 8..8192");
   k.shape(n->mods >= 1 && n->mods <= 1 << 30 && n->group >= 1, "mods and group must be >= 1");
 }
@@ -162,7 +162,10 @@ void cross_sizes(Check& k, const ravel_cross* c) {
           "n_q_heads must be a multiple of n_kv_heads, at most 256");
   k.shape(c->rows >= 0 && c->rows <= 1 << 20, "rows must be in 0..2^20");
   k.shape(c->keys >= 0 && c->keys <= 1 << 24, "keys must be in 0..2^24");
-  if (k.ok()) k.shape((int64_t)c->rows * c->n_q_heads <= 1 << 30, "too many rows times heads");
+  if (!k.ok()) return;
+  k.shape((int64_t)c->rows * c->n_q_heads <= 1 << 30, "too many rows times heads");
+  const int64_t heads = (int64_t)c->batch * c->n_kv_heads, all = (int64_t)c->rows * (c->n_q_heads / c->n_kv_heads);
+  k.shape(heads * (all <= 16 ? 1 : all <= 128 ? 2 : (all + 63) / 64) < 1 << 24, "too many rows: a launch holds 2^24 - 1 tiles of 64");
 }
 // Strides of [batch, n, heads, head_dim].  Kernels address the rows, keys and heads of a tile with 24 by 24 bit products.
 void cross_strides(Check& k, const ravel_cross* c, const int64_t* st, int64_t n, int64_t heads, bool output) {
@@ -201,7 +204,10 @@ ravel_status cross_call(const ravel_cross* c, hipStream_t s) {
 void cross_grad_sizes(Check& k, const ravel_cross* c, const ravel_cross_grad* g) {
   cross_sizes(k, c);
   k.valid(g, "null struct");
-  if (k.ok()) k.valid(!g->dk == !g->dv, "dk and dv go together");
+  if (!k.ok()) return;
+  k.valid(!g->dk == !g->dv, "dk and dv go together");
+  const int64_t heads = (int64_t)c->batch * c->n_kv_heads, tiles = c->keys <= 32 ? 1 : c->keys <= 256 ? 4 : (c->keys + 63) / 64;
+  k.shape(!g->dk || heads * tiles < 1 << 24, "too many keys: a launch holds 2^24 - 1 tiles of 64");
 }
 
 ravel_status cross_grad_call(const ravel_cross* c, const ravel_cross_grad* g, hipStream_t s) {

@@ -213,10 +213,10 @@ struct RowBuffer {
 // output's own norm, m = f rf, dm = dF (1 + post): df = rf (dm - m mean(dm m)).  The sums of t^2, dn t and f^2 are
 // formed together; the last one needs dt and comes second.
 //
-// All loads of a row are issued a row ahead (beyond 4096 elements, where registers do not hold two rows, at its start).  Loads and stores are waited for in the order of their issue, and the
-// compiler waits for as many as are certain to have been issued: a row therefore has no branch, only buffers of no
-// length for what is not there (with branches around its stores every row waited for the one before to be stored: 69 us
-// instead of 53 for 6400 x 2048: 4.4 TB/s).
+// All loads of a row are issued a row ahead (beyond 4096 elements, where registers do not hold two rows, at its start).
+// Loads and stores are waited for in the order of their issue, and the compiler waits for as many as are certain to have
+// been issued: a row therefore has no branch, only buffers of no length for what is not there (with branches around its
+// stores every row waited for the one before to be stored: 69 us instead of 53 for 6400 x 2048, which is 4.4 TB/s).
 template <typename S, typename T, int TPR, int NC>
 __global__ __launch_bounds__(TPR * rows_per_block<TPR>()) void norm_residual_grad_kernel(ravel_norm a, ravel_norm_grad g,
                                                                                       GradPlan p) {

@@ -198,3 +198,25 @@ def test_values_that_are_not_finite_reach_only_who_sees_them():
     same[0, :, 2, 5], same[0, 4, 1] = False, False
     assert (out[same] == plain["out"].float()[same]).all()
     assert (got["dq"][1] == plain["dq"][1]).all() and (got["dk"][1] == plain["dk"][1]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [1, 150])
+def test_a_single_key_has_no_stride(dtype, rows):
+    """The stride of a dimension with one index says nothing; values that are not finite meet no 0 that they are not given."""
+    import torch
+    from paper_2609_34170_amd import ravel
+    t = {"bf16": torch.bfloat16, "f32": torch.float32}[dtype]
+    q, dout = (torch.randn(2, rows, 4, 64, device="cuda").to(t) for _ in range(2))
+    k, v = (torch.randn(2, 1, 2, 64, device="cuda").to(t) for _ in range(2))
+    v[1, 0, 1, 5] = float("inf")
+    odd = [x.as_strided(x.shape, (128, 0, 64, 1)) for x in (k, v)]
+    lse = torch.empty(2, 4, rows, device="cuda")
+    out, other = ravel.cross_attention(q, k, v, lse=lse), ravel.cross_attention(q, *odd)
+    assert torch.equal(out, other)
+    # p = exp2(s cs - m) with m = s cs rounded, |s| < 2^7: 1 within 2^-16, divided by itself but for 3 roundings
+    want = v.repeat_interleave(2, 2).expand_as(out)
+    assert torch.equal(out, want) if dtype == "bf16" else torch.allclose(out, want, rtol=2.0 ** -21, atol=0)
+    grads = [ravel.cross_attention_grad(q[:1], a[:1], b[:1], out[:1], lse[:1], dout[:1]) for a, b in ((k, v), odd)]
+    for x, y in zip(*grads):
+        assert torch.equal(x, y) and bool(torch.isfinite(x).all())

@@ -116,3 +116,19 @@ def test_values_that_are_not_finite_stay_in_their_row():
     x[69, 71] = float("nan")
     h = ravel.gated_mlp(x, wg, wu)
     assert torch.isnan(h[69].float()).all() and torch.equal(h[:69], h0[:69])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_single_row_has_no_stride(dtype):
+    """As far as dwg = dg x is infinite where x is, and nothing else."""
+    import torch
+    from paper_2609_34170_amd import ravel
+    t = {"bf16": torch.bfloat16, "f32": torch.float32}[dtype]
+    n = lambda *s: torch.randn(*s, device="cuda").to(t)  # noqa: E731
+    x, wg, wu, dh, gate, up = n(1, 72), n(40, 72), n(40, 72), n(1, 40), n(1, 40), n(1, 40)
+    x[0, 3] = float("inf")
+    odd = x.as_strided((1, 72), (0, 1))
+    got = [ravel.gated_mlp_grad(a, wg, wu, gate, up, dh) for a in (x, odd)]
+    for one, other in zip(*got):
+        assert torch.equal(one, other)
+    assert torch.isinf(got[1][1][:, 3].float()).all() and torch.isfinite(got[1][1][:, 4:].float()).all()

@@ -84,7 +84,7 @@ def _refused(status, want):
 
 BOTH_NORM = [(dict(stream_dtype=2), INVALID), (dict(dtype=-1), INVALID), (dict(stream_dtype=1, dtype=0), INVALID),
              (dict(rows=-1), SHAPE), (dict(width=0), SHAPE), (dict(width=68), SHAPE), (dict(width=8200), SHAPE),
-             (dict(mods=0), SHAPE), (dict(group=0), SHAPE), (dict(eps=0.0), INVALID), (dict(eps=float("nan")), INVALID),
+             (dict(rows=1 << 23), SHAPE), (dict(mods=0), SHAPE), (dict(group=0), SHAPE), (dict(eps=0.0), INVALID), (dict(eps=float("nan")), INVALID),
              (dict(eps=float("inf")), INVALID), (dict(reserved=1), INVALID), (dict(f=_addr(1) + 8), INVALID),
              (dict(gate=_addr(4) + 4), INVALID), (dict(alpha=_addr(3) + 2), INVALID), (dict(f_stride=66), SHAPE),
              (dict(f_stride=-64), SHAPE), (dict(x_out_stride=62), SHAPE), (dict(scale_stride=65), SHAPE),
@@ -125,7 +125,8 @@ BOTH_CROSS = [(dict(dtype=2), INVALID), (dict(batch=-1), SHAPE), (dict(batch=655
               (dict(scale=2.0 ** 101), INVALID), (dict(q=None), INVALID), (dict(k=None), INVALID), (dict(out=None), INVALID),
               (dict(v=_addr(2) + 8), INVALID), (dict(k_len=_addr(9) + 2), INVALID), (dict(q_stride=(4096, 256, 60)), SHAPE),
               (dict(k_stride=(4096, -256, 64)), SHAPE), (dict(v_stride=(4096, 1 << 22, 64)), SHAPE),
-              (dict(q_stride=(1 << 60, 256, 64)), SHAPE)]
+              (dict(q_stride=(1 << 60, 256, 64)), SHAPE),
+              (dict(batch=65535, rows=1 << 20), SHAPE)]  # more tiles than a launch holds
 
 
 @pytest.mark.parametrize("kw,status", BOTH_CROSS + [
@@ -149,6 +150,15 @@ def test_cross_grad_inputs(kw, status):
     (dict(workspace_bytes=64), INVALID)])
 def test_cross_grad(kw, status):
     _refused(_call("ravel_cross_attention_grad", _cross(keys=200), _cross_grad(**kw)), status)
+
+
+def test_cross_grad_tiles_of_keys():
+    n = ctypes.c_int64(0)
+    many = _cross(batch=60000, rows=1, keys=1 << 20)
+    name = "ravel_cross_attention_grad_workspace"
+    _refused(getattr(_ravel().load_library(), name)(ctypes.byref(many), ctypes.byref(_cross_grad()), ctypes.byref(n)), SHAPE)
+    dq = _cross_grad(dk=None, dv=None)
+    assert getattr(_ravel().load_library(), name)(ctypes.byref(many), ctypes.byref(dq), ctypes.byref(n)) == 0
 
 
 BOTH_MLP = [(dict(dtype=2), INVALID), (dict(act=2), INVALID), (dict(rows=-1), SHAPE), (dict(width=60), SHAPE), (dict(width=0), SHAPE),
