@@ -35,7 +35,8 @@ RAVEL_DEV void put4(bf16_t* p, f32x4_t v) { *(u32x2_t*)p = u32x2_t{pack_bf16x2(v
 // Outputs are written in 64 (the forward's) or 128 bytes of a row: a 16 x 16 block leaves the matrix instructions with 4
 // columns of row l16 in a lane, 8 bytes.  Stored so, 32 bytes of a row, the forward of 3200 rows, 1024 -> 4096, took 82 us
 // instead of 72 and the gradients' products 68 and 65 instead of 64 and 60.
-// Lanes l and l ^ 8 trade: afterwards p is of row l16 & 7 and q of row l16 | 8, the lower lanes' columns p's, the upper ones' q's.
+// Lanes l and l ^ 8 trade: afterwards p is of row l16 & 7 and q of row l16 | 8, the lower lanes' columns p's, the upper
+// ones' q's.
 RAVEL_DEV void trade_rows(u32x4_t& p, u32x4_t& q) {
 #pragma unroll
   for (int r = 0; r < 4; ++r) {  // row_ror:8
@@ -72,6 +73,13 @@ RAVEL_DEV void put_blocks(bf16_t* out, int64_t ld, int m0, int M, int n, int N, 
 }
 
 // BM x BN outputs a block of WM x WN waves.  AC, BC: A, B lie as rows across the contraction.  O: type of the outputs.
+//
+// What bounds it: a tile of 256 x 256 outputs and 64 contraction indices takes a CU 2048 clocks of matrix instructions and
+// 2048 of LDS traffic (192 KB of fragments read, 64 KB filled); the two overlap as far as the schedule below lets them, to
+// 3400.  256 x 256 is the largest tile whose sums and two steps' fragments fit the registers of two waves a SIMD; four
+// waves of 128 x 128 would read a third less but spill (1210 us instead of 484).  6400 rows, 2048 <-> 8192: forward 430 us
+// (1.00 PFLOP/s, with its three outputs; the products alone as one library call 403), dx 450 (0.95; 200 blocks for 256
+// CUs), dw 360 (1.19); 3200 rows, 1024 <-> 4096: 72, 63 + 10 for the ranges' sums, and 58.
 template <typename T, typename O, int BM, int BN, int WM, int WN, bool AC, bool BC, int MODE>
 __global__ __launch_bounds__(64 * WM * WN) void mlp_matrix_kernel(MatArgs a) {
   typedef Mat<T> M;
@@ -244,7 +252,8 @@ __global__ __launch_bounds__(64 * WM * WN) void mlp_matrix_kernel(MatArgs a) {
 
 // Few rows (up to 16 MT): the weights are all there is to read, once, so nothing is staged.  A block takes 16 hidden
 // units, its eight waves a range of the contraction each, with every weight of the range (up to 512 bytes a row) requested
-// before the first is used; the waves' sums meet in LDS.
+// before the first is used; the waves' sums meet in LDS.  Bound by HBM: one row, 2048 -> 8192, 13.0 us, 5.2 TB/s; 50 rows,
+// 1024 -> 4096, 8.3 us, of which the chain of loads, products and join is most.
 template <typename T, int MT>
 __global__ __launch_bounds__(512) void mlp_rows_kernel(MatArgs a) {
   typedef Mat<T> M;
@@ -299,7 +308,7 @@ __global__ __launch_bounds__(512) void mlp_rows_kernel(MatArgs a) {
   }
 }
 
-// Ranges of the contraction added in order.
+// Ranges of the contraction added in order, bound by HBM: 4 ranges of 3200 x 1024, 10 us, 5.9 TB/s (they lie in cache in part).
 template <typename O>
 __global__ __launch_bounds__(256) void mlp_sum_kernel(const float* part, int splits, int64_t range, O* c0, O* c1, int64_t ldc,
                                                       int M, int N) {
@@ -314,7 +323,10 @@ __global__ __launch_bounds__(256) void mlp_sum_kernel(const float* part, int spl
   put4((blockIdx.y ? c1 : c0) + m * ldc + n, s);
 }
 
-// The hidden gradients, dg = dh u act'(g) and du = dh act(g), [rows, hidden] each.
+// The hidden gradients, dg = dh u act'(g) and du = dh act(g), [rows, hidden] each.  In bf16 calls they are rounded to it: they
+// are the operands of two matrix products, which take bf16, and written once instead of formed in each of the products' blocks.
+// With gate and up that makes 3.1e-3 against 64 bits where rounding the results alone gives 1.7e-3.  Bound by HBM: three
+// tensors read, two written, 6400 x 8192 in 95 to 102 us, 5.1 to 5.5 TB/s.
 RAVEL_DEV void act_grad(float x, int kind, float& y, float& slope) {
   if (kind == RAVEL_SILU) {
     const float s = 1.f / (1.f + __expf(-x));

