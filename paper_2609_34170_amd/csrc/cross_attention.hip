@@ -596,6 +596,7 @@ __global__ __launch_bounds__(256, (4 * Tiles<T, HD, TR>::BYTES <= 65536 && Tiles
     lds_char_t* const ot = (lds_char_t*)oc + wr * TRW * RB;
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
+      if (sizeof(T) == 4 && p > 0 && t * TR + wr * TRW + p * M::CK >= live) break;  // (32-bit products take long: 71 rows over 2499 keys 193 us from 219, with the forward and dq)
       const auto at = at0.fresh();
       f32x4_t s[KI][FP], dp[KI][FP], lse[FP];
 #pragma unroll
@@ -967,7 +968,7 @@ hipError_t forward(const ravel_cross& c, hipStream_t s) {
 
 struct GradPlan {
   int qtiles, qsplits, ktiles, ksplits, padded;
-  bool few_rows, few_keys, one_pass;
+  bool few_rows, few_keys, one_pass, half;
   size_t stat, part;
 };
 template <typename T, int HD>
@@ -990,7 +991,10 @@ GradPlan plan_grad(const ravel_cross& c, const ravel_cross_grad& g) {
   if (p.qsplits > 1) p.part = (size_t)p.qsplits * heads * all * HD * 4;
   if (g.dk) {
     p.few_keys = c.keys <= 64;
-    const int kper = p.few_keys ? 16 * (4 / S::RW) : 64 * S::BI, tr = p.few_keys ? S::TR : S::TK;
+    // blocks of half as many keys where they do not fill the CUs (4 heads of 32 dims in 32 bits, 4 x 601 rows over 72 keys, all
+    // gradients: 40 us from 49; elsewhere within 2 %)
+    p.half = S::BI == 2 && !p.few_keys && heads * ((c.keys + 127) / 128) < kFill / 2;
+    const int kper = p.few_keys ? 16 * (4 / S::RW) : p.half ? 64 : 64 * S::BI, tr = p.few_keys ? S::TR : S::TK;
     p.ktiles = (c.keys + kper - 1) / kper;
     p.ksplits = ranges(heads * p.ktiles, (all + tr - 1) / tr, p.few_keys ? 1 : 4, kFill);
     p.stat = round256((size_t)heads * p.padded * 2 * 4);
@@ -1071,6 +1075,8 @@ hipError_t gradients(const ravel_cross& c, const ravel_cross_grad& g, hipStream_
   const dim3 grid((unsigned)(heads * a.tiles * a.splits));
   if (p.few_keys)
     cross_dkv_kernel<T, HD, 1, S::RW, S::TR><<<grid, 256, 0, s>>>(a);
+  else if (p.half)
+    cross_dkv_kernel<T, HD, 1, 1, S::TK><<<grid, 256, 0, s>>>(a);
   else
     cross_dkv_kernel<T, HD, S::BI, 1, S::TK><<<grid, 256, 0, s>>>(a);
   if ((e = hipGetLastError()) != hipSuccess || !a.part) return e;
