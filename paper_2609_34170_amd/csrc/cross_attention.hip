@@ -695,8 +695,8 @@ __global__ __launch_bounds__(256, (4 * Tiles<T, HD, TR>::BYTES <= 65536 && Tiles
 // ---------------------------------------------------------------------------
 // Every row tile sees all keys, so its scores serve dq and, through LDS (the contraction over rows needs them as columns),
 // its share of dk and dv as well: q and dout are read once, not by two passes (with 16 keys of 256 dims 64 x 400 rows
-// take 17 us, 2.3 TB/s, and 4.6 for the ranges' sums, instead of 37 and 4.6; a block's chain of load, products, exchange
-// and products, four tiles long, bounds it).  A wave takes 16 rows, or where a tile has fewer than 64 a part of their dims;
+// take 17 us, 3.3 TB/s with the ranges' sums, and 4.6 to add these, instead of 37 and 4.6; a block's chain of load,
+// products, exchange and products, two tiles long, bounds it).  A wave takes 16 rows, or where a tile has fewer than 64 a part of their dims;
 // for dk and dv the dims are dealt out to the waves.
 template <typename T, int HD, int KF, int TR>
 __global__ __launch_bounds__(256) void cross_few_keys_grad_kernel(CrossArgs a) {
