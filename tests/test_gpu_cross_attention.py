@@ -98,6 +98,15 @@ def test_forward_and_gradients(dtype, heads, B, R, K, q_len, k_len):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hd", [32, 64, 128, 256])
+def test_heads_that_fill_the_chip(hd, dtype):
+    """Blocks of the most rows and keys, in the forward and both gradients, with lengths that end inside their tiles."""
+    c = _case(dtype, (8, 4, hd), 16, 201, 391, [201, 0, 130, 65, 64, 1, 33, 200] * 2, [391, 100, 0, 1, 65, 128, 129, 385] * 2)
+    _, _, got = _run(c)
+    _compare(c, got)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_strided_tensors(dtype):
     c = _case(dtype, ODD, 2, 21, 70, [21, 8], [70, 33])
     _, _, plain = _run(c)

@@ -43,7 +43,12 @@ def _near(got, want, tol, name):
     ("bf16", "silu", 65, 1000, 136, 0, False), ("bf16", "gelu", 200, 264, 520, 16, True), ("f32", "silu", 77, 328, 888, 0, False),
     ("bf16", "gelu", 700, 256, 1032, 0, False), ("bf16", "silu", 1111, 136, 2056, 0, False), ("f32", "gelu", 300, 72, 264, 0, False),
     ("bf16", "gelu", 2100, 520, 4096, 0, False), ("bf16", "silu", 4200, 264, 4096, 8, False),  # the last: rows in two pieces
-    ("f32", "gelu", 513, 1032, 520, 0, False)])
+    ("f32", "gelu", 513, 1032, 520, 0, False),
+    # every tile of the gradients' products, whole and in ranges of the contraction
+    ("bf16", "gelu", 70, 72, 8200, 0, False), ("bf16", "silu", 70, 1544, 2568, 8, False), ("bf16", "gelu", 70, 1544, 2568, 0, True),
+    ("bf16", "gelu", 777, 2568, 72, 0, False), ("bf16", "silu", 2100, 4104, 72, 8, False), ("bf16", "silu", 3000, 72, 4104, 0, False),
+    ("bf16", "gelu", 4200, 136, 6152, 8, True), ("bf16", "silu", 4200, 136, 6152, 0, False), ("f32", "gelu", 70, 1032, 1544, 4, False),
+    ("f32", "silu", 520, 72, 4104, 0, False), ("f32", "gelu", 3000, 1032, 72, 0, False), ("f32", "silu", 70, 4104, 520, 0, False)])
 def test_forward_and_gradients(dtype, kind, M, K, F, pad, wide):
     import torch
     from paper_2609_34170_amd import ravel
