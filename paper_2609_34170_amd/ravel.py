@@ -593,14 +593,15 @@ _tools = None
 
 
 def _layer_tools():
-    """(torch, library, torch's types as RAVEL_*, device -> its current stream's handle)"""
+    """(torch, library, torch's types as RAVEL_*, (device -> its current stream's handle, the current device))"""
     global _tools
     if _tools is None:
         import torch
 
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
             lambda device: torch.cuda.current_stream(device).cuda_stream)
-        _tools = torch, load_library(), {torch.float32: F32, torch.bfloat16: BF16}, raw
+        here = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device  # (there is a tensor on a GPU by then)
+        _tools = torch, load_library(), {torch.float32: F32, torch.bfloat16: BF16}, (raw, here)
     return _tools
 
 
@@ -610,7 +611,7 @@ _HERE = contextlib.nullcontext()
 def _place(stream, first, *rest):
     """(guard, handle): a context that makes the tensors' device and the call's stream current, for the launches and what
     the call allocates, and the stream's handle."""
-    torch, _, _, raw = _tools or _layer_tools()
+    torch, _, _, (raw, here) = _tools or _layer_tools()
     device = first.get_device()
     if device < 0:
         raise ValueError("the call needs its tensors on a GPU")
@@ -618,7 +619,7 @@ def _place(stream, first, *rest):
         if t is not None and t.get_device() != device:
             raise ValueError(f"every tensor of the call must be on {first.device}")
     if stream is None:
-        return (_HERE if device == torch.cuda.current_device() else torch.cuda.device(device)), raw(device)
+        return (_HERE if device == here() else torch.cuda.device(device)), raw(device)
     if isinstance(stream, int):
         stream = torch.cuda.ExternalStream(stream, device=first.device)
     elif stream.device != first.device:
@@ -647,6 +648,10 @@ def _rows2(name, t, shape, dtype):
     """(address, row stride) of a matrix, or (0, 0) for None."""
     if t is None:
         return 0, 0
+    if t.shape == shape and t.dtype is dtype:
+        row, one = t.stride()
+        if one == 1:
+            return t.data_ptr(), row
     return t.data_ptr(), _like(name, t, shape, dtype)[0]
 
 

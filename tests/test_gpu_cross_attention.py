@@ -229,3 +229,35 @@ def test_a_single_key_has_no_stride(dtype, rows):
     grads = [ravel.cross_attention_grad(q[:1], a[:1], b[:1], out[:1], lse[:1], dout[:1]) for a, b in ((k, v), odd)]
     for x, y in zip(*grads):
         assert torch.equal(x, y) and bool(torch.isfinite(x).all())
+
+
+def test_offsets_beyond_32_bits():
+    """Keys, values and their gradients of more than 2^31 elements; the weight lies on keys at both ends and between."""
+    import torch
+    from paper_2609_34170_amd import ravel
+    K, hd, at = (1 << 23) + 77, 256, [3, 1 << 22, (1 << 23) - 1, (1 << 23) + 76]
+    q = torch.ones(1, 1, 1, hd, device="cuda", dtype=torch.bfloat16)
+    k = torch.zeros(1, K, 1, hd, device="cuda", dtype=torch.bfloat16)
+    v = torch.zeros_like(k)
+    r = torch.Generator(device="cuda").manual_seed(5)
+    for i, n in enumerate(at):
+        k[0, n] = 1.5 + 0.0625 * i  # scores 24 + i against 0: all weight but 2^23 e^-24 (3e-4)
+        v[0, n] = torch.randn(1, hd, generator=r, device="cuda").bfloat16()
+    dout = torch.randn(1, 1, 1, hd, generator=r, device="cuda").bfloat16()
+    lse = torch.empty(1, 1, 1, device="cuda")
+    out = ravel.cross_attention(q, k, v, lse=lse)
+    dq, dk, dv = ravel.cross_attention_grad(q, k, v, out, lse, dout)
+    s = torch.tensor([24.0 + i for i in range(4)], dtype=torch.float64)
+    p = s.exp() / (s.exp().sum() + (K - 4))
+    near, d = v[0, at, 0].double().cpu(), dout.double().cpu().view(hd)
+    want = p @ near
+    # probabilities and results are rounded once each (2^-8 relative)
+    tol = 2.0 ** -8 * (p @ near.abs()) + 2.0 ** -8 * want.abs() + 1e-5
+    assert ((out.double().cpu().view(hd) - want).abs() <= tol).all()
+    assert ((dv[0, at, 0].double().cpu() - p[:, None] * d).abs() <= 2.0 ** -7 * p[:, None] * d.abs() + 1e-7).all()
+    # ds = p (dout v - dout out) / 16 with out as it was rounded
+    ds = p * (near @ d - out.double().cpu().view(hd) @ d) / 16
+    assert ((dk[0, at, 0].double().cpu() - ds[:, None]).abs() <= 2.0 ** -6 * ds.abs()[:, None] + 1e-5).all()
+    others = torch.ones(K, dtype=torch.bool, device="cuda")
+    others[at] = False
+    assert float(dv[0, others].abs().max()) <= 1e-9 and bool(torch.isfinite(dq).all())
