@@ -620,9 +620,10 @@ typedef struct {
   int32_t n_q_heads;  /* at most 256                            */
   int32_t n_kv_heads; /* divides n_q_heads                      */
   int32_t head_dim;   /* 32, 64, 128 or 256                     */
-  int32_t rows;       /* 0 .. 2^20; batch * n_kv_heads * tiles of 64 rows
+  int32_t rows;       /* 0 .. 2^20; batch * n_kv_heads * tiles of rows
                          (times query heads of a KV head) or, for dk and
-                         dv, of 64 keys: below 2^24             */
+                         dv, of keys: below 2^24 (tiles of at least 64;
+                         of 16 up to 32 rows or 64 keys)        */
   int32_t keys;       /* 0 .. 2^24                              */
   float scale;        /* of the scores, e.g. 1 / sqrt(head_dim) */
   const int32_t* q_len; /* [batch] or NULL: rows; outside 0..rows: the nearer bound */

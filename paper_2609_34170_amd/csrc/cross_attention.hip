@@ -16,6 +16,8 @@
 // that the sums leave registers for, cover each other in part: matrix instructions are busy 43 to 46 % of the time.  16 x
 // 800 rows of 16 heads over 2048 keys of 4 heads, 128 dims: forward 247 us (870 TFLOP/s), dq 336 (959), dk and dv 379
 // (1133); with lengths of 512 to 2048 and one of 0 150, 200 and 355.
+#include <algorithm>
+
 #include "layer.h"
 #include "lds_tile.h"
 
@@ -33,7 +35,7 @@ struct CrossArgs {
   ravel_cross c;
   ravel_cross_grad g;
   int G, tiles, splits;  // query heads of a KV head; tiles of what the blocks own; ranges of what they walk
-  int padded;            // rows of stat (and of a partial) per (batch row, KV head)
+  int padded;            // rows of stat per (batch row, KV head): whole tiles of the pass that writes it
   float* part;           // partial results [split][batch][KV head][row or key][head_dim], or null
   float* part_ml;        // forward: [split][batch][KV head][row][2], maximum (log2 units) and sum
   float* stat;           // gradients: [2][batch][KV head][padded]: -lse / scale (f32: -lse log2 e) and -D
@@ -555,7 +557,7 @@ __global__ __launch_bounds__(256, (4 * Tiles<T, HD, TR>::BYTES <= 65536 && Tiles
   const auto issue = [&](int t, char* qt, char* ot, float* st) {
     const auto seg = seg0.fresh();
     if (wave < 2) {  // one of lse and D (through LDS: loads into registers would wait for the tiles issued before them)
-      const rsrc_t from = buffer_from(stat + wave * apart + t * TR);
+      const rsrc_t from = buffer_from(stat + wave * apart + t * TR, (int64_t)(live - t * TR) * 4);  // 0 behind the last row
 #pragma unroll
       for (int i = 0; i < TS / 64; ++i)
         __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_dst_t*)(st + wave * TS + i * 64), 4,
@@ -983,11 +985,11 @@ GradPlan plan_grad(const ravel_cross& c, const ravel_cross_grad& g) {
     p.part = g.dk && p.ksplits > 1 ? round256((size_t)p.ksplits * heads * c.keys * HD * 4 * 2) : 0;
     return p;
   }
-  p.padded = (all + 127) / 128 * 128;  // whole tiles of either pass: every row that one reads has its lse and D
-  p.few_rows = all <= 32 || heads * (p.padded / (64 * S::BI)) < kFill / 2;
+  p.few_rows = all <= 32 || heads * ((all + 64 * S::BI - 1) / (64 * S::BI)) < kFill / 2;
   const int per = p.few_rows ? 16 * (4 / S::KW) : 64 * S::BI, tk = p.few_rows ? S::TF : S::TK;
-  p.qtiles = p.padded / per;
-  p.qsplits = g.dq ? ranges(heads * ((all + per - 1) / per), (c.keys + tk - 1) / tk, 4, p.few_rows ? 3 * kFill : kFill) : 1;
+  p.qtiles = (all + per - 1) / per;
+  p.padded = p.qtiles * per;
+  p.qsplits = g.dq ? ranges(heads * p.qtiles, (c.keys + tk - 1) / tk, 4, p.few_rows ? 3 * kFill : kFill) : 1;
   if (p.qsplits > 1) p.part = (size_t)p.qsplits * heads * all * HD * 4;
   if (g.dk) {
     p.few_keys = c.keys <= 64;
@@ -1098,6 +1100,20 @@ auto by_shape(const ravel_cross& c, F f) {
 
 }  // namespace
 
+int64_t cross_blocks(const ravel_cross& c) {
+  const int64_t heads = (int64_t)c.batch * c.n_kv_heads;
+  return by_shape(c, [&](auto t, auto hd) {
+    const Plan p = plan_forward<decltype(t), hd.value>(c);
+    return heads * p.tiles * p.splits;
+  });
+}
+int64_t cross_grad_blocks(const ravel_cross& c, const ravel_cross_grad& g) {
+  const int64_t heads = (int64_t)c.batch * c.n_kv_heads;
+  return by_shape(c, [&](auto t, auto hd) {
+    const GradPlan p = plan_grad<decltype(t), hd.value>(c, g);
+    return heads * std::max((int64_t)p.qtiles * p.qsplits, (int64_t)(p.one_pass ? 1 : p.ktiles) * p.ksplits);
+  });
+}
 size_t cross_workspace(const ravel_cross& c) {
   return by_shape(c, [&](auto t, auto hd) { return plan_forward<decltype(t), hd.value>(c).bytes; });
 }

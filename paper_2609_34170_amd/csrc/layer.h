@@ -19,8 +19,10 @@ hipError_t launch_norm_residual(const ravel_norm& n, hipStream_t s);
 size_t norm_grad_workspace(const ravel_norm& n, const ravel_norm_grad& g);
 hipError_t launch_norm_residual_grad(const ravel_norm& n, const ravel_norm_grad& g, hipStream_t s);
 
+int64_t cross_blocks(const ravel_cross& c);  // of the largest launch
 size_t cross_workspace(const ravel_cross& c);
 hipError_t launch_cross_attention(const ravel_cross& c, hipStream_t s);
+int64_t cross_grad_blocks(const ravel_cross& c, const ravel_cross_grad& g);
 size_t cross_grad_workspace(const ravel_cross& c, const ravel_cross_grad& g);
 hipError_t launch_cross_attention_grad(const ravel_cross& c, const ravel_cross_grad& g, hipStream_t s);
 

@@ -56,6 +56,7 @@ struct Check {
     return e == hipSuccess ? RAVEL_OK : set_error(RAVEL_E_HIP, std::string(call) + ": " + hipGetErrorString(e));
   }
 };
+constexpr int64_t kBlocks = 1 << 24;  // blocks of 256 threads: below 2^32 of them in a launch
 int bytes_of(int32_t dtype) { return dtype == RAVEL_F32 ? 4 : 2; }
 
 // ---------------------------------------------------------------------------
@@ -164,8 +165,7 @@ void cross_sizes(Check& k, const ravel_cross* c) {
   k.shape(c->keys >= 0 && c->keys <= 1 << 24, "keys must be in 0..2^24");
   if (!k.ok()) return;
   k.shape((int64_t)c->rows * c->n_q_heads <= 1 << 30, "too many rows times heads");
-  const int64_t heads = (int64_t)c->batch * c->n_kv_heads, all = (int64_t)c->rows * (c->n_q_heads / c->n_kv_heads);
-  k.shape(heads * (all <= 16 ? 1 : all <= 128 ? 2 : (all + 63) / 64) < 1 << 24, "too many rows: a launch holds 2^24 - 1 tiles of 64");
+  if (k.ok()) k.shape(cross_blocks(*c) < kBlocks, "too many rows: a launch holds 2^24 - 1 tiles");
 }
 // Strides of [batch, n, heads, head_dim].  Kernels address the rows, keys and heads of a tile with 24 by 24 bit products.
 void cross_strides(Check& k, const ravel_cross* c, const int64_t* st, int64_t n, int64_t heads, bool output) {
@@ -206,8 +206,7 @@ void cross_grad_sizes(Check& k, const ravel_cross* c, const ravel_cross_grad* g)
   k.valid(g, "null struct");
   if (!k.ok()) return;
   k.valid(!g->dk == !g->dv, "dk and dv go together");
-  const int64_t heads = (int64_t)c->batch * c->n_kv_heads, tiles = c->keys <= 32 ? 1 : c->keys <= 256 ? 4 : (c->keys + 63) / 64;
-  k.shape(!g->dk || heads * tiles < 1 << 24, "too many keys: a launch holds 2^24 - 1 tiles of 64");
+  if (k.ok()) k.shape(cross_grad_blocks(*c, *g) < kBlocks, "too many rows or keys: a launch holds 2^24 - 1 tiles");
 }
 
 ravel_status cross_grad_call(const ravel_cross* c, const ravel_cross_grad* g, hipStream_t s) {
