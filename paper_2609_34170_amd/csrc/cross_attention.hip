@@ -116,24 +116,24 @@ RAVEL_DEV void load_keys(const Segments<T, HD * sizeof(T)>& at, const T* head, i
     load_segment(from, tile, seg, row + at.byte_of(seg) + seg * at.ROWS * step);
   }
 }
-// Rows [first, first + TR) of a (batch row, KV head)'s row space; rows from `end` on are zeros.  head: row 0 of the first
-// query head.  Quotients by G through its reciprocal `inv` = ceil(2^23 / G), exact for what is below 2^23 / G.
+// Rows [first, first + TR) of a (batch row, KV head)'s row space; rows from `end` on are zeros, or with REPEAT the last row (there
+// is one) again.  head: row 0 of the first query head.  Quotients by G through its reciprocal `inv` = ceil(2^23 / G), exact for what is below 2^23 / G.
 struct RowSpace {
   int G, inv;
 };
-template <typename T, int HD, int TR>
+template <typename T, int HD, int TR, bool REPEAT = false>
 RAVEL_DEV void load_rows(const Segments<T, HD * sizeof(T)>& at, const T* head, int64_t row_stride, int head_stride, RowSpace sp, int first,
                          int end, char* tile, int wave) {
   typedef Tiles<T, HD, TR> Z;
-  const int i0 = first / sp.G, rest = first - i0 * sp.G;
+  const int i0 = first / sp.G, rest = first - i0 * sp.G, last = end - 1 - first;
   const rsrc_t from = buffer_from(head + i0 * row_stride);
 #pragma unroll
   for (int i = 0; i < Z::SEGS; ++i) {
     const int seg = wave * Z::SEGS + i, r = seg * at.ROWS + at.row;
     if (Z::BYTES % 4096 && seg * 1024 >= Z::BYTES) break;
-    const unsigned x = rest + r, q = __umul24(x, sp.inv) >> 23, g = x - __umul24(q, sp.G);
+    const unsigned x = rest + (REPEAT ? min(r, last) : r), q = __umul24(x, sp.inv) >> 23, g = x - __umul24(q, sp.G);
     const unsigned off = __umul24(q, (unsigned)row_stride * (unsigned)sizeof(T)) + __umul24(g, head_stride * (unsigned)sizeof(T));
-    load_segment(from, tile, seg, first + r < end ? off + at.byte_of(seg) : kOutside);
+    load_segment(from, tile, seg, REPEAT || r <= last ? off + at.byte_of(seg) : kOutside);
   }
 }
 
@@ -554,16 +554,20 @@ __global__ __launch_bounds__(256, (4 * Tiles<T, HD, TR>::BYTES <= 65536 && Tiles
   const size_t apart = (size_t)c.batch * c.n_kv_heads * a.padded;  // from lse to D
   const RowSpace space{a.G, ((1 << 23) + a.G - 1) / a.G};
   const Segments<T, RB> seg0(lane);
+  // Rows that do not exist take part as the last one again, with zeros for dout and D: their gradients are 0 times what the last
+  // row has (as rows of zeros they would make an infinite key's score 0 times infinity).
   const auto issue = [&](int t, char* qt, char* ot, float* st) {
     const auto seg = seg0.fresh();
     if (wave < 2) {  // one of lse and D (through LDS: loads into registers would wait for the tiles issued before them)
-      const rsrc_t from = buffer_from(stat + wave * apart + t * TR, (int64_t)(live - t * TR) * 4);  // 0 behind the last row
+      const rsrc_t from = buffer_from(stat + wave * apart + t * TR);
+      const int last = live - t * TR - 1;
+      const unsigned behind = wave == 0 ? last * 4u : kOutside;
 #pragma unroll
       for (int i = 0; i < TS / 64; ++i)
         __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_dst_t*)(st + wave * TS + i * 64), 4,
-                                                 (int)(lane < TR ? (i * 64 + lane) * 4 : kOutside), 0, 0, 0);
+                                                 (int)(i * 64 + lane <= last ? (i * 64 + lane) * 4u : behind), 0, 0, 0);
     }
-    load_rows<T, HD, TR>(seg, q, c.q_stride[1], (int)c.q_stride[2], space, t * TR, live, qt, wave);
+    load_rows<T, HD, TR, true>(seg, q, c.q_stride[1], (int)c.q_stride[2], space, t * TR, live, qt, wave);
     load_rows<T, HD, TR>(seg, dout, g.dout_stride[1], (int)g.dout_stride[2], space, t * TR, live, ot, wave);
   };
   if (t0 < t1) issue(t0, q0, o0, s0);
@@ -749,7 +753,7 @@ __global__ __launch_bounds__(256) void cross_few_keys_grad_kernel(CrossArgs a) {
     load_rows<T, HD, TR>(seg, dout, g.dout_stride[1], (int)g.dout_stride[2], space, t * TR, live, ot, wave);
     const int r = t * TR + rf * 16 + l16, qr = r / a.G, gh = w.h * a.G + r - qr * a.G;
     const bool in = r < live;
-    const float lse = in ? c.lse[((size_t)w.b * c.n_q_heads + gh) * c.rows + qr] * kLog2e : INFINITY;
+    const float lse = in ? c.lse[((size_t)w.b * c.n_q_heads + gh) * c.rows + qr] * kLog2e : 0.f;
     tile_barrier<0>();
     const auto at = at0.fresh();
     f32x4_t s[2], dp[2];
@@ -768,19 +772,21 @@ __global__ __launch_bounds__(256) void cross_few_keys_grad_kernel(CrossArgs a) {
         dp[f] = M::mma(at.along_row((lds_char_t*)vt, f, x), of, dp[f]);
       }
     }
-    float D = 0.f;  // sum p dout v^T, which is dout out before out was rounded
+    // D = sum p dout v^T, which is dout out before out was rounded.  Rows that do not exist are selected away: their zeros times
+    // an infinite key or value are not 0.
+    float D = 0.f;
 #pragma unroll
     for (int f = 0; f < KF; ++f)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        s[f][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[f][i], cs, -lse));
+        s[f][i] = in ? __builtin_amdgcn_exp2f(__builtin_fmaf(s[f][i], cs, -lse)) : 0.f;
         D += s[f][i] * dp[f][i];
       }
     D = column_sum(D);
 #pragma unroll
     for (int f = 0; f < KF; ++f)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) dp[f][i] = s[f][i] * (dp[f][i] - D);
+      for (int i = 0; i < 4; ++i) dp[f][i] = in ? s[f][i] * (dp[f][i] - D) : 0.f;
     if (dw == 0) {  // columns 16 f + 4 grp .. + 3 of the row's probabilities and their gradients
       const int row = rf * 16 + l16;
 #pragma unroll
