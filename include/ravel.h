@@ -613,7 +613,7 @@ ravel_status ravel_norm_residual_grad(const ravel_norm* norm, const ravel_norm_g
  * for all rows of a batch row without keys.  lse, if given, is the logarithm of each row's sum of
  * exp(scale q k), -infinity for rows that are 0.  Scores, softmax and sums are in 32 bits; in bf16
  * calls probabilities (and in the gradients the scores') are rounded to bf16 before they are
- * multiplied, outputs at the end.  scale is in 0..2^100. */
+ * multiplied, outputs at the end.  scale is 0 or in 2^-100..2^100. */
 typedef struct {
   int32_t dtype; /* RAVEL_F32 or RAVEL_BF16: q, k, v, out and their gradients */
   int32_t batch;

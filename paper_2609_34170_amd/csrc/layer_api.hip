@@ -155,8 +155,9 @@ void cross_sizes(Check& k, const ravel_cross* c) {
   k.valid(c, "null struct");
   if (!k.ok()) return;
   k.dtype(c->dtype);
-  // (times log2 e it has to stay finite: 0 times infinity is not 0)
-  k.valid(c->scale >= 0.f && c->scale <= 0x1p100f, "scale must be in 0..2^100");
+  // (times log2 e it has to stay finite: 0 times infinity is not 0; and so has the logarithm of a row's sum over the scale, from
+  // which the gradients' scores start)
+  k.valid(c->scale == 0.f || (c->scale >= 0x1p-100f && c->scale <= 0x1p100f), "scale must be 0 or in 2^-100..2^100");
   k.shape(c->batch >= 0 && c->batch <= 65535, "batch must be in 0..65535");
   k.shape(c->head_dim == 32 || c->head_dim == 64 || c->head_dim == 128 || c->head_dim == 256, "head_dim must be 32, 64, 128 or 256");
   k.shape(c->n_kv_heads >= 1 && c->n_q_heads >= 1 && c->n_q_heads <= 256 && c->n_q_heads % c->n_kv_heads == 0,
