@@ -305,7 +305,7 @@ __global__ __launch_bounds__(TPR * rows_per_block<TPR>()) void norm_residual_gra
       v[2] += sum4(f[c] * f[c]);
     }
     row_sum<TPR>(v, part, 0);
-    const float r = 1.f / sqrtf(v[0] * inv + a.eps), k = r * r * (v[1] * inv);
+    const float r = 1.f / sqrtf(v[0] * inv + a.eps), k = r * (r * (v[1] * inv));  // (r r may overflow)
     const float rf = post_of != 0.f ? 1.f / sqrtf(v[2] * inv + a.eps) : 1.f;
     const RowBuffer dx(g.dx, g.dx_stride, row, a.width, sizeof(S), in), df(g.df, g.df_stride, row, a.width, sizeof(T), in);
     float u[1] = {0.f};
