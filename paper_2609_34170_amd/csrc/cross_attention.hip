@@ -274,6 +274,7 @@ __global__ __launch_bounds__(256, (4 * Tiles<T, HD, TK>::BYTES <= 65536 ? 2 : 1)
     step(t, k0, v0, k1, v1);
     if (t + 1 < t1) step(t + 1, k1, v1, k0, v0);
   }
+  results_ready(o);
 #pragma unroll
   for (int i = 0; i < MI; ++i) l[i] = column_sum(l[i]);
   if constexpr (KW > 1) {  // the waves that share rows: wave wk = 0 takes their sum
@@ -486,6 +487,7 @@ __global__ __launch_bounds__(256, (4 * Tiles<T, HD, TK>::BYTES <= 65536 ? 2 : 1)
     step(t, k0, v0, k1, v1);
     if (t + 1 < t1) step(t + 1, k1, v1, k0, v0);
   }
+  results_ready(dq);
   if constexpr (KW > 1) {  // the waves that share rows: wave wk = 0 takes their sum
     const auto sums = [&](int w) { return (float*)(w == 0 ? k0 : w == 1 ? v0 : w == 2 ? k1 : v1); };
     __syncthreads();
@@ -649,6 +651,8 @@ __global__ __launch_bounds__(256, (4 * Tiles<T, HD, TR>::BYTES <= 65536 && Tiles
     step(t, q0, o0, s0, q1, o1, s1);
     if (t + 1 < t1) step(t + 1, q1, o1, s1, q0, o0, s0);
   }
+  results_ready(dk);
+  results_ready(dv);
   if constexpr (RW > 1) {  // the waves that share keys: wave wr = 0 takes their sum, dv first, then dk
     const auto sums = [&](int w) { return (float*)(w == 0 ? q0 : w == 1 ? o0 : w == 2 ? q1 : o1); };
     float* const mine = sums(wave);
@@ -844,6 +848,8 @@ __global__ __launch_bounds__(256) void cross_few_keys_grad_kernel(CrossArgs a) {
     __syncthreads();
   }
   if (!g.dk) return;
+  results_ready(dk);
+  results_ready(dv);
 #pragma unroll
   for (int f = 0; f < KF; ++f) {
     const int key = f * 16 + l16;

@@ -199,6 +199,7 @@ __global__ __launch_bounds__(64 * WM * WN) void mlp_matrix_kernel(MatArgs a) {
       if (t + 1 < k1) tile(t + 1, As1, Bs1, As0, Bs0);
     }
   }
+  results_ready(acc);
 
   // acc[i][j] is row l16, columns 4 grp .. + 3 of its 16 x 16 block
 #pragma unroll
@@ -290,6 +291,7 @@ __global__ __launch_bounds__(512) void mlp_rows_kernel(MatArgs a) {
         acc[1][i] = M::mma(u[j], x[j][i], acc[1][i]);
       }
   }
+  results_ready(acc);
 #pragma unroll
   for (int i = 0; i < MT; ++i) part[wave][0][i][lane] = acc[0][i], part[wave][1][i][lane] = acc[1][i];
   __syncthreads();

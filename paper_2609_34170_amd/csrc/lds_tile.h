@@ -169,6 +169,20 @@ RAVEL_DEV void tile_barrier() {
   __atomic_signal_fence(__ATOMIC_SEQ_CST);
 }
 
+// Sums of matrix instructions, before they are used by others behind a loop or a branch: 16 wait states, where the 16 x 16
+// products need 8 (bf16) and 10 (32 bits).  The compiler leaves them itself, but has been seen to leave too few where a uniform
+// branch skips a few instructions; once a block costs nothing.  What uses a result comes behind the asm that names it; copies
+// that the compiler puts in front of that, as everything in a loop, are found by tests/test_machine_code.py.
+template <int N, int M>
+RAVEL_DEV void results_ready(f32x4_t (&acc)[N][M]) {
+  asm volatile("s_nop 15" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int j = 0; j < M; ++j) asm volatile("" : "+v"(acc[i][j]));
+}
+
 // Instructions of the region up to here in this order: N of a kind (LDS_READS, GLOBAL_LOADS), each followed by its share
 // of PRODUCTS matrix instructions, so that neither waits for the other's queue.
 enum { MATRIX = 0x8, GLOBAL_LOADS = 0x20, LDS_READS = 0x100 };
