@@ -585,24 +585,39 @@ class Cache:
 # A layer's operators (ravel_norm_residual, ravel_cross_attention, ravel_gated_mlp and their gradients)
 #
 # Tensors are the caller's, on one GPU; outputs that are not given are allocated.  Calls are enqueued on ``stream``
-# (default: torch's current one of that GPU).
+# (default: torch's current one of that GPU).  Automatic differentiation does not record them: results belong to no graph,
+# whatever their inputs, and a program that trains calls them, forward and gradients, from a torch.autograd.Function of its own
+# or forms the gradients itself.  What a call writes counts as written, so that a saved tensor that is overwritten is noticed;
+# an output (x_out=x, say) that requires gradients is refused while these are recorded.
 # ---------------------------------------------------------------------------------------------------------------------
 GELU_TANH, SILU = 0, 1
 _ACTS = {"gelu": GELU_TANH, "silu": SILU}
-_tools = None
+_tools = _autograd = None
 
 
 def _layer_tools():
     """(torch, library, torch's types as RAVEL_*, (device -> its current stream's handle, the current device))"""
-    global _tools
+    global _tools, _autograd
     if _tools is None:
         import torch
 
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
             lambda device: torch.cuda.current_stream(device).cuda_stream)
         here = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device  # (there is a tensor on a GPU by then)
+        _autograd = torch.is_grad_enabled, (getattr(torch._C, "_increment_version", None) or torch.autograd.graph.increment_version)
         _tools = torch, load_library(), {torch.float32: F32, torch.bfloat16: BF16}, (raw, here)
     return _tools
+
+
+def _writes(outs):
+    """Tensors that the call is about to write."""
+    recording, written = _autograd
+    if recording():
+        for t in outs:
+            if t.requires_grad:
+                raise ValueError("an output that requires gradients would be written past automatic differentiation: detach it, "
+                                 "or call under torch.no_grad()")
+    written(outs)
 
 
 _HERE = contextlib.nullcontext()
@@ -711,7 +726,8 @@ def norm_residual(x, f=None, post=None, alpha=None, gate=None, scale=None, shift
 
     y has f's dtype (without f: that of a given y, or bfloat16).  ``post`` ``[width]`` and ``alpha`` (one number) are
     float32 tensors; ``gate``, ``scale`` and ``shift`` float32 ``[width]`` or ``[mods, width]``, of which row r uses
-    (r // group) % mods.  Without f, x_out is x itself.  x_out may be x.
+    (r // group) % mods.  Without f, x_out is x itself.  x_out may be x.  The results belong to no graph (norm_residual_grad has
+    their gradients).
     """
     torch, lib, types, _ = _tools or _layer_tools()
     if x.dim() != 2:
@@ -732,6 +748,7 @@ def norm_residual(x, f=None, post=None, alpha=None, gate=None, scale=None, shift
         fp, fs = _rows2("f", f, shape, T)
         yp, ys = _rows2("y", y, shape, T)
         op, os_ = _rows2("x_out", x_out, shape, S)
+        _writes((y,) if f is None else (y, x_out))
         _check(lib.ravel_norm_residual(_pack_norm(*sizes, mods, group, eps, 0, xp, fp, *ptr, op, yp, xs, fs, os_, ys, *stride),
                                        handle))
     return y, x if f is None else x_out
@@ -786,6 +803,7 @@ def norm_residual_grad(x_out, dy=None, d_out=None, f=None, post=None, alpha=None
         fields = (yp, dp, gx, gf, *gp, *tail)
         key = (sizes, mods, group, tuple(map(bool, gp)), tuple(map(bool, gs)))
         memory, ws, n = _scratch(lib.ravel_norm_residual_grad_workspace, x_out.device, key, (norm, ()), (_pack_norm_grad, fields))
+        _writes(tuple(out.values()))
         _check(lib.ravel_norm_residual_grad(norm, _pack_norm_grad(*fields, ws, n), handle))
     return out
 
@@ -813,7 +831,7 @@ def cross_attention(q, k, v, q_len=None, k_len=None, scale=None, out=None, lse=N
     """out = softmax(scale q k^T) v: q ``[batch, rows, n_q_heads, head_dim]`` over k, v ``[batch, keys, n_kv_heads,
     head_dim]`` of one dtype; the first ``k_len`` keys and ``q_len`` rows of each batch row take part (int32 tensors
     ``[batch]``; None: all), out is 0 for the other rows and where there are no keys.  ``lse``: float32 ``[batch,
-    n_q_heads, rows]`` that receives what the gradients need."""
+    n_q_heads, rows]`` that receives what the gradients need (cross_attention_grad; the result belongs to no graph)."""
     torch, lib, _, _ = _tools or _layer_tools()
     sizes = _cross_sizes(q, k, scale)
     guard, handle = _place(stream, q, k, v, q_len, k_len, out, lse)
@@ -830,6 +848,7 @@ def cross_attention(q, k, v, q_len=None, k_len=None, scale=None, out=None, lse=N
         fields = (*sizes, _lengths("q_len", q_len, sizes[1]), _lengths("k_len", k_len, sizes[1]), qp, kp, vp, op,
                   0 if lse is None else lse.data_ptr(), *qs, *ks, *vs, *os_)
         memory, ws, n = _scratch(lib.ravel_cross_attention_workspace, q.device, sizes, (_pack_cross, fields))
+        _writes((out,) if lse is None else (out, lse))
         _check(lib.ravel_cross_attention(_pack_cross(*fields, ws, n), handle))
     return out
 
@@ -867,6 +886,7 @@ def cross_attention_grad(q, k, v, out, lse, dout, q_len=None, k_len=None, scale=
         fields = (dp, gq, gk, gv, *ds, *gqs, *gks, *gvs)
         memory, ws, n = _scratch(lib.ravel_cross_attention_grad_workspace, q.device, (sizes, need_q, need_kv), (cross, ()),
                                  (_pack_cross_grad, fields))
+        _writes([t for t in (dq, dk, dv) if t is not None])
         _check(lib.ravel_cross_attention_grad(cross, _pack_cross_grad(*fields, ws, n), handle))
     return dq, dk, dv
 
@@ -893,7 +913,8 @@ def _pair(name, a, b, shape, dtype):
 
 def gated_mlp(x, wg, wu, act: str = "gelu", h=None, gate=None, up=None, stream=None):
     """h = act(x wg^T) * (x wu^T): x ``[rows, width]``, wg and wu ``[hidden, width]``, act "gelu" (tanh form) or "silu".
-    ``gate`` and ``up`` ``[rows, hidden]`` receive x wg^T and x wu^T, for the gradients."""
+    ``gate`` and ``up`` ``[rows, hidden]`` receive x wg^T and x wu^T, for the gradients (gated_mlp_grad; the result belongs to no
+    graph)."""
     torch, lib, _, _ = _tools or _layer_tools()
     sizes = _mlp_sizes(x, wg, wu, act)
     guard, handle = _place(stream, x, wg, wu, h, gate, up)
@@ -907,6 +928,7 @@ def gated_mlp(x, wg, wu, act: str = "gelu", h=None, gate=None, up=None, stream=N
         gp, up_, gs = _pair("gate and up", gate, up, shape, T)
         fields = (*sizes, xp, wp, vp, hp, gp, up_, xs, ws, hs, gs)
         memory, at, n = _scratch(lib.ravel_gated_mlp_workspace, x.device, sizes, (_pack_mlp, fields))
+        _writes((h,) if gate is None else (h, gate, up))
         _check(lib.ravel_gated_mlp(_pack_mlp(*fields, at, n), handle))
     return h
 
@@ -939,5 +961,6 @@ def gated_mlp_grad(x, wg, wu, gate, up, dh, act: str = "gelu", dx=None, dwg=None
         fields = (types.get(W, -1), 0, hp, dxp, dgp, dup, hs, dxs, dws)
         memory, at, n = _scratch(lib.ravel_gated_mlp_grad_workspace, x.device, (sizes, need_x, need_w), (mlp, ()),
                                  (_pack_mlp_grad, fields))
+        _writes([t for t in (dx, dwg, dwu) if t is not None])
         _check(lib.ravel_gated_mlp_grad(mlp, _pack_mlp_grad(*fields, at, n), handle))
     return dx, dwg, dwu
