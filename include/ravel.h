@@ -665,11 +665,14 @@ ravel_status ravel_cross_attention_grad_workspace(const ravel_cross* cross, cons
 ravel_status ravel_cross_attention_grad(const ravel_cross* cross, const ravel_cross_grad* grad, void* stream);
 
 /* 3. Gated MLP, up to its hidden values: h = act(x Wg^T) * (x Wu^T), products and activation in 32 bits.
- * gate and up, if given, receive x Wg^T and x Wu^T in dtype, for the gradients. */
-enum { RAVEL_GELU_TANH = 0, RAVEL_SILU = 1 };
+ * gate and up, if given, receive x Wg^T and x Wu^T, for the gradients: in dtype, or with RAVEL_GATE_F32 in
+ * 32 bits.  A bf16 call's gradients are 2.3e-3 off 64 bits with gate and up in 32 bits, 3.1e-3 in bf16, where
+ * rounding the results alone makes 1.7e-3. */
+enum { RAVEL_GELU_TANH = 0, RAVEL_SILU = 1, RAVEL_GATE_F32 = 256 };
 typedef struct {
   int32_t dtype;    /* RAVEL_F32 or RAVEL_BF16, of all tensors      */
-  int32_t act;      /* RAVEL_GELU_TANH or RAVEL_SILU                */
+  int32_t act;      /* RAVEL_GELU_TANH or RAVEL_SILU; | RAVEL_GATE_F32:
+                       gate and up are RAVEL_F32 whatever dtype     */
   int32_t rows;     /* 0 .. 2^28                                    */
   int32_t width;    /* of x: multiple of 8, <= 2^18                 */
   int32_t hidden;   /* of h: multiple of 8, <= 2^18                 */
@@ -691,8 +694,8 @@ ravel_status ravel_gated_mlp_workspace(const ravel_mlp* mlp, int64_t* bytes);
 ravel_status ravel_gated_mlp(const ravel_mlp* mlp, void* stream);
 
 /* Its gradients from dh, with gate and up as the call above left them; h is not read.  dx may be NULL,
- * and so may dwg and dwu together.  The gradients of gate and up, dh * up * act'(gate) and dh *
- * act(gate), are rounded to dtype before they are multiplied. */
+ * and so may dwg and dwu together.  act says what gate and up are, as above.  Their gradients, dh * up *
+ * act'(gate) and dh * act(gate), are rounded to dtype before they are multiplied. */
 typedef struct {
   int32_t weight_dtype; /* of dwg and dwu: dtype or RAVEL_F32 */
   int32_t reserved;     /* 0 */

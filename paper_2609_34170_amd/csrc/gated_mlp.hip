@@ -72,7 +72,8 @@ RAVEL_DEV void put_blocks(bf16_t* out, int64_t ld, int m0, int M, int n, int N, 
   put_two_rows(out, ld, m0 + (lane & 7), M, n + (lane & 8) * 4 + joined_column(lane), N, p, q);
 }
 
-// BM x BN outputs a block of WM x WN waves.  AC, BC: A, B lie as rows across the contraction.  O: type of the outputs.
+// BM x BN outputs a block of WM x WN waves.  AC, BC: A, B lie as rows across the contraction.  O: type of the outputs, G: of the
+// forward's gate and up values.
 //
 // What bounds it: a tile of 256 x 256 outputs and 64 contraction indices takes a CU 2048 clocks of matrix instructions and
 // 2048 of LDS traffic (192 KB of fragments read, 64 KB filled); the two overlap as far as the schedule below lets them, to
@@ -80,7 +81,7 @@ RAVEL_DEV void put_blocks(bf16_t* out, int64_t ld, int m0, int M, int n, int N, 
 // waves of 128 x 128 would read a third less but spill (1210 us instead of 484).  6400 rows, 2048 <-> 8192: forward 430 us
 // (1.00 PFLOP/s, with its three outputs; the products alone as one library call 403), dx 450 (0.95; 200 blocks for 256
 // CUs), dw 360 (1.19); 3200 rows, 1024 <-> 4096: 72, 63 + 10 for the ranges' sums, and 58.
-template <typename T, typename O, int BM, int BN, int WM, int WN, bool AC, bool BC, int MODE>
+template <typename T, typename O, typename G, int BM, int BN, int WM, int WN, bool AC, bool BC, int MODE>
 __global__ __launch_bounds__(64 * WM * WN) void mlp_matrix_kernel(MatArgs a) {
   typedef Mat<T> M;
   typedef typename M::frag frag;
@@ -214,7 +215,8 @@ __global__ __launch_bounds__(64 * WM * WN) void mlp_matrix_kernel(MatArgs a) {
         for (int k = 0; k < STEP / 2; ++k)
 #pragma unroll
           for (int r = 0; r < 4; ++r) h[k][r] = act_f(acc[i][j + 2 * k][r], a.act) * acc[i][j + 2 * k + 1][r];
-        O *const hidden = (O*)a.C[0], *const gate = (O*)a.C[1], *const up = (O*)a.C[2];
+        O* const hidden = (O*)a.C[0];
+        G *const gate = (G*)a.C[1], *const up = (G*)a.C[2];
         if constexpr (STEP == 4) {
           put_blocks(hidden, a.ldc, m, a.M, u, units, lane, h[0], h[1]);
           if (gate) {
@@ -255,7 +257,7 @@ __global__ __launch_bounds__(64 * WM * WN) void mlp_matrix_kernel(MatArgs a) {
 // units, its eight waves a range of the contraction each, with every weight of the range (up to 512 bytes a row) requested
 // before the first is used; the waves' sums meet in LDS.  Bound by HBM: one row, 2048 -> 8192, 13.0 us, 5.2 TB/s; 50 rows,
 // 1024 -> 4096, 8.3 us, of which the chain of loads, products and join is most.
-template <typename T, int MT>
+template <typename T, typename G, int MT>
 __global__ __launch_bounds__(512) void mlp_rows_kernel(MatArgs a) {
   typedef Mat<T> M;
   typedef typename M::frag frag;
@@ -305,8 +307,8 @@ __global__ __launch_bounds__(512) void mlp_rows_kernel(MatArgs a) {
   for (int r = 0; r < 4; ++r) h[r] = act_f(g[r], a.act) * u[r];
   put4((T*)a.C[0] + m * a.ldc + n, h);
   if (a.C[1]) {
-    put4((T*)a.C[1] + m * a.ldg + n, g);
-    put4((T*)a.C[2] + m * a.ldg + n, u);
+    put4((G*)a.C[1] + m * a.ldg + n, g);
+    put4((G*)a.C[2] + m * a.ldg + n, u);
   }
 }
 
@@ -327,8 +329,8 @@ __global__ __launch_bounds__(256) void mlp_sum_kernel(const float* part, int spl
 
 // The hidden gradients, dg = dh u act'(g) and du = dh act(g), [rows, hidden] each.  In bf16 calls they are rounded to it: they
 // are the operands of two matrix products, which take bf16, and written once instead of formed in each of the products' blocks.
-// With gate and up that makes 3.1e-3 against 64 bits where rounding the results alone gives 1.7e-3.  Bound by HBM: three
-// tensors read, two written, 6400 x 8192 in 95 to 102 us, 5.1 to 5.5 TB/s.
+// That makes 2.3e-3 against 64 bits where rounding the results alone gives 1.7e-3, and 3.1e-3 where gate and up (G) are bf16
+// as well: the caller's choice.  Bound by HBM: three tensors read, two written, 6400 x 8192 in 95 to 102 us, 5.1 to 5.5 TB/s.
 RAVEL_DEV void act_grad(float x, int kind, float& y, float& slope) {
   if (kind == RAVEL_SILU) {
     const float s = 1.f / (1.f + __expf(-x));
@@ -362,7 +364,7 @@ RAVEL_DEV void put8(float* p, const float (&v)[8]) {
 RAVEL_DEV void put8(bf16_t* p, const float (&v)[8]) {
   *(u32x4_t*)p = u32x4_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
 }
-template <typename T>
+template <typename T, typename G>
 __global__ __launch_bounds__(256) void mlp_hidden_grad_kernel(ravel_mlp a, ravel_mlp_grad g, T* dg, T* du) {
   const int n8 = a.hidden / 8;
   const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -370,8 +372,8 @@ __global__ __launch_bounds__(256) void mlp_hidden_grad_kernel(ravel_mlp a, ravel
   const int64_t m = id / n8;
   const int n = (int)(id - m * n8) * 8;
   float x[8], u[8], dh[8];
-  get8((const T*)a.gate + m * a.gate_stride + n, x);
-  get8((const T*)a.up + m * a.gate_stride + n, u);
+  get8((const G*)a.gate + m * a.gate_stride + n, x);
+  get8((const G*)a.up + m * a.gate_stride + n, u);
   get8((const T*)g.dh + m * g.dh_stride + n, dh);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
@@ -420,21 +422,21 @@ MatPlan plan_matrix(int64_t M, int64_t N, int64_t K, int pairs, int products, in
   return best;
 }
 
-template <typename T, typename O, bool AC, bool BC, int MODE>
+template <typename T, typename O, bool AC, bool BC, int MODE, typename G = O>
 hipError_t launch_matrix(const MatArgs& a, int tile, hipStream_t s) {
   const int64_t blocks = (int64_t)ceil_div(a.M, kTile[tile]) * ceil_div(a.N, kTile[tile]) * a.splits * (MODE == BOTH ? 2 : 1);
   const dim3 grid((unsigned)blocks);
   if (tile == 0) {
-    if constexpr (sizeof(T) == 2) mlp_matrix_kernel<T, O, 256, 256, 2, 4, AC, BC, MODE><<<grid, 512, 0, s>>>(a);
+    if constexpr (sizeof(T) == 2) mlp_matrix_kernel<T, O, G, 256, 256, 2, 4, AC, BC, MODE><<<grid, 512, 0, s>>>(a);
   } else if (tile == 1) {
-    mlp_matrix_kernel<T, O, 128, 128, 2, 2, AC, BC, MODE><<<grid, 256, 0, s>>>(a);
+    mlp_matrix_kernel<T, O, G, 128, 128, 2, 2, AC, BC, MODE><<<grid, 256, 0, s>>>(a);
   } else {
-    mlp_matrix_kernel<T, O, 64, 64, 2, 2, AC, BC, MODE><<<grid, 256, 0, s>>>(a);
+    mlp_matrix_kernel<T, O, G, 64, 64, 2, 2, AC, BC, MODE><<<grid, 256, 0, s>>>(a);
   }
   return hipGetLastError();
 }
 
-template <typename T>
+template <typename T, typename G>
 hipError_t forward(const ravel_mlp& m, hipStream_t s) {
   MatArgs a{};
   a.A[0] = m.x;
@@ -454,9 +456,9 @@ hipError_t forward(const ravel_mlp& m, hipStream_t s) {
   a.act = m.act;
   if (a.M <= 64) {
     const dim3 grid((unsigned)ceil_div(m.hidden, 16));
-    if (a.M <= 16) mlp_rows_kernel<T, 1><<<grid, 512, 0, s>>>(a);
-    else if (a.M <= 32) mlp_rows_kernel<T, 2><<<grid, 512, 0, s>>>(a);
-    else mlp_rows_kernel<T, 4><<<grid, 512, 0, s>>>(a);
+    if (a.M <= 16) mlp_rows_kernel<T, G, 1><<<grid, 512, 0, s>>>(a);
+    else if (a.M <= 32) mlp_rows_kernel<T, G, 2><<<grid, 512, 0, s>>>(a);
+    else mlp_rows_kernel<T, G, 4><<<grid, 512, 0, s>>>(a);
     return hipGetLastError();
   }
   // Blocks of 256 x 256 run one a CU, in rounds: the rows behind the last full round go into a launch of smaller tiles where
@@ -477,14 +479,14 @@ hipError_t forward(const ravel_mlp& m, hipStream_t s) {
   a.M = first;
   a.splits = p.splits;
   a.per = p.per;
-  const hipError_t e = launch_matrix<T, T, false, false, FORWARD>(a, p.tile, s);
+  const hipError_t e = launch_matrix<T, T, false, false, FORWARD, G>(a, p.tile, s);
   if (e != hipSuccess || first == all) return e;
   a.M = all - first;
   a.per = rest.per;
   a.A[0] = (const T*)a.A[0] + first * a.lda;
   a.C[0] = (T*)a.C[0] + first * a.ldc;
-  if (a.C[1]) a.C[1] = (T*)a.C[1] + first * a.ldg, a.C[2] = (T*)a.C[2] + first * a.ldg;
-  return launch_matrix<T, T, false, false, FORWARD>(a, rest.tile, s);
+  if (a.C[1]) a.C[1] = (G*)a.C[1] + first * a.ldg, a.C[2] = (G*)a.C[2] + first * a.ldg;
+  return launch_matrix<T, T, false, false, FORWARD, G>(a, rest.tile, s);
 }
 
 struct GradBytes {
@@ -515,7 +517,7 @@ hipError_t add_ranges(const MatArgs& a, int products, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <typename T>
+template <typename T, typename G>
 hipError_t gradients(const ravel_mlp& m, const ravel_mlp_grad& g, hipStream_t s) {
   const GradBytes b = grad_bytes(m, g);
   char* const ws = (char*)g.workspace;
@@ -523,7 +525,7 @@ hipError_t gradients(const ravel_mlp& m, const ravel_mlp_grad& g, hipStream_t s)
   float* const part = (float*)(ws + 2 * b.hidden);
   hipError_t e;
   if (m.rows > 0) {
-    mlp_hidden_grad_kernel<T><<<ceil_div((int64_t)m.rows * (m.hidden / 8), 256), 256, 0, s>>>(m, g, dg, du);
+    mlp_hidden_grad_kernel<T, G><<<ceil_div((int64_t)m.rows * (m.hidden / 8), 256), 256, 0, s>>>(m, g, dg, du);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (g.dx && m.rows > 0) {
@@ -565,17 +567,23 @@ hipError_t gradients(const ravel_mlp& m, const ravel_mlp_grad& g, hipStream_t s)
 }  // namespace
 
 size_t mlp_workspace(const ravel_mlp&) { return 0; }
-hipError_t launch_gated_mlp(const ravel_mlp& m, hipStream_t s) {
+hipError_t launch_gated_mlp(ravel_mlp m, hipStream_t s) {
   if (m.rows == 0) return hipSuccess;
-  return m.dtype == RAVEL_F32 ? forward<float>(m, s) : forward<bf16_t>(m, s);
+  const bool wide = m.act & RAVEL_GATE_F32;
+  m.act &= ~RAVEL_GATE_F32;
+  return m.dtype == RAVEL_F32 ? forward<float, float>(m, s) : wide ? forward<bf16_t, float>(m, s) : forward<bf16_t, bf16_t>(m, s);
 }
 size_t mlp_grad_workspace(const ravel_mlp& m, const ravel_mlp_grad& g) {
   const GradBytes b = grad_bytes(m, g);
   return 2 * b.hidden + b.part;
 }
-hipError_t launch_gated_mlp_grad(const ravel_mlp& m, const ravel_mlp_grad& g, hipStream_t s) {
+hipError_t launch_gated_mlp_grad(ravel_mlp m, const ravel_mlp_grad& g, hipStream_t s) {
   if (!g.dx && !g.dwg) return hipSuccess;
-  return m.dtype == RAVEL_F32 ? gradients<float>(m, g, s) : gradients<bf16_t>(m, g, s);
+  const bool wide = m.act & RAVEL_GATE_F32;
+  m.act &= ~RAVEL_GATE_F32;
+  return m.dtype == RAVEL_F32 ? gradients<float, float>(m, g, s)
+         : wide               ? gradients<bf16_t, float>(m, g, s)
+                              : gradients<bf16_t, bf16_t>(m, g, s);
 }
 
 }  // namespace ravel

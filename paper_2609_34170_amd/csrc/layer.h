@@ -27,8 +27,8 @@ size_t cross_grad_workspace(const ravel_cross& c, const ravel_cross_grad& g);
 hipError_t launch_cross_attention_grad(const ravel_cross& c, const ravel_cross_grad& g, hipStream_t s);
 
 size_t mlp_workspace(const ravel_mlp& m);
-hipError_t launch_gated_mlp(const ravel_mlp& m, hipStream_t s);
+hipError_t launch_gated_mlp(ravel_mlp m, hipStream_t s);
 size_t mlp_grad_workspace(const ravel_mlp& m, const ravel_mlp_grad& g);
-hipError_t launch_gated_mlp_grad(const ravel_mlp& m, const ravel_mlp_grad& g, hipStream_t s);
+hipError_t launch_gated_mlp_grad(ravel_mlp m, const ravel_mlp_grad& g, hipStream_t s);
 
 }  // namespace ravel

@@ -239,7 +239,8 @@ void mlp_sizes(Check& k, const ravel_mlp* m) {
   k.valid(m, "null struct");
   if (!k.ok()) return;
   k.dtype(m->dtype);
-  k.valid(m->act == RAVEL_GELU_TANH || m->act == RAVEL_SILU, "act must be RAVEL_GELU_TANH or RAVEL_SILU");
+  const int32_t kind = m->act & ~RAVEL_GATE_F32;
+  k.valid(kind == RAVEL_GELU_TANH || kind == RAVEL_SILU, "act must be RAVEL_GELU_TANH or RAVEL_SILU, with or without RAVEL_GATE_F32");
   k.valid(m->reserved == 0, "reserved must be 0");
   k.shape(m->rows >= 0 && m->rows <= 1 << 28, "rows must be in 0..2^28");
   k.shape(m->width >= 8 && m->width <= 1 << 18 && m->width % 8 == 0, "width must be a multiple of 8 in 8..2^18");
@@ -250,6 +251,7 @@ void mlp_rows(Check& k, int64_t n, int64_t stride, int64_t inner, int elt, bool 
   k.rows(n, stride, inner, elt, output);
   if (n > 1) k.shape(stride * elt <= 1 << 22, "strides must be at most 2^22 bytes");
 }
+int gate_bytes(const ravel_mlp* m) { return m->act & RAVEL_GATE_F32 ? 4 : bytes_of(m->dtype); }
 void mlp_inputs(Check& k, const ravel_mlp* m) {
   const int e = bytes_of(m->dtype);
   k.aligned({m->x, m->wg, m->wu, m->h, m->gate, m->up});
@@ -265,7 +267,7 @@ ravel_status mlp_call(const ravel_mlp* m, hipStream_t s) {
   const int e = bytes_of(m->dtype);
   mlp_rows(k, m->rows, m->h_stride, m->hidden, e, true);
   k.valid(!m->gate == !m->up, "gate and up go together");
-  if (m->gate) mlp_rows(k, m->rows, m->gate_stride, m->hidden, e, true);
+  if (m->gate) mlp_rows(k, m->rows, m->gate_stride, m->hidden, gate_bytes(m), true);
   if (!k.ok() || m->rows == 0) return k.status;
   k.present({m->x, m->wg, m->wu, m->h});
   k.apart({m->h, m->gate, m->up, m->x, m->wg, m->wu}, 3);
@@ -289,7 +291,7 @@ ravel_status mlp_grad_call(const ravel_mlp* m, const ravel_mlp_grad* g, hipStrea
   if (!k.ok()) return k.status;
   mlp_inputs(k, m);
   const int e = bytes_of(m->dtype);
-  mlp_rows(k, m->rows, m->gate_stride, m->hidden, e, false);
+  mlp_rows(k, m->rows, m->gate_stride, m->hidden, gate_bytes(m), false);
   mlp_rows(k, m->rows, g->dh_stride, m->hidden, e, false);
   if (g->dx) mlp_rows(k, m->rows, g->dx_stride, m->width, e, true);
   if (g->dwg) mlp_rows(k, m->hidden, g->dw_stride, m->width, bytes_of(g->weight_dtype), true);
