@@ -329,11 +329,13 @@ def _own(s):
         ravel.cross_attention_grad(s["q"], s["k"], s["v"], s["out"], s["lse"], s["dout"], k_len=s["k_len"], dq=s["dq"],
                                    dk=s["dk"], dv=s["dv"])
         return {x: s[x] for x in ("out", "dq", "dk", "dv")}
-    ravel.gated_mlp(s["x"], s["wg"], s["wu"], act=c["act"], h=s["h"], gate=s.get("g"), up=s.get("u"))
     if not c["train"]:
+        ravel.gated_mlp(s["x"], s["wg"], s["wu"], act=c["act"], h=s["h"])
         return {"h": s["h"]}
-    ravel.gated_mlp_grad(s["x"], s["wg"], s["wu"], s["g"], s["u"], s["dh"], act=c["act"], dx=s["dx"], dwg=s["dwg"],
-                         dwu=s["dwu"])
+    # what the gradients go on from stays in 32 bits, as in the plain form
+    gate, up = (t if t.dtype is torch.float32 else torch.empty(t.shape, device=DEV) for t in (s["g"], s["u"]))
+    ravel.gated_mlp(s["x"], s["wg"], s["wu"], act=c["act"], h=s["h"], gate=gate, up=up)
+    ravel.gated_mlp_grad(s["x"], s["wg"], s["wu"], gate, up, s["dh"], act=c["act"], dx=s["dx"], dwg=s["dwg"], dwu=s["dwu"])
     return {x: s[x] for x in ("h", "dx", "dwg", "dwu")}
 
 
