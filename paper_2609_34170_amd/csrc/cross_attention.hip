@@ -13,9 +13,15 @@
 //
 // What bounds it with many rows: LDS.  Each of the four waves reads the fragments of a tile's 64 keys, and with the next
 // tile's fill that takes 1.2 to 1.4 times as long as the products; exponentials come in between, and two waves a SIMD, all
-// that the sums leave registers for, cover each other in part: matrix instructions are busy 43 to 46 % of the time.  16 x
-// 800 rows of 16 heads over 2048 keys of 4 heads, 128 dims: forward 247 us (870 TFLOP/s), dq 336 (959), dk and dv 379
-// (1133); with lengths of 512 to 2048 and one of 0 150, 200 and 355.
+// that the sums leave registers for, cover each other in part: matrix instructions are busy 45 % of the time in the forward, 50 %
+// for dq, 54 % for dk and dv.  16 x 800 rows of 16 heads over 2048 keys of 4 heads, 128 dims: forward 250 us (860 TFLOP/s), dq 341
+// (945), dk and dv 384 (1118); with lengths of 512 to 2048 and one of 0, 144, 202 and 346.  The last does not shrink as the
+// keys do: its 1024 blocks of 128 keys are equally long, some 630 of them live, which is two rounds of 512, the second a quarter full.
+//
+// What a bf16 call rounds: probabilities before p v and p^T dout, the scores' gradients before ds k and ds^T q (operands of
+// bf16 matrix instructions; 2.3e-3 off 64 bits with the results' own rounding, which alone makes 1.7e-3), and D takes out as the
+// forward has rounded it: exact sums would need the keys once more.  That is little where many keys share the weight, and
+// most of the error where one key has it all (a mean largest probability of 0.89: 5.9e-3).  Calls in 32 bits round nothing between.
 #include <algorithm>
 
 #include "layer.h"
@@ -116,8 +122,9 @@ RAVEL_DEV void load_keys(const Segments<T, HD * sizeof(T)>& at, const T* head, i
     load_segment(from, tile, seg, row + at.byte_of(seg) + seg * at.ROWS * step);
   }
 }
-// Rows [first, first + TR) of a (batch row, KV head)'s row space; rows from `end` on are zeros, or with REPEAT the last row (there
-// is one) again.  head: row 0 of the first query head.  Quotients by G through its reciprocal `inv` = ceil(2^23 / G), exact for what is below 2^23 / G.
+// Rows [first, first + TR) of a (batch row, KV head)'s row space; rows from `end` on are zeros, or with REPEAT the last row
+// (there is one) again.  head: row 0 of the first query head.  Quotients by G through its reciprocal `inv` = ceil(2^23 / G), exact
+// for what is below 2^23 / G.
 struct RowSpace {
   int G, inv;
 };
@@ -141,7 +148,8 @@ RAVEL_DEV void load_rows(const Segments<T, HD * sizeof(T)>& at, const T* head, i
 // forward
 // ---------------------------------------------------------------------------
 // Four waves: KW of them share 16 MI rows and split a tile's keys between them (few rows), 4 / KW groups of rows.  Few rows
-// are bound by HBM: 64 batch rows of one row over up to 4096 keys, 66 us and 6 to join the ranges, 5.1 TB/s.
+// are bound by HBM: 64 batch rows of one row over up to 4096 keys, 64 us and 6 to join the ranges, 5.2 TB/s, where a bare read of
+// 320 MB has 6.5.
 template <typename T, int HD, int MI, int KW, int TK>
 __global__ __launch_bounds__(256, (4 * Tiles<T, HD, TK>::BYTES <= 65536 ? 2 : 1)) void cross_kernel(CrossArgs a) {
   typedef Tiles<T, HD, TK> Z;

@@ -79,8 +79,8 @@ RAVEL_DEV void put_blocks(bf16_t* out, int64_t ld, int m0, int M, int n, int N, 
 // 2048 of LDS traffic (192 KB of fragments read, 64 KB filled); the two overlap as far as the schedule below lets them, to
 // 3400.  256 x 256 is the largest tile whose sums and two steps' fragments fit the registers of two waves a SIMD; four
 // waves of 128 x 128 would read a third less but spill (1210 us instead of 484).  6400 rows, 2048 <-> 8192: forward 430 us
-// (1.00 PFLOP/s, with its three outputs; the products alone as one library call 403), dx 450 (0.95; 200 blocks for 256
-// CUs), dw 360 (1.19); 3200 rows, 1024 <-> 4096: 72, 63 + 10 for the ranges' sums, and 58.
+// (1.00 PFLOP/s, with its three outputs in bf16; 458 with gate and up in 32 bits; the products alone as one library call 398), dx
+// 441 (0.97; 200 blocks for 256 CUs), dw 359 (1.20); 3200 rows, 1024 <-> 4096: 72 (80), 63 + 10 for the ranges' sums, and 62.
 template <typename T, typename O, typename G, int BM, int BN, int WM, int WN, bool AC, bool BC, int MODE>
 __global__ __launch_bounds__(64 * WM * WN) void mlp_matrix_kernel(MatArgs a) {
   typedef Mat<T> M;
@@ -255,8 +255,9 @@ __global__ __launch_bounds__(64 * WM * WN) void mlp_matrix_kernel(MatArgs a) {
 
 // Few rows (up to 16 MT): the weights are all there is to read, once, so nothing is staged.  A block takes 16 hidden
 // units, its eight waves a range of the contraction each, with every weight of the range (up to 512 bytes a row) requested
-// before the first is used; the waves' sums meet in LDS.  Bound by HBM: one row, 2048 -> 8192, 13.0 us, 5.2 TB/s; 50 rows,
-// 1024 -> 4096, 8.3 us, of which the chain of loads, products and join is most.
+// before the first is used; the waves' sums meet in LDS.  Bound by memory: one row, 2048 -> 8192, 12.6 us for 67 MB, where a bare
+// read of as much takes 10.2 (the same again and again, from cache) to 11.3 (other memory each time); 50 rows, 1024 -> 4096,
+// 8.1 us, of which the chain of loads, products and join is most.
 template <typename T, typename G, int MT>
 __global__ __launch_bounds__(512) void mlp_rows_kernel(MatArgs a) {
   typedef Mat<T> M;
@@ -330,7 +331,8 @@ __global__ __launch_bounds__(256) void mlp_sum_kernel(const float* part, int spl
 // The hidden gradients, dg = dh u act'(g) and du = dh act(g), [rows, hidden] each.  In bf16 calls they are rounded to it: they
 // are the operands of two matrix products, which take bf16, and written once instead of formed in each of the products' blocks.
 // That makes 2.3e-3 against 64 bits where rounding the results alone gives 1.7e-3, and 3.1e-3 where gate and up (G) are bf16
-// as well: the caller's choice.  Bound by HBM: three tensors read, two written, 6400 x 8192 in 95 to 102 us, 5.1 to 5.5 TB/s.
+// as well: the caller's choice.  Bound by HBM: three tensors read, two written, 6400 x 8192 in 150 us, 4.9 TB/s (with gate and
+// up in bf16 95 to 102 us, 5.1 to 5.5 TB/s).
 RAVEL_DEV void act_grad(float x, int kind, float& y, float& slope) {
   if (kind == RAVEL_SILU) {
     const float s = 1.f / (1.f + __expf(-x));
