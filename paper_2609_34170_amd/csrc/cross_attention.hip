@@ -108,18 +108,17 @@ struct Tiles {
   static constexpr int RB = HD * sizeof(T), BYTES = ROWS * RB, SEGS = (BYTES + 4095) / 4096;  // segments per wave
 };
 
-// Keys [first, first + TK) of one head into a tile; keys behind the head's last `bytes` are zeros.
+// Keys [first, first + TK) of one head into a tile; keys from `end` on are zeros (by their index: their memory may be a live key's).
 template <typename T, int HD, int TK>
-RAVEL_DEV void load_keys(const Segments<T, HD * sizeof(T)>& at, const T* head, int64_t bytes, int stride, int first, char* tile, int wave) {
+RAVEL_DEV void load_keys(const Segments<T, HD * sizeof(T)>& at, const T* head, int stride, int first, int end, char* tile, int wave) {
   typedef Tiles<T, HD, TK> Z;
-  const int step = stride * (int)sizeof(T), row = __umul24(at.row, step);
-  const int64_t skip = (int64_t)first * step;
-  const rsrc_t from = buffer_from((const char*)head + skip, bytes - skip);
+  const unsigned step = (unsigned)stride * (unsigned)sizeof(T), row = __umul24(at.row, step);
+  const rsrc_t from = buffer_from((const char*)head + (int64_t)first * (int)step);
 #pragma unroll
   for (int i = 0; i < Z::SEGS; ++i) {
     const int seg = wave * Z::SEGS + i;
     if (Z::BYTES % 4096 && seg * 1024 >= Z::BYTES) break;
-    load_segment(from, tile, seg, row + at.byte_of(seg) + seg * at.ROWS * step);
+    load_segment(from, tile, seg, seg * at.ROWS + at.row < end - first ? row + at.byte_of(seg) + seg * at.ROWS * step : kOutside);
   }
 }
 // Rows [first, first + TR) of a (batch row, KV head)'s row space; rows from `end` on are zeros, or with REPEAT the last row
@@ -176,13 +175,11 @@ __global__ __launch_bounds__(256, (4 * Tiles<T, HD, TK>::BYTES <= 65536 ? 2 : 1)
   const T* const q = (const T*)c.q + w.b * c.q_stride[0] + (int64_t)w.h * a.G * c.q_stride[2];
   const T* const k = (const T*)c.k + w.b * c.k_stride[0] + w.h * c.k_stride[2];
   const T* const v = (const T*)c.v + w.b * c.v_stride[0] + w.h * c.v_stride[2];
-  const int64_t k_bytes = ((int64_t)(klen - 1) * (int)c.k_stride[1] + HD) * sizeof(T);
-  const int64_t v_bytes = ((int64_t)(klen - 1) * (int)c.v_stride[1] + HD) * sizeof(T);
   const Segments<T, RB> seg0(lane);
   const auto issue = [&](int t, char* kt, char* vt) {
     const auto seg = seg0.fresh();
-    load_keys<T, HD, TK>(seg, k, k_bytes, (int)c.k_stride[1], t * TK, kt, wave);
-    load_keys<T, HD, TK>(seg, v, v_bytes, (int)c.v_stride[1], t * TK, vt, wave);
+    load_keys<T, HD, TK>(seg, k, (int)c.k_stride[1], t * TK, klen, kt, wave);
+    load_keys<T, HD, TK>(seg, v, (int)c.v_stride[1], t * TK, klen, vt, wave);
   };
   if (t0 < t1) issue(t0, k0, v0);
 
@@ -393,13 +390,11 @@ __global__ __launch_bounds__(256, (4 * Tiles<T, HD, TK>::BYTES <= 65536 ? 2 : 1)
 
   const T* const k = (const T*)c.k + w.b * c.k_stride[0] + w.h * c.k_stride[2];
   const T* const v = (const T*)c.v + w.b * c.v_stride[0] + w.h * c.v_stride[2];
-  const int64_t k_bytes = ((int64_t)(klen - 1) * (int)c.k_stride[1] + HD) * sizeof(T);
-  const int64_t v_bytes = ((int64_t)(klen - 1) * (int)c.v_stride[1] + HD) * sizeof(T);
   const Segments<T, RB> seg0(lane);
   const auto issue = [&](int t, char* kt, char* vt) {
     const auto seg = seg0.fresh();
-    load_keys<T, HD, TK>(seg, k, k_bytes, (int)c.k_stride[1], t * TK, kt, wave);
-    load_keys<T, HD, TK>(seg, v, v_bytes, (int)c.v_stride[1], t * TK, vt, wave);
+    load_keys<T, HD, TK>(seg, k, (int)c.k_stride[1], t * TK, klen, kt, wave);
+    load_keys<T, HD, TK>(seg, v, (int)c.v_stride[1], t * TK, klen, vt, wave);
   };
   if (t0 < t1) issue(t0, k0, v0);
 
@@ -744,8 +739,8 @@ __global__ __launch_bounds__(256) void cross_few_keys_grad_kernel(CrossArgs a) {
   const T* const dout = (const T*)g.dout + w.b * g.dout_stride[0] + (int64_t)w.h * a.G * g.dout_stride[2];
   const RowSpace space{a.G, ((1 << 23) + a.G - 1) / a.G};
   const Segments<T, RB> seg(lane);
-  load_keys<T, HD, 32>(seg, k, ((int64_t)(klen - 1) * (int)c.k_stride[1] + HD) * E, (int)c.k_stride[1], 0, kt, wave);
-  load_keys<T, HD, 32>(seg, v, ((int64_t)(klen - 1) * (int)c.v_stride[1] + HD) * E, (int)c.v_stride[1], 0, vt, wave);
+  load_keys<T, HD, 32>(seg, k, (int)c.k_stride[1], 0, klen, kt, wave);
+  load_keys<T, HD, 32>(seg, v, (int)c.v_stride[1], 0, klen, vt, wave);
   const TileLane<T, RB> at0(lane);
   const TileLane<T, PB> ap0(lane);
   const float cs = c.scale > 0.f ? c.scale * kLog2e : 1.f;
@@ -942,12 +937,6 @@ struct Plan {
 };
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
-// A single key's stride is of no account to the caller, but says where a tile's next rows, zeros, would lie.
-ravel_cross with_key_strides(ravel_cross c) {
-  if (c.keys == 1) c.k_stride[1] = c.v_stride[1] = c.head_dim;
-  return c;
-}
-
 template <typename T, int HD>
 Plan plan_forward(const ravel_cross& c) {
   typedef Shape<T, HD> S;
@@ -968,7 +957,7 @@ hipError_t forward(const ravel_cross& c, hipStream_t s) {
   typedef Shape<T, HD> S;
   const Plan p = plan_forward<T, HD>(c);
   CrossArgs a{};
-  a.c = with_key_strides(c);
+  a.c = c;
   a.G = c.n_q_heads / c.n_kv_heads;
   a.tiles = p.tiles;
   a.splits = p.splits;
@@ -1051,7 +1040,7 @@ hipError_t gradients(const ravel_cross& c, const ravel_cross_grad& g, hipStream_
   typedef Shape<T, HD> S;
   const GradPlan p = plan_grad<T, HD>(c, g);
   CrossArgs a{};
-  a.c = with_key_strides(c);
+  a.c = c;
   a.g = g;
   a.G = c.n_q_heads / c.n_kv_heads;
   a.padded = p.padded;

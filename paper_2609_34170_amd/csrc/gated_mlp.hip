@@ -108,7 +108,7 @@ __global__ __launch_bounds__(64 * WM * WN) void mlp_matrix_kernel(MatArgs a) {
 
   // An operand's rows are its own (AC false) or the contraction's; behind its last element are zeros.  Columns
   // behind a row's end read the next row: across the contraction they are outputs that are not stored, along it (the
-  // last tile) they are cut off.
+  // last tile) they are cut off.  So are, by their index, rows behind the contraction's end (their memory may be a live row's).
   const Segments<T, RA> sa0(lane);
   const Segments<T, RBB> sb0(lane);
   const int lda = (int)a.lda * E, ldb = (int)a.ldb * E;
@@ -122,13 +122,13 @@ __global__ __launch_bounds__(64 * WM * WN) void mlp_matrix_kernel(MatArgs a) {
   const auto issue = [&](int t, char* Ad, char* Bd) {  // behind the last tile: zeros
     const auto sa = sa0.fresh();
     const auto sb = sb0.fresh();
-    const int pair = t >= tiles_k ? 1 : 0, kt = t - pair * tiles_k, left = a.K * E - kt * 128;
+    const int pair = t >= tiles_k ? 1 : 0, kt = t - pair * tiles_k, left = a.K * E - kt * 128, rows = a.K - kt * BK;
     const rsrc_t fa = buffer_from((const char*)a.A[MODE == BOTH ? which : pair] + a_first + kt * a_next, t < k1 ? a_left - kt * a_next : 0);
     const int ra = __umul24(sa.row, lda), rb = __umul24(sb.row, ldb);
 #pragma unroll
     for (int i = 0; i < SA; ++i) {
       const int seg = wave * SA + i, c = sa.byte_of(seg);
-      load_segment(fa, Ad, seg, AC || c < left ? ra + c + seg * sa.ROWS * lda : kOutside);
+      load_segment(fa, Ad, seg, (AC ? seg * sa.ROWS + sa.row < rows : c < left) ? ra + c + seg * sa.ROWS * lda : kOutside);
     }
     const rsrc_t fb = buffer_from((const char*)a.B[MODE == STORE ? pair : 0] + b_first + kt * b_next, t < k1 ? b_left - kt * b_next : 0);
     if constexpr (MODE == FORWARD) {  // rows 32 j .. + 15 of the tile: gate, the next 16: up weights of the same units
@@ -142,7 +142,7 @@ __global__ __launch_bounds__(64 * WM * WN) void mlp_matrix_kernel(MatArgs a) {
 #pragma unroll
       for (int i = 0; i < SB; ++i) {
         const int seg = wave * SB + i, c = sb.byte_of(seg);
-        load_segment(fb, Bd, seg, BC || c < left ? rb + c + seg * sb.ROWS * ldb : kOutside);
+        load_segment(fb, Bd, seg, (BC ? seg * sb.ROWS + sb.row < rows : c < left) ? rb + c + seg * sb.ROWS * ldb : kOutside);
       }
     }
   };
@@ -550,7 +550,7 @@ hipError_t gradients(const ravel_mlp& m, const ravel_mlp_grad& g, hipStream_t s)
     a.A[0] = dg, a.A[1] = du;
     a.B[0] = m.x;
     a.lda = m.hidden;
-    a.ldb = m.rows > 1 ? m.x_stride : m.width;  // (one row has no stride, but where the next, zeros, would lie)
+    a.ldb = m.rows > 1 ? m.x_stride : m.width;  // (one row has no stride)
     a.M = m.hidden, a.N = m.width, a.K = m.rows, a.pairs = 1;
     a.C[0] = g.dwg, a.C[1] = g.dwu;
     a.ldc = g.dw_stride;
