@@ -332,8 +332,10 @@ def _own(s):
     if not c["train"]:
         ravel.gated_mlp(s["x"], s["wg"], s["wu"], act=c["act"], h=s["h"])
         return {"h": s["h"]}
-    # what the gradients go on from stays in 32 bits, as in the plain form
-    gate, up = (t if t.dtype is torch.float32 else torch.empty(t.shape, device=DEV) for t in (s["g"], s["u"]))
+    # what the gradients go on from stays in 32 bits, as in the plain form, in memory that a program keeps as it keeps h's
+    if s["g"].dtype is not torch.float32:
+        s["g"], s["u"] = (torch.empty(t.shape, device=DEV) for t in (s["g"], s["u"]))
+    gate, up = s["g"], s["u"]
     ravel.gated_mlp(s["x"], s["wg"], s["wu"], act=c["act"], h=s["h"], gate=gate, up=up)
     ravel.gated_mlp_grad(s["x"], s["wg"], s["wu"], gate, up, s["dh"], act=c["act"], dx=s["dx"], dwg=s["dwg"], dwu=s["dwu"])
     return {x: s[x] for x in ("h", "dx", "dwg", "dwu")}
