@@ -615,7 +615,8 @@ ravel_status ravel_norm_residual_grad(const ravel_norm* norm, const ravel_norm_g
  * calls probabilities (and in the gradients the scores') are rounded to bf16 before they are
  * multiplied, outputs at the end, and the gradients take out as it was rounded (but not for up to 32
  * keys): results are 2.3e-3 off 64 bits where rounding them alone makes 1.7e-3, gradients of rows that
- * one key dominates up to 5.9e-3.  Calls in RAVEL_F32 round nothing in between (4e-7).  scale is 0 or in 2^-100..2^100. */
+ * one key dominates up to 5.9e-3.  Calls in RAVEL_F32 round nothing in between (4e-7 and 7e-6).  scale
+ * is 0 or in 2^-100..2^100. */
 typedef struct {
   int32_t dtype; /* RAVEL_F32 or RAVEL_BF16: q, k, v, out and their gradients */
   int32_t batch;
